@@ -511,6 +511,66 @@ int o5_surgery_fold_input(int D, int H, int A1, int Dk, const float* E,
                           float* v_new, void* stream);
 
 /* ------------------------------------------------------------------------
+ * o5_linattn_fwd / _bwd / _step -- linear attention with a decay for each
+ * head: a recurrent core whose state is a matrix and whose steps need not be
+ * run one after another, for a policy that trains on whole segments instead
+ * of short samples.  State head n of sample b (shared by the nh / nkv query
+ * heads h = n nh/nkv ... of its group; d_n = decay[n]):
+ *
+ *   S_t = d_n (1 - reset[t,b]) S_{t-1} + k_t v_t^T        (S_{-1} = S0)
+ *   o_{t,h} = scale S_t^T q_{t,h}
+ *
+ * dt       type of q, k, v, o and of dout, dq, dk, dv.
+ * T, B     steps and samples, >= 1, T*B below 2^31.   nh: query heads, a
+ *          multiple of nkv, the key/value and state heads; B*nh below 2^24.
+ * dk, dv   widths of a key (and query) and of a value, multiples of 8 in
+ *          8..128.
+ * q        head h of row t*B + b at q + (t*B + b)*ldq + h*dk.   k, v: the
+ *          same with nkv heads of dk and dv.   o: nh heads of dv.  Row strides
+ *          ld* in elements: multiples of 8, at least the heads' width and
+ *          below 2^31, so that q, k and v may be parts of one wider buffer.
+ * decay    [nkv] fp32 in [0, 1] (not checked; it is a constant of the head:
+ *          no gradient is taken).   scale: finite, on the outputs.
+ * S0       [B, nkv, dk, dv] fp32, the states before the first step, or NULL
+ *          (= 0).   ST: out, the states after the last step, or NULL.
+ * reset    [T, B] uint8 or NULL (no resets): nonzero cuts the carried state
+ *          off before step t, whatever it held, infinities and NaN too.
+ * ws       scratch of o5_linattn_*_workspace_bytes(...) bytes.
+ *
+ * o5_linattn_bwd differentiates J = sum_t <dout_t, o_t> + <dST, S_{T-1}>:
+ *
+ *   G_t = scale sum_h q_{t,h} dout_{t,h}^T + d_n (1 - reset[t+1,b]) G_{t+1}
+ *                                                     (dST joins at t = T-1)
+ *   dq_{t,h} = scale S_t dout_{t,h},  dk_t = G_t v_t,  dv_t = G_t^T k_t,
+ *   dS0 = d_n (1 - reset[0,b]) G_0
+ *
+ * dST, dS0: [B, nkv, dk, dv] fp32 or NULL (= 0; not wanted).
+ *
+ * o5_linattn_step is one step (T = 1) that updates the states S in place.
+ * ------------------------------------------------------------------------ */
+size_t o5_linattn_fwd_workspace_bytes(o5_dtype dt, int T, int B, int nh,
+                                      int nkv, int dk, int dv);
+int o5_linattn_fwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv,
+                   const void* q, size_t ldq, const void* k, size_t ldk,
+                   const void* v, size_t ldv, const float* decay, float scale,
+                   const float* S0, const uint8_t* reset, void* o, size_t ldo,
+                   float* ST, void* ws, size_t ws_bytes, void* stream);
+size_t o5_linattn_bwd_workspace_bytes(o5_dtype dt, int T, int B, int nh,
+                                      int nkv, int dk, int dv);
+int o5_linattn_bwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv,
+                   const void* q, size_t ldq, const void* k, size_t ldk,
+                   const void* v, size_t ldv, const float* decay, float scale,
+                   const float* S0, const uint8_t* reset, const void* dout,
+                   size_t lddo, const float* dST, void* dq, size_t lddq,
+                   void* dkey, size_t lddk, void* dval, size_t lddv,
+                   float* dS0, void* ws, size_t ws_bytes, void* stream);
+int o5_linattn_step(o5_dtype dt, int B, int nh, int nkv, int dk, int dv,
+                    const void* q, size_t ldq, const void* k, size_t ldk,
+                    const void* v, size_t ldv, const float* decay,
+                    float scale, const uint8_t* reset, float* S, void* o,
+                    size_t ldo, void* stream);
+
+/* ------------------------------------------------------------------------
  * o5_f32_to_bf16 -- round n fp32 values to bfloat16 (nearest, ties to
  * even; NaN stays NaN).  Used to build the bf16 GEMM operands.
  * ------------------------------------------------------------------------ */

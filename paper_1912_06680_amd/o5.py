@@ -29,6 +29,8 @@ EXPORTED = (
     "o5_ppo_loss_grad_workspace_bytes", "o5_ppo_loss_grad", "o5_ppo_head_grad_ld", "o5_ppo_loss_grad_factored",
     "o5_adam_step",
     "o5_policy_sample_workspace_bytes", "o5_policy_sample", "o5_policy_sample_static",
+    "o5_linattn_fwd_workspace_bytes", "o5_linattn_fwd", "o5_linattn_bwd_workspace_bytes", "o5_linattn_bwd",
+    "o5_linattn_step",
     "o5_f32_to_bf16",
     "o5_param_count", "o5_surgery_widen", "o5_surgery_fold_input",
     "o5_ktimer_enable", "o5_ktimer_enable_sites", "o5_ktimer_read", "o5_ktimer_site_name",
@@ -108,6 +110,12 @@ _SIGS = {
                               _vp]),
     "o5_policy_sample_static": (_i, [_i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp, _vp,
                                      _vp]),
+    "o5_linattn_fwd_workspace_bytes": (_sz, [_i] * 7),
+    "o5_linattn_fwd": (_i, [_i] * 7 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp, _vp, _sz, _vp]),
+    "o5_linattn_bwd_workspace_bytes": (_sz, [_i] * 7),
+    "o5_linattn_bwd": (_i, [_i] * 7 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp] + [_vp, _sz] * 3
+                       + [_vp, _vp, _sz, _vp]),
+    "o5_linattn_step": (_i, [_i] * 6 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp]),
     "o5_f32_to_bf16": (_i, [_sz, _vp, _vp, _vp]),
     "o5_param_count": (_sz, [_i, _i, _i]),
     "o5_surgery_widen": (_i, [_i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _u64, _vp]),
@@ -331,6 +339,36 @@ def o5_surgery_fold_input(D, H, A1, Dk, E, p_old, m_old, v_old, p_new, m_new, v_
     _check("o5_surgery_fold_input", lib().o5_surgery_fold_input(D, H, A1, Dk, _p(E), _p(p_old), _p(m_old),
                                                                 _p(v_old), _p(p_new), _p(m_new), _p(v_new),
                                                                 _stream(stream)))
+
+
+def o5_linattn_fwd_workspace_bytes(dt, T, B, nh, nkv, dk, dv):
+    return lib().o5_linattn_fwd_workspace_bytes(dt, T, B, nh, nkv, dk, dv)
+
+
+def o5_linattn_fwd(dt, T, B, nh, nkv, dk, dv, q, ldq, k, ldk, v, ldv, decay, scale, S0, reset, o, ldo, ST, ws,
+                   stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_linattn_fwd", lib().o5_linattn_fwd(
+        dt, T, B, nh, nkv, dk, dv, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(decay), float(scale), _p(S0), _p(reset),
+        _p(o), ldo, _p(ST), wp, wn, _stream(stream)))
+
+
+def o5_linattn_bwd_workspace_bytes(dt, T, B, nh, nkv, dk, dv):
+    return lib().o5_linattn_bwd_workspace_bytes(dt, T, B, nh, nkv, dk, dv)
+
+
+def o5_linattn_bwd(dt, T, B, nh, nkv, dk, dv, q, ldq, k, ldk, v, ldv, decay, scale, S0, reset, dout, lddo, dST,
+                   dq, lddq, dkey, lddk, dval, lddv, dS0, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_linattn_bwd", lib().o5_linattn_bwd(
+        dt, T, B, nh, nkv, dk, dv, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(decay), float(scale), _p(S0), _p(reset),
+        _p(dout), lddo, _p(dST), _p(dq), lddq, _p(dkey), lddk, _p(dval), lddv, _p(dS0), wp, wn, _stream(stream)))
+
+
+def o5_linattn_step(dt, B, nh, nkv, dk, dv, q, ldq, k, ldk, v, ldv, decay, scale, reset, S, o, ldo, stream=None):
+    _check("o5_linattn_step", lib().o5_linattn_step(
+        dt, B, nh, nkv, dk, dv, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(decay), float(scale), _p(reset), _p(S),
+        _p(o), ldo, _stream(stream)))
 
 
 def o5_f32_to_bf16(n, src, dst, stream=None):
