@@ -571,6 +571,51 @@ int o5_linattn_step(o5_dtype dt, int B, int nh, int nkv, int dk, int dv,
                     size_t ldo, void* stream);
 
 /* ------------------------------------------------------------------------
+ * o5_resnorm_fwd / _bwd -- the RMS norms after one block and before the next
+ * around a residual stream, fused with the block's gate and its residual
+ * scale; one pass over the rows:
+ *
+ *   x' = x + rho . sigmoid(gate) . (w_post . u r_u)
+ *   n  = w_pre . x' r_x'          r_z = 1 / sqrt(mean_j z_j^2 + eps)
+ *
+ * xt       type of the stream x, x' and of dxo, dx.   dt: type of u, gate,
+ *          n and of their gradients; O5_BF16 where xt is.
+ * N, D     rows, 1..2^30-1, and their width, a multiple of 8 in 8..8192.
+ * x        [N, D] xt.
+ * u        [N, D] dt, the block's output, or NULL: no block yet, x' = x (the
+ *          norm before the first block; gate must be NULL and xo is unused).
+ * gate     rows of D dt with a stride of ldg elements (a multiple of 8, >= D,
+ *          below 2^31), or NULL (a factor of 1).
+ * w_post, rho [D] fp32: gain of the norm after, residual scale (with u).
+ * w_pre    [D] fp32, gain of the norm before, or NULL: n is not wanted (after
+ *          the last block).   eps: > 0.
+ * xo       out [N, D] xt = x' (may be x itself).   n: out [N, D] dt, of x'
+ *          before it is rounded to xt.
+ * r_post, r_pre out [N] fp32 = r_u and r_x', for the backward pass, or NULL.
+ *
+ * o5_resnorm_bwd takes dxo = dJ/dx' as it arrives along the stream and dn =
+ * dJ/dn and returns dx = dJ/dx (dx may be dxo itself), du, dgate (rows of
+ * stride lddg) and the gains' gradients, sums over the rows in a fixed order.
+ * xo, dn, w_pre, r_pre and dw_pre go together, and u, w_post, rho, r_post,
+ * du, dw_post and drho, and gate and dgate; the parts that the forward pass
+ * had not are NULL.
+ * ws       scratch of o5_resnorm_bwd_workspace_bytes(...) bytes.
+ * ------------------------------------------------------------------------ */
+int o5_resnorm_fwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* x,
+                   const void* u, const void* gate, size_t ldg,
+                   const float* w_post, const float* rho, const float* w_pre,
+                   float eps, void* xo, void* n, float* r_post, float* r_pre,
+                   void* stream);
+size_t o5_resnorm_bwd_workspace_bytes(o5_dtype xt, o5_dtype dt, int N, int D);
+int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
+                   const void* u, const void* gate, size_t ldg,
+                   const float* w_post, const float* rho, const float* w_pre,
+                   const float* r_post, const float* r_pre, const void* dxo,
+                   const void* dn, void* dx, void* du, void* dgate,
+                   size_t lddg, float* dw_post, float* drho, float* dw_pre,
+                   void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * o5_f32_to_bf16 -- round n fp32 values to bfloat16 (nearest, ties to
  * even; NaN stays NaN).  Used to build the bf16 GEMM operands.
  * ------------------------------------------------------------------------ */

@@ -1,0 +1,447 @@
+// RMS norms before and after a block, fused with its gate and residual
+// scale, o5_resnorm_*.
+//
+//   x' = x + rho . sigmoid(gate) . (w_post . u r_u),   r_u = (mean u^2 + eps)^(-1/2)
+//   n  = w_pre . x' r_x',                             r_x' = (mean x'^2 + eps)^(-1/2)
+//
+// so the norm after one block, its gate, the residual sum and the norm before
+// the next block are one pass over the row: each array is read or written
+// once, and a row stays in registers between its two reductions.  HBM-bound.
+#include "common.h"
+#include "reduce.h"
+
+namespace o5 {
+namespace {
+
+constexpr int kMaxWidth = 8192;
+
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
+
+template <typename E> struct Run8;  // 8 consecutive elements as they are stored
+template <> struct Run8<float> {
+  f4_t a, b;
+  __device__ __forceinline__ void load(const void* p, size_t i) {
+    const f4_t* q = reinterpret_cast<const f4_t*>(static_cast<const float*>(p) + i);
+    a = q[0];
+    b = q[1];
+  }
+  __device__ __forceinline__ float operator[](int j) const { return j < 4 ? a[j] : b[j - 4]; }
+};
+template <> struct Run8<uint16_t> {
+  u4_t a;
+  __device__ __forceinline__ void load(const void* p, size_t i) {
+    a = *reinterpret_cast<const u4_t*>(static_cast<const uint16_t*>(p) + i);
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    return __uint_as_float((j & 1) ? (a[j / 2] & 0xffff0000u) : (a[j / 2] << 16));
+  }
+};
+
+template <typename E> __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8]);
+template <> __device__ __forceinline__ void store8<float>(void* p, size_t i, const float (&v)[8]) {
+  f4_t* q = reinterpret_cast<f4_t*>(static_cast<float*>(p) + i);
+  q[0] = f4_t{v[0], v[1], v[2], v[3]};
+  q[1] = f4_t{v[4], v[5], v[6], v[7]};
+}
+template <> __device__ __forceinline__ void store8<uint16_t>(void* p, size_t i, const float (&v)[8]) {
+  *reinterpret_cast<u4_t*>(static_cast<uint16_t*>(p) + i) =
+      u4_t{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
+}
+
+// Sum over the TR threads of a row (whole waves), the same in each of them.
+template <int TR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (TR == 64) return v;
+  const int w = threadIdx.x >> 6, w0 = threadIdx.x / TR * (TR / 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[w] = v;
+  __syncthreads();
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < TR / 64; ++i) s += red[w0 + i];
+  return s;
+}
+
+struct NormFwd {
+  const void *x, *u, *gate;
+  const float *w_post, *rho, *w_pre;
+  void *xo, *n;
+  float *r_post, *r_pre;
+  int N, D;
+  size_t ldg;
+  float eps;
+};
+
+// TR threads of a block of max(256, TR) take a row, 8 elements each in NJ runs.
+template <typename X, typename E, int TR, int NJ>
+__global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_fwd(NormFwd p) {
+  constexpr int BT = TR < 256 ? 256 : TR;
+  __shared__ float red[BT / 64];
+  const int row = blockIdx.x * (BT / TR) + threadIdx.x / TR, t = threadIdx.x % TR;
+  const bool in = row < p.N;
+  const size_t base = static_cast<size_t>(in ? row : 0) * p.D, gbase = static_cast<size_t>(in ? row : 0) * p.ldg;
+  const float inv = 1.0f / static_cast<float>(p.D);
+  float x[NJ][8];
+  bool on[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int c = (t + j * TR) * 8;
+    on[j] = in && c < p.D;
+    Run8<X> r;
+    if (on[j]) r.load(p.x, base + c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[j][i] = on[j] ? r[i] : 0.0f;
+  }
+  if (p.u) {
+    float u[NJ][8], ss = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      Run8<E> r;
+      if (on[j]) r.load(p.u, base + (t + j * TR) * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u[j][i] = on[j] ? r[i] : 0.0f;
+        ss = fmaf(u[j][i], u[j][i], ss);
+      }
+    }
+    const float r = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
+    if (p.r_post && t == 0 && in) p.r_post[row] = r;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (!on[j]) continue;
+      const int c = (t + j * TR) * 8;
+      Run8<float> w, rho;
+      Run8<E> g;
+      w.load(p.w_post, c);
+      rho.load(p.rho, c);
+      if (p.gate) g.load(p.gate, gbase + c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float y = u[j][i] * r * (w[i] * rho[i]);
+        if (p.gate) y *= sigmoid_f(g[i]);
+        x[j][i] += y;
+      }
+      store8<X>(p.xo, base + c, x[j]);
+    }
+  }
+  if (p.w_pre) {
+    float ss = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(x[j][i], x[j][i], ss);
+    const float r = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
+    if (p.r_pre && t == 0 && in) p.r_pre[row] = r;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (!on[j]) continue;
+      const int c = (t + j * TR) * 8;
+      Run8<float> w;
+      w.load(p.w_pre, c);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = x[j][i] * r * w[i];
+      store8<E>(p.n, base + c, y);
+    }
+  }
+}
+
+struct NormBwd {
+  const void *x, *u, *gate;
+  const float *w_post, *rho, *w_pre, *r_post, *r_pre;
+  const void *dxo, *dn;
+  void *dx, *du, *dgate;
+  float *part;  // [blocks * rows per block][2][D]: the row groups' column sums for dw_pre, and for drho and dw_post
+  int N, D;
+  size_t ldg, lddg;
+};
+
+// The rows' gradients, and each row group's sums over its rows:
+//   a = dn w_pre,  d = dx' + r_x' (a - x' r_x'^2 mean(a x')),  dx = d
+//   s = sigmoid(gate), y = u r_u:  dgate = d y w_post rho s (1 - s),
+//   a = d s w_post rho,  du = r_u (a - y mean(a y))
+//   dw_pre = sum dn x' r_x',  drho = w_post sum d s y,  dw_post = rho sum d s y
+template <typename X, typename E, int TR, int NJ>
+__global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_bwd(NormBwd p) {
+  constexpr int BT = TR < 256 ? 256 : TR;
+  __shared__ float red[BT / 64];
+  const int group = blockIdx.x * (BT / TR) + threadIdx.x / TR, groups = gridDim.x * (BT / TR), t = threadIdx.x % TR;
+  const float inv = 1.0f / static_cast<float>(p.D);
+  float spre[NJ][8] = {}, spost[NJ][8] = {};
+  const int rounds = (p.N + groups - 1) / groups;
+  for (int k = 0; k < rounds; ++k) {
+    const int row = group + k * groups;
+    const bool in = row < p.N;
+    const size_t base = static_cast<size_t>(in ? row : 0) * p.D;
+    float d[NJ][8];
+    bool on[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = (t + j * TR) * 8;
+      on[j] = in && c < p.D;
+      Run8<X> r;
+      if (on[j]) r.load(p.dxo, base + c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[j][i] = on[j] ? r[i] : 0.0f;
+    }
+    if (p.w_pre) {
+      float a[NJ][8], x[NJ][8], dot = 0.0f;
+      const float r = in ? p.r_pre[row] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int c = (t + j * TR) * 8;
+        Run8<X> xr;
+        Run8<E> nr;
+        Run8<float> w;
+        if (on[j]) {
+          xr.load(p.x, base + c);
+          nr.load(p.dn, base + c);
+          w.load(p.w_pre, c);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[j][i] = on[j] ? xr[i] : 0.0f;
+          const float dn = on[j] ? nr[i] : 0.0f;
+          a[j][i] = on[j] ? dn * w[i] : 0.0f;
+          dot = fmaf(a[j][i], x[j][i], dot);
+          spre[j][i] = fmaf(dn, x[j][i] * r, spre[j][i]);
+        }
+      }
+      const float m = row_sum<TR>(dot, red) * inv * (r * r);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[j][i] += r * (a[j][i] - x[j][i] * m);
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      if (on[j]) store8<X>(p.dx, base + (t + j * TR) * 8, d[j]);
+    if (p.u) {
+      float a[NJ][8], y[NJ][8], dot = 0.0f;
+      const float r = in ? p.r_post[row] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int c = (t + j * TR) * 8;
+        Run8<E> ur, gr;
+        Run8<float> w, rho;
+        if (on[j]) {
+          ur.load(p.u, base + c);
+          w.load(p.w_post, c);
+          rho.load(p.rho, c);
+          if (p.gate) gr.load(p.gate, static_cast<size_t>(row) * p.ldg + c);
+        }
+        float dg[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[j][i] = on[j] ? ur[i] * r : 0.0f;
+          const float wr = on[j] ? w[i] * rho[i] : 0.0f;
+          float ds = d[j][i];
+          if (p.gate) {
+            const float s = on[j] ? sigmoid_f(gr[i]) : 0.0f;
+            dg[i] = ds * y[j][i] * wr * s * (1.0f - s);
+            ds *= s;
+          }
+          spost[j][i] = fmaf(ds, y[j][i], spost[j][i]);
+          a[j][i] = ds * wr;
+          dot = fmaf(a[j][i], y[j][i], dot);
+        }
+        if (p.gate && on[j]) store8<E>(p.dgate, static_cast<size_t>(row) * p.lddg + c, dg);
+      }
+      const float m = row_sum<TR>(dot, red) * inv;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (!on[j]) continue;
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = r * (a[j][i] - y[j][i] * m);
+        store8<E>(p.du, base + (t + j * TR) * 8, o);
+      }
+    }
+  }
+  float* part = p.part + static_cast<size_t>(group) * 2 * p.D;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int c = (t + j * TR) * 8;
+    if (c >= p.D) continue;
+    if (p.w_pre) store8<float>(part, c, spre[j]);
+    if (p.u) store8<float>(part + p.D, c, spost[j]);
+  }
+}
+
+// dw_pre, drho and dw_post from the row groups' sums: a block takes 64 columns
+// of one of the two sums, wave w adds the groups w, w + 16, ... in order, and
+// the 16 waves' sums are added in order.
+__global__ void __launch_bounds__(1024) resnorm_columns(int groups, int D, const float* __restrict__ part,
+                                                        const float* __restrict__ w_post,
+                                                        const float* __restrict__ rho, float* __restrict__ dw_pre,
+                                                        float* __restrict__ drho, float* __restrict__ dw_post) {
+  __shared__ float red[16][64];
+  const int which = blockIdx.y + (dw_pre ? 0 : 1);  // 0: dw_pre, 1: the sum of the other two
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const float* col = part + static_cast<size_t>(which) * D + c;
+  float s = 0.0f;
+  if (c < D && w < groups)
+    s = ordered_sum((groups - w + 15) / 16, [&](int i) { return col[static_cast<size_t>(w + 16 * i) * 2 * D]; });
+  red[w][lane] = s;
+  __syncthreads();
+  if (w != 0 || c >= D) return;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += red[i][lane];
+  if (which == 0) {
+    dw_pre[c] = s;
+  } else {
+    drho[c] = w_post[c] * s;
+    dw_post[c] = rho[c] * s;
+  }
+}
+
+// Threads of a row: 8 or 16 elements each.
+int row_threads(int D) { return D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
+
+// Row groups that walk the N rows in the backward pass.
+int bwd_blocks(int N, int D) {
+  const int tr = row_threads(D), per = tr < 256 ? 256 / tr : 1;
+  return std::min((N + per - 1) / per, 512);
+}
+int bwd_groups(int N, int D) {
+  const int tr = row_threads(D);
+  return bwd_blocks(N, D) * (tr < 256 ? 256 / tr : 1);
+}
+
+template <typename X, typename E>
+void launch_fwd(const NormFwd& p, hipStream_t s) {
+  const int tr = row_threads(p.D), bt = tr < 256 ? 256 : tr, per = bt / tr;
+  const dim3 grid(static_cast<unsigned>((p.N + per - 1) / per));
+  auto k = tr == 64    ? (p.D <= 512 ? resnorm_fwd<X, E, 64, 1> : resnorm_fwd<X, E, 64, 2>)
+           : tr == 128 ? resnorm_fwd<X, E, 128, 2>
+           : tr == 256 ? resnorm_fwd<X, E, 256, 2>
+                       : resnorm_fwd<X, E, 512, 2>;
+  hipLaunchKernelGGL(k, grid, dim3(bt), 0, s, p);
+}
+
+template <typename X, typename E>
+void launch_bwd(const NormBwd& p, hipStream_t s) {
+  const int tr = row_threads(p.D), bt = tr < 256 ? 256 : tr;
+  auto k = tr == 64    ? (p.D <= 512 ? resnorm_bwd<X, E, 64, 1> : resnorm_bwd<X, E, 64, 2>)
+           : tr == 128 ? resnorm_bwd<X, E, 128, 2>
+           : tr == 256 ? resnorm_bwd<X, E, 256, 2>
+                       : resnorm_bwd<X, E, 512, 2>;
+  hipLaunchKernelGGL(k, dim3(bwd_blocks(p.N, p.D)), dim3(bt), 0, s, p);
+}
+
+int check_common(const char* fn, o5_dtype xt, o5_dtype dt, int N, int D) {
+  O5_CHECK((xt == O5_F32 || xt == O5_BF16) && (dt == O5_F32 || dt == O5_BF16), O5_E_DTYPE, "%s: unknown dtype", fn);
+  O5_CHECK(!(xt == O5_BF16 && dt == O5_F32), O5_E_DTYPE, "%s: a bf16 residual stream needs bf16 blocks", fn);
+  O5_CHECK(N >= 1 && N < (1 << 30) && D >= 8 && D <= kMaxWidth && D % 8 == 0, O5_E_SHAPE,
+           "%s: N=%d must be in 1..2^30-1 and D=%d a multiple of 8 in 8..%d", fn, N, D, kMaxWidth);
+  return O5_OK;
+}
+
+int check_gate(const char* fn, const char* name, const void* gate, size_t ld, int D) {
+  if (gate)
+    O5_CHECK(ld >= static_cast<size_t>(D) && ld % 8 == 0 && ld < (1ull << 31), O5_E_SHAPE,
+             "%s: %s=%zu must be a multiple of 8, at least D and below 2^31", fn, name, ld);
+  return O5_OK;
+}
+
+#define O5_TRY(expr)              \
+  do {                            \
+    const int st_ = (expr);       \
+    if (st_ != O5_OK) return st_; \
+  } while (0)
+
+}  // namespace
+}  // namespace o5
+
+using namespace o5;
+
+extern "C" int o5_resnorm_fwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* x, const void* u, const void* gate,
+                              size_t ldg, const float* w_post, const float* rho, const float* w_pre, float eps, void* xo,
+                              void* n, float* r_post, float* r_pre, void* stream) {
+  const char* fn = "o5_resnorm_fwd";
+  O5_TRY(check_common(fn, xt, dt, N, D));
+  O5_CHECK(eps > 0.0f && std::isfinite(eps), O5_E_ARG, "%s: eps must be positive", fn);
+  O5_CHECK(u != nullptr || w_pre != nullptr, O5_E_ARG, "%s: u and w_pre are both NULL", fn);
+  O5_CHECK(u != nullptr || gate == nullptr, O5_E_ARG, "%s: a gate needs u", fn);
+  O5_TRY(check_gate(fn, "ldg", gate, ldg, D));
+  O5_PTR(x, "x");
+  O5_OPT_PTR(gate, "gate");
+  O5_OPT_PTR(r_post, "r_post");
+  O5_OPT_PTR(r_pre, "r_pre");
+  if (u) {
+    O5_PTR(u, "u");
+    O5_PTR(w_post, "w_post");
+    O5_PTR(rho, "rho");
+    O5_PTR(xo, "xo");
+  }
+  if (w_pre) {
+    O5_PTR(w_pre, "w_pre");
+    O5_PTR(n, "n");
+  }
+  const NormFwd p = {x, u, gate, w_post, rho, w_pre, xo, n, r_post, r_pre, N, D, ldg, eps};
+  if (xt == O5_BF16)
+    launch_fwd<uint16_t, uint16_t>(p, as_stream(stream));
+  else if (dt == O5_BF16)
+    launch_fwd<float, uint16_t>(p, as_stream(stream));
+  else
+    launch_fwd<float, float>(p, as_stream(stream));
+  return check_launch(fn);
+}
+
+extern "C" size_t o5_resnorm_bwd_workspace_bytes(o5_dtype xt, o5_dtype dt, int N, int D) {
+  if (check_common("o5_resnorm_bwd_workspace_bytes", xt, dt, N, D) != O5_OK) return 0;
+  return static_cast<size_t>(bwd_groups(N, D)) * 2 * D * sizeof(float);
+}
+
+extern "C" int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo, const void* u, const void* gate,
+                              size_t ldg, const float* w_post, const float* rho, const float* w_pre,
+                              const float* r_post, const float* r_pre, const void* dxo, const void* dn, void* dx,
+                              void* du, void* dgate, size_t lddg, float* dw_post, float* drho, float* dw_pre, void* ws,
+                              size_t ws_bytes, void* stream) {
+  const char* fn = "o5_resnorm_bwd";
+  O5_TRY(check_common(fn, xt, dt, N, D));
+  O5_CHECK(u != nullptr || w_pre != nullptr, O5_E_ARG, "%s: u and w_pre are both NULL", fn);
+  O5_CHECK(u != nullptr || gate == nullptr, O5_E_ARG, "%s: a gate needs u", fn);
+  O5_TRY(check_gate(fn, "ldg", gate, ldg, D));
+  O5_TRY(check_gate(fn, "lddg", gate, lddg, D));
+  O5_PTR(dxo, "dxo");
+  O5_PTR(dx, "dx");
+  if (u) {
+    O5_PTR(u, "u");
+    O5_PTR(w_post, "w_post");
+    O5_PTR(rho, "rho");
+    O5_PTR(r_post, "r_post");
+    O5_PTR(du, "du");
+    O5_PTR(dw_post, "dw_post");
+    O5_PTR(drho, "drho");
+  }
+  if (gate) {
+    O5_PTR(gate, "gate");
+    O5_PTR(dgate, "dgate");
+  }
+  if (w_pre) {
+    O5_PTR(xo, "xo");
+    O5_PTR(w_pre, "w_pre");
+    O5_PTR(r_pre, "r_pre");
+    O5_PTR(dn, "dn");
+    O5_PTR(dw_pre, "dw_pre");
+  }
+  O5_CHECK(ws != nullptr && ws_bytes >= o5_resnorm_bwd_workspace_bytes(xt, dt, N, D), O5_E_WORKSPACE,
+           "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
+  O5_PTR(ws, "ws");
+  const NormBwd p = {xo, u, gate, w_post, rho, w_pre, r_post, r_pre, dxo, dn, dx, du, dgate, static_cast<float*>(ws), N, D,
+                     ldg, lddg};
+  if (xt == O5_BF16)
+    launch_bwd<uint16_t, uint16_t>(p, as_stream(stream));
+  else if (dt == O5_BF16)
+    launch_bwd<float, uint16_t>(p, as_stream(stream));
+  else
+    launch_bwd<float, float>(p, as_stream(stream));
+  const dim3 grid((D + 63) / 64, (u ? 1 : 0) + (w_pre ? 1 : 0));
+  hipLaunchKernelGGL(resnorm_columns, grid, dim3(1024), 0, as_stream(stream), bwd_groups(N, D), D,
+                     static_cast<const float*>(ws), w_post, rho, w_pre ? dw_pre : nullptr, drho, dw_post);
+  return check_launch(fn);
+}

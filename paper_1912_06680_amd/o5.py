@@ -31,6 +31,7 @@ EXPORTED = (
     "o5_policy_sample_workspace_bytes", "o5_policy_sample", "o5_policy_sample_static",
     "o5_linattn_fwd_workspace_bytes", "o5_linattn_fwd", "o5_linattn_bwd_workspace_bytes", "o5_linattn_bwd",
     "o5_linattn_step",
+    "o5_resnorm_fwd", "o5_resnorm_bwd_workspace_bytes", "o5_resnorm_bwd",
     "o5_f32_to_bf16",
     "o5_param_count", "o5_surgery_widen", "o5_surgery_fold_input",
     "o5_ktimer_enable", "o5_ktimer_enable_sites", "o5_ktimer_read", "o5_ktimer_site_name",
@@ -116,6 +117,9 @@ _SIGS = {
     "o5_linattn_bwd": (_i, [_i] * 7 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp] + [_vp, _sz] * 3
                        + [_vp, _vp, _sz, _vp]),
     "o5_linattn_step": (_i, [_i] * 6 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp]),
+    "o5_resnorm_fwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 3 + [_f] + [_vp] * 5),
+    "o5_resnorm_bwd_workspace_bytes": (_sz, [_i] * 4),
+    "o5_resnorm_bwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 10 + [_sz] + [_vp] * 4 + [_sz, _vp]),
     "o5_f32_to_bf16": (_i, [_sz, _vp, _vp, _vp]),
     "o5_param_count": (_sz, [_i, _i, _i]),
     "o5_surgery_widen": (_i, [_i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _u64, _vp]),
@@ -369,6 +373,24 @@ def o5_linattn_step(dt, B, nh, nkv, dk, dv, q, ldq, k, ldk, v, ldv, decay, scale
     _check("o5_linattn_step", lib().o5_linattn_step(
         dt, B, nh, nkv, dk, dv, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(decay), float(scale), _p(reset), _p(S),
         _p(o), ldo, _stream(stream)))
+
+
+def o5_resnorm_fwd(xt, dt, N, D, x, u, gate, ldg, w_post, rho, w_pre, eps, xo, n, r_post, r_pre, stream=None):
+    _check("o5_resnorm_fwd", lib().o5_resnorm_fwd(
+        xt, dt, N, D, _p(x), _p(u), _p(gate), ldg, _p(w_post), _p(rho), _p(w_pre), float(eps), _p(xo), _p(n),
+        _p(r_post), _p(r_pre), _stream(stream)))
+
+
+def o5_resnorm_bwd_workspace_bytes(xt, dt, N, D):
+    return lib().o5_resnorm_bwd_workspace_bytes(xt, dt, N, D)
+
+
+def o5_resnorm_bwd(xt, dt, N, D, xo, u, gate, ldg, w_post, rho, w_pre, r_post, r_pre, dxo, dn, dx, du, dgate, lddg,
+                   dw_post, drho, dw_pre, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_resnorm_bwd", lib().o5_resnorm_bwd(
+        xt, dt, N, D, _p(xo), _p(u), _p(gate), ldg, _p(w_post), _p(rho), _p(w_pre), _p(r_post), _p(r_pre), _p(dxo),
+        _p(dn), _p(dx), _p(du), _p(dgate), lddg, _p(dw_post), _p(drho), _p(dw_pre), wp, wn, _stream(stream)))
 
 
 def o5_f32_to_bf16(n, src, dst, stream=None):
