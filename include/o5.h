@@ -616,6 +616,66 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
                    void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * o5_adamw_plan / _step / _moments -- AdamW over many tensors in one launch,
+ * with the per-parameter clip of o5_adam_step, decay of the weights apart from
+ * the gradient, and moments in 32 bits or in 8:
+ *
+ *   v = b2 v + (1-b2) g^2;  vh = v / (1 - b2^step)
+ *   g' = clamp(g, -clip_k sqrt(vh), clip_k sqrt(vh))     (clip_k <= 0: g' = g)
+ *   m = b1 m + (1-b1) g';   mh = m / (1 - b1^step)
+ *   p = (1 - lr wd) p - lr mh / (sqrt(vh) + eps)     (lr: hp.lr * lr_scale)
+ *
+ * A tensor: n elements (1..2^40-1); p [n] fp32, updated in place; g [n] of
+ * type g_dt; p_bf16 out [n], a bf16 copy of the new p, or NULL; lr_scale and
+ * weight_decay >= 0.  bits = 32: m, v [n] fp32, in place (m_exp, v_exp
+ * unused).  bits = 8: m, v [n] bytes and m_exp, v_exp, one byte for each 256
+ * elements (the last may be partial; no alignment needed), start from zeros
+ * everywhere.  With a = max(exp - 127, -90) and e, f the code's exponent field and its 3
+ * mantissa bits, a code stands for
+ *     m: sign bit, e of 4 bits:  +- (e ? 8 + f : f) 2^(a - 17 + max(e, 1))
+ *     v: e of 5 bits:               (e ? 8 + f : f) 2^(a - 33 + max(e, 1))
+ * (m 0x7f, with either sign, and v 0xff: NaN, for a moment that is not
+ * finite).  a is the exponent of the group's largest finite new value, and a
+ * value is rounded up in magnitude with the chance
+ * of the part that is cut off: element i of tensor k (its place in the plan)
+ * takes word i mod 4 of Philox4x32-7 (Salmon et al., SC'11) at the counter
+ * (i div 4, i div 2^34, step, k) and the key `seed`, its low half for m and its
+ * high half for v.  A positive v never gets code 0.
+ *
+ * o5_adamw_plan  writes into `plan` (host, 16-byte aligned, bytes >=
+ *          o5_adamw_plan_bytes, which is 0 for invalid tensors) what the
+ *          other two calls need of count tensors (host array; 1..2^20).  The
+ *          caller copies those bytes to device memory once and passes both,
+ *          and keeps the tensors where they are while the plan is used.
+ * o5_adamw_step  one step; hp as for o5_adam_step; step >= 1.
+ * o5_adamw_moments  the values of the moments, as a checkpoint holds them: m,
+ *          v out, fp32; tensor k starts at the sum of the earlier tensors'
+ *          n, each rounded up to 256 (the gaps are not written).
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t n;
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* m_exp;
+  uint8_t* v_exp;
+  uint16_t* p_bf16;
+  float lr_scale;
+  float weight_decay;
+  o5_dtype g_dt;
+  int bits;
+} o5_adamw_tensor;
+
+size_t o5_adamw_plan_bytes(int count, const o5_adamw_tensor* tensors);
+int o5_adamw_plan(int count, const o5_adamw_tensor* tensors, void* plan,
+                  size_t bytes);
+int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp hp,
+                  uint64_t seed, int step, void* stream);
+int o5_adamw_moments(const void* plan, const void* plan_dev, float* m,
+                     float* v, void* stream);
+
+/* ------------------------------------------------------------------------
  * o5_f32_to_bf16 -- round n fp32 values to bfloat16 (nearest, ties to
  * even; NaN stays NaN).  Used to build the bf16 GEMM operands.
  * ------------------------------------------------------------------------ */

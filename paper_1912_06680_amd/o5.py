@@ -32,6 +32,7 @@ EXPORTED = (
     "o5_linattn_fwd_workspace_bytes", "o5_linattn_fwd", "o5_linattn_bwd_workspace_bytes", "o5_linattn_bwd",
     "o5_linattn_step",
     "o5_resnorm_fwd", "o5_resnorm_bwd_workspace_bytes", "o5_resnorm_bwd",
+    "o5_adamw_plan_bytes", "o5_adamw_plan", "o5_adamw_step", "o5_adamw_moments",
     "o5_f32_to_bf16",
     "o5_param_count", "o5_surgery_widen", "o5_surgery_fold_input",
     "o5_ktimer_enable", "o5_ktimer_enable_sites", "o5_ktimer_read", "o5_ktimer_site_name",
@@ -74,6 +75,21 @@ def _unit(u):
 class RewardHp(ctypes.Structure):
     _fields_ = [("tau", ctypes.c_float), ("decay_base", ctypes.c_float), ("decay_minutes", ctypes.c_float),
                 ("eps", ctypes.c_float)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_size_t), ("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("p_bf16", ctypes.c_void_p), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("g_dt", ctypes.c_int), ("bits", ctypes.c_int)]
+
+
+def adamw_tensor(p, g, m, v, m_exp=None, v_exp=None, p_bf16=None, lr_scale=1.0, weight_decay=0.0):
+    """An o5_adamw_tensor over torch tensors (keep the tensors alive while the plan is used): g's type by its dtype,
+    moments in 8 bits where m is a tensor of bytes."""
+    return AdamwTensor(p.numel(), _p(p), _p(g), _p(m), _p(v), _p(m_exp), _p(v_exp), _p(p_bf16), float(lr_scale),
+                       float(weight_decay), O5_BF16 if g.dtype == torch.bfloat16 else O5_F32,
+                       8 if m.dtype == torch.uint8 else 32)
 
 
 _vp = ctypes.c_void_p
@@ -120,6 +136,10 @@ _SIGS = {
     "o5_resnorm_fwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 3 + [_f] + [_vp] * 5),
     "o5_resnorm_bwd_workspace_bytes": (_sz, [_i] * 4),
     "o5_resnorm_bwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 10 + [_sz] + [_vp] * 4 + [_sz, _vp]),
+    "o5_adamw_plan_bytes": (_sz, [_i, _vp]),
+    "o5_adamw_plan": (_i, [_i, _vp, _vp, _sz]),
+    "o5_adamw_step": (_i, [_vp, _vp, AdamHp, _u64, _i, _vp]),
+    "o5_adamw_moments": (_i, [_vp] * 5),
     "o5_f32_to_bf16": (_i, [_sz, _vp, _vp, _vp]),
     "o5_param_count": (_sz, [_i, _i, _i]),
     "o5_surgery_widen": (_i, [_i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _u64, _vp]),
@@ -391,6 +411,28 @@ def o5_resnorm_bwd(xt, dt, N, D, xo, u, gate, ldg, w_post, rho, w_pre, r_post, r
     _check("o5_resnorm_bwd", lib().o5_resnorm_bwd(
         xt, dt, N, D, _p(xo), _p(u), _p(gate), ldg, _p(w_post), _p(rho), _p(w_pre), _p(r_post), _p(r_pre), _p(dxo),
         _p(dn), _p(dx), _p(du), _p(dgate), lddg, _p(dw_post), _p(drho), _p(dw_pre), wp, wn, _stream(stream)))
+
+
+def _tensors(tensors):
+    return (AdamwTensor * len(tensors))(*tensors)
+
+
+def o5_adamw_plan_bytes(tensors):
+    return lib().o5_adamw_plan_bytes(len(tensors), _tensors(tensors))
+
+
+def o5_adamw_plan(tensors, plan):
+    """Write the plan of a list of adamw_tensor()s into `plan`, a CPU tensor of bytes."""
+    _check("o5_adamw_plan", lib().o5_adamw_plan(len(tensors), _tensors(tensors), _p(plan), plan.numel()))
+
+
+def o5_adamw_step(plan, plan_dev, lr, beta1, beta2, eps, clip_k, seed, step, stream=None):
+    hp = AdamHp(lr, beta1, beta2, eps, clip_k)
+    _check("o5_adamw_step", lib().o5_adamw_step(_p(plan), _p(plan_dev), hp, int(seed), int(step), _stream(stream)))
+
+
+def o5_adamw_moments(plan, plan_dev, m, v, stream=None):
+    _check("o5_adamw_moments", lib().o5_adamw_moments(_p(plan), _p(plan_dev), _p(m), _p(v), _stream(stream)))
 
 
 def o5_f32_to_bf16(n, src, dst, stream=None):
