@@ -45,16 +45,14 @@ __device__ __forceinline__ float ld(const void* p, size_t i) {
 //   p_ij = oscale kscale l^(i-j) q_i . k_j
 //   S' = (r_{L-1} < 0) l^L S + sum_{j >= r_{L-1}} kscale l^(L-e-j) k_j v_j^T
 //
-// A block of 4 waves takes one state and runs through its chunks; a wave owns
-// a quarter of the state's columns in its accumulators.  Products are formed
-// transposed (o^T = S^T q^T, v^T p^T), so that the accumulators of S and the
-// tiles of p are, as they lie, operands of the next product.
+// A block of 4 waves takes one state and runs through its chunks; each wave
+// owns a quarter of the state's columns in its accumulators.  Products are
+// formed transposed (o^T = S^T q^T + v^T p^T), so that the accumulators of S
+// are, as they lie, operands of the next product.
 //
 // The reduction index of every product runs in blocks of 32; of a block, lane
 // group g = lane / 16 holds 4 g + r and 16 + 4 g + r (r = 0..3), which is how
-// two 16 x 16 accumulators hold their rows.  Rows of q, k and p lie in LDS with
-// the runs of 4 of a block in the order 0 4 1 5 2 6 3 7, so that a group's two
-// runs are one read.
+// two 16 x 16 accumulators hold their rows.
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -62,21 +60,30 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kPad = 16;  // bytes after each row in LDS: 16 rows start on 16 different groups of 4 banks
-
 template <typename E> struct Mx;
 
 template <> struct Mx<uint16_t> {
-  static constexpr int CL = 64;  // steps of a chunk
-  typedef bf16x8 Frag;
+  static constexpr int CL = 64;     // steps of a chunk
+  static constexpr int TERMS = 3;   // bf16 terms of an fp32 operand: 24 bits
+  // Rows in LDS: 8 rows of 32 bytes (a transposing read) then lie on 64 different banks, and with the 16-byte units
+  // of every second 8 rows exchanged in pairs so do 16 rows of 16 bytes (a read of rows).
+  static constexpr int PAD = 32;
+  static __device__ __forceinline__ int swap(int row) { return (row & 8) * 2; }
+  typedef u32x4 Frag;
   static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
-  static __device__ __forceinline__ Frag rows(const char* at) { return *reinterpret_cast<const Frag*>(at); }
-  // columns: rows 4 g + r and 16 + 4 g + r of column lane % 16, of a tile whose runs of 4 columns lie `run` bytes apart
-  template <int STRIDE, int RUN>
-  static __device__ __forceinline__ Frag columns(const char* tile, int lane) {
-    const char* p = tile + (4 * (lane >> 4) + ((lane & 15) >> 2)) * STRIDE + (lane & 3) * RUN;
+  // 4 g + r and 16 + 4 g + r of a row, `at` pointing to its block's element 4 g
+  static __device__ __forceinline__ Frag rows(const char* at) {
+    const u32x2 a = *reinterpret_cast<const u32x2*>(at), b = *reinterpret_cast<const u32x2*>(at + 32);
+    return Frag{a[0], a[1], b[0], b[1]};
+  }
+  // rows 4 g + r and 16 + 4 g + r of column lane % 16 of a tile: within 16 lanes, lane j of a transposing read
+  // takes 4 elements of row j / 4 from column 4 (j % 4) on and lane i receives the 4 rows of column i
+  template <int STRIDE, bool SWAP>
+  static __device__ __forceinline__ Frag columns(const char* block, int byte, int lane) {
+    const int row = 4 * (lane >> 4) + ((lane & 15) >> 2);
+    const char* p = block + row * STRIDE + ((byte + (lane & 3) * 8) ^ (SWAP ? swap(row) : 0));
     struct {
       s16x4 a, b;
     } f;
@@ -84,22 +91,22 @@ template <> struct Mx<uint16_t> {
     f.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 16 * STRIDE));
     return __builtin_bit_cast(Frag, f);
   }
-  static __device__ __forceinline__ float get(const Frag& f, int i) { return static_cast<float>(f[i]); }
-  static __device__ __forceinline__ void set(Frag& f, int i, float v) { f[i] = static_cast<__bf16>(v); }
+  static __device__ __forceinline__ float get(const Frag& f, int i) {
+    return __uint_as_float((i & 1) ? f[i / 2] & 0xffff0000u : f[i / 2] << 16);
+  }
+  static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
+    return Frag{f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]), f32x2_to_bf16x2(x[4], x[5]), f32x2_to_bf16x2(x[6], x[7])};
+  }
   static __device__ __forceinline__ void store4(void* p, f32x4 v) {
     *static_cast<u32x2*>(p) = u32x2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-  }
-  // 16 bytes of a row into LDS, their runs of 4 in the blocks' order
-  static __device__ __forceinline__ void put(char* row, int unit, u32x4 x) {
-    const int m = unit & 3;
-    char* p = row + (unit >> 2) * 64 + ((m & 1) * 4 + (m >> 1)) * 8;
-    *reinterpret_cast<u32x2*>(p) = u32x2{x[0], x[1]};
-    *reinterpret_cast<u32x2*>(p + 16) = u32x2{x[2], x[3]};
   }
 };
 
 template <> struct Mx<float> {
   static constexpr int CL = 32;
+  static constexpr int TERMS = 1;
+  static constexpr int PAD = 16;
+  static __device__ __forceinline__ int swap(int) { return 0; }
   struct Frag {
     f32x4 h[2];
   };
@@ -111,11 +118,11 @@ template <> struct Mx<float> {
     return c;
   }
   static __device__ __forceinline__ Frag rows(const char* at) {
-    return {{*reinterpret_cast<const f32x4*>(at), *reinterpret_cast<const f32x4*>(at + 16)}};
+    return {{*reinterpret_cast<const f32x4*>(at), *reinterpret_cast<const f32x4*>(at + 64)}};
   }
-  template <int STRIDE, int RUN>
-  static __device__ __forceinline__ Frag columns(const char* tile, int lane) {
-    const char* p = tile + 4 * (lane >> 4) * STRIDE + ((lane & 15) >> 2) * RUN + (lane & 3) * 4;
+  template <int STRIDE, bool SWAP>
+  static __device__ __forceinline__ Frag columns(const char* block, int byte, int lane) {
+    const char* p = block + 4 * (lane >> 4) * STRIDE + byte + (lane & 15) * 4;
     Frag f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -124,58 +131,74 @@ template <> struct Mx<float> {
     return f;
   }
   static __device__ __forceinline__ float get(const Frag& f, int i) { return f.h[i >> 2][i & 3]; }
-  static __device__ __forceinline__ void set(Frag& f, int i, float v) { f.h[i >> 2][i & 3] = v; }
-  static __device__ __forceinline__ void store4(void* p, f32x4 v) { *static_cast<f32x4*>(p) = v; }
-  static __device__ __forceinline__ void put(char* row, int unit, u32x4 x) {
-    const int q = unit & 7;
-    *reinterpret_cast<u32x4*>(row + (unit >> 3) * 128 + ((q & 3) * 2 + (q >> 2)) * 16) = x;
+  static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
+    return {{f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]}}};
   }
+  static __device__ __forceinline__ void store4(void* p, f32x4 v) { *static_cast<f32x4*>(p) = v; }
 };
 
-// l^n for n >= 0, exact at 0 (l2 = log2 l, -inf for l = 0).
+// l^n for n > 0 (l2 = log2 l, -inf for l = 0) and n = 0; for other n any number.
 __device__ __forceinline__ float power(float l2, int n) {
   return n == 0 ? 1.0f : __builtin_amdgcn_exp2f(l2 * static_cast<float>(n));
 }
+__device__ __forceinline__ float uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 template <typename E, int DA, int DC>
 struct Tiles {
-  static constexpr int CL = Mx<E>::CL, ES = sizeof(E);
-  static constexpr int QS = DA * ES + kPad, VS = DC * ES + kPad, PS = CL * ES + kPad;  // row strides
+  static constexpr int CL = Mx<E>::CL, ES = sizeof(E), PAD = Mx<E>::PAD;
+  static constexpr int QS = DA * ES + PAD, VS = DC * ES + PAD, PS = CL * ES + 16;  // row strides
   alignas(16) char q[CL * QS];
   alignas(16) char k[CL * QS];
   alignas(16) char v[CL * VS];
   alignas(16) char p[CL * PS];
 };
 
-// One operand's rows of a chunk on the way from memory to LDS.
-template <typename E, int D>
+// One operand's rows of a chunk on the way from memory to LDS, BT threads.
+template <typename E, int D, int BT>
 struct Stage {
-  static constexpr int CL = Mx<E>::CL, U = D * static_cast<int>(sizeof(E)) / 16, N = CL * U / 256, PER = 16 / sizeof(E);
+  static constexpr int CL = Mx<E>::CL, U = D * static_cast<int>(sizeof(E)) / 16, N = CL * U / BT, PER = 16 / sizeof(E);
+  static_assert(N >= 1 && CL * U % BT == 0, "every thread takes whole units");
   u32x4 x[N];
-  // rows u0 .. u0 + L - 1 of the pass's order; columns from `d` on are zero
-  __device__ __forceinline__ void load(const E* base, size_t ld, const LinPass& p, int b, int u0, int L, int d) {
+  // `base`: row 0 of the chunk; `step`: elements between rows; rows before `pad` and columns from d on are zero
+  __device__ __forceinline__ void load(const E* base, ptrdiff_t step, int pad, int d) {
+    int row = threadIdx.x / U;
+    const int c = threadIdx.x % U * PER;
+    asm volatile("" : "+v"(row));  // the address is worked out anew for each chunk: kept, it would cost two registers
+    const E* at = base + row * step + c;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int idx = threadIdx.x + n * 256, row = idx / U, c = (idx % U) * PER;
       x[n] = u32x4{0, 0, 0, 0};
-      if (row < L && c < d) {
-        const int t = p.rev ? p.T - 1 - (u0 + row) : u0 + row;
-        x[n] = *reinterpret_cast<const u32x4*>(base + (static_cast<size_t>(t) * p.B + b) * ld + c);
-      }
+      if (c < d && row + n * (BT / U) >= pad) x[n] = *reinterpret_cast<const u32x4*>(at + n * (BT / U) * step);
     }
   }
-  template <int STRIDE, bool PERM>
+  template <int STRIDE, bool SWAP>
   __device__ __forceinline__ void store(char* lds) const {
+    const int row = threadIdx.x / U, byte = threadIdx.x % U * 16;
+    static_assert(BT / U % 16 == 0 || !SWAP || Mx<E>::TERMS == 1 || N == 1, "a thread's rows exchange alike");
+    char* at = lds + row * STRIDE + (byte ^ (SWAP ? Mx<E>::swap(row) : 0));
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int idx = threadIdx.x + n * 256, row = idx / U, unit = idx % U;
-      if (PERM)
-        Mx<E>::put(lds + row * STRIDE, unit, x[n]);
-      else
-        *reinterpret_cast<u32x4*>(lds + row * STRIDE + unit * 16) = x[n];
-    }
+    for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(at + n * (BT / U) * STRIDE) = x[n];
   }
 };
+
+// Adds p_ij v_jc for the j of row i's episode whose v is not finite, columns c .. c + 3.
+template <typename E, typename TL>
+__device__ __forceinline__ f32x4 odd_terms(const TL& lds, int i, int ri, int c) {
+  f32x4 o = {0, 0, 0, 0};
+#pragma unroll 1
+  for (int j = max(ri, 0); j <= i; ++j) {
+    const float pj = elem<E>::to_f32(*reinterpret_cast<const E*>(lds.p + i * TL::PS + j * sizeof(E)));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float x = elem<E>::to_f32(*reinterpret_cast<const E*>(lds.v + j * TL::VS + (c + r) * sizeof(E)));
+      if (!finite(x)) o[r] = fmaf(pj, x, o[r]);
+    }
+  }
+  return o;
+}
 
 // Where the chunks of a split begin and what it starts from.
 struct Split {
@@ -186,24 +209,26 @@ struct Split {
 
 // kOut: write the outputs; else only add up each split's own part of the state.
 // kMany: gk > 1, the outputs are sums over the group.
+// Where T is no multiple of CL the first chunk is short: it starts `pad` steps
+// before step 0, and those rows are zero and not written.
 template <typename E, int DA, int DC, bool kOut, bool kMany>
-__global__ void __launch_bounds__(256, 2) linattn_chunks(LinPass p, Split sp) {
+__global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(LinPass p, Split sp) {
   typedef Mx<E> M;
   typedef typename M::Frag Frag;
   typedef Tiles<E, DA, DC> TL;
-  constexpr int CL = M::CL, ES = sizeof(E), NI = CL / 16, NB = CL / 32;
-  constexpr int NA = DA / 16, NC = DC / 64, NU = DA / 32;
+  constexpr int BT = 256, WAVES = 4, NC = DC / 64;
+  constexpr int CL = M::CL, ES = sizeof(E), NI = CL / 16, NB = CL / 32, NA = DA / 16, NU = DA / 32;
   __shared__ TL lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int heads = kOut ? p.nkv * p.gq : p.nkv;
   const int b = blockIdx.x / heads, hq = blockIdx.x % heads, n = kOut ? hq / p.gq : hq;
   const int chunks = (p.T + CL - 1) / CL;
   const int c0 = blockIdx.y * sp.chunks, c1 = min(chunks, c0 + sp.chunks);
-  const float l2 = log2f(p.decay[n]);
   const int e = p.rev ? 0 : 1;
   const int bn = b * p.nkv + n;
   const size_t sbase = static_cast<size_t>(bn) * p.da * p.dc;
-  const int cw = wave * (DC / 4);  // the wave's first column
+  const int col0 = wave * 16 * NC;  // the wave's first column
 
   // the state before the first chunk
   f32x4 S[NA][NC];
@@ -213,72 +238,97 @@ __global__ void __launch_bounds__(256, 2) linattn_chunks(LinPass p, Split sp) {
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
-      for (int c = 0; c < NC; ++c) S[a][c] = st[(a * NC + c) * 64 + lane];
+      for (int c = 0; c < NC; ++c) S[a][c] = st[(c * NA + a) * 64 + lane];
   } else {
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+    for (int c = 0; c < NC; ++c) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int row = a * 16 + g4 * 4, col = cw + c * 16 + l16;
-        S[a][c] = f32x4{0, 0, 0, 0};
-        if (kOut && p.s0 && row < p.da && col < p.dc) {
-          if (p.s0t) {
-            S[a][c] = *reinterpret_cast<const f32x4*>(p.s0 + sbase + static_cast<size_t>(col) * p.da + row);
-          } else {
+      for (int a = 0; a < NA; ++a) S[a][c] = f32x4{0, 0, 0, 0};
+      const int col = col0 + c * 16 + l16;
+      if (!kOut || !p.s0 || col >= p.dc) continue;
+      const float* s0 = p.s0 + sbase + (p.s0t ? col * p.da + g4 * 4 : g4 * 4 * p.dc + col);
+      if (p.s0t) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[a][c][r] = p.s0[sbase + static_cast<size_t>(row + r) * p.dc + col];
+        for (int a = 0; a < NA; ++a)
+          if (a * 16 + g4 * 4 < p.da) S[a][c] = *reinterpret_cast<const f32x4*>(s0 + a * 16);
+      } else {
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+          if (a * 16 + g4 * 4 < p.da) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[a][c][r] = s0[(a * 16 + r) * p.dc];
           }
-        }
       }
+    }
   }
 
-  const E* qb = static_cast<const E*>(p.q) + static_cast<size_t>(hq) * p.da;
-  const E* kb = static_cast<const E*>(p.k) + static_cast<size_t>(n) * p.gk * p.da;
-  const E* vb = static_cast<const E*>(p.v) + static_cast<size_t>(n) * p.gk * p.dc;
-  E* ob = static_cast<E*>(p.o) + static_cast<size_t>(hq) * p.dc;
-  Stage<E, DA> sq, sk;
-  Stage<E, DC> sv;
+  // powers of the decay
+  const float l2 = uniform(log2f(p.decay[n]));
+  const float l16th = uniform(power(l2, 16)), l32 = uniform(power(l2, 32)), l48 = l16th * l32;
+  float in[4];  // the factor on what enters the state from a chunk's last 16 steps
+#pragma unroll
+  for (int r = 0; r < 4; ++r) in[r] = p.kscale * power(l2, 16 - e - (g4 * 4 + r));
+  const float pscale = p.oscale * p.kscale;
+
+  const int pad0 = chunks * CL - p.T;
+  const ptrdiff_t dir = p.rev ? -p.B : p.B;
+  const ptrdiff_t qstep = dir * static_cast<ptrdiff_t>(p.ldq), kstep = dir * static_cast<ptrdiff_t>(p.ldk);
+  const ptrdiff_t vstep = dir * static_cast<ptrdiff_t>(p.ldv), ostep = dir * static_cast<ptrdiff_t>(p.ldo);
+  const ptrdiff_t row0 = static_cast<ptrdiff_t>(p.rev ? p.T - 1 : 0) * p.B + b;  // of the pass's step 0
+  typedef Stage<E, DA, BT> StQ;
+  typedef Stage<E, DC, BT> StV;
+  // row 0 of chunk c0 (before the buffer where that chunk starts with padding, which is not read)
+  const ptrdiff_t u00 = static_cast<ptrdiff_t>(c0) * CL - pad0;
+  const E* qb = static_cast<const E*>(p.q) + row0 * static_cast<ptrdiff_t>(p.ldq) + u00 * qstep + hq * p.da;
+  const E* kb = static_cast<const E*>(p.k) + row0 * static_cast<ptrdiff_t>(p.ldk) + u00 * kstep + n * p.gk * p.da;
+  const E* vb = static_cast<const E*>(p.v) + row0 * static_cast<ptrdiff_t>(p.ldv) + u00 * vstep + n * p.gk * p.dc;
+  E* ob = static_cast<E*>(p.o) + row0 * static_cast<ptrdiff_t>(p.ldo) + u00 * ostep + hq * p.dc;
+  StQ sq, sk;
+  StV sv;
   bool cut_any = false;  // a reset in this split so far
   f32x4 acc[kMany ? NI : 1][NC];
 
-  auto fetch = [&](int it) {  // the tiles of flat index it = chunk * gk + g
-    const int ch = c0 + (kMany ? it / p.gk : it), g = kMany ? it % p.gk : 0;
-    const int u0 = ch * CL, L = min(CL, p.T - u0);
-    if (kOut && g == 0) sq.load(qb, p.ldq, p, b, u0, L, p.da);
-    sk.load(kb + static_cast<size_t>(g) * p.da, p.ldk, p, b, u0, L, p.da);
-    sv.load(vb + static_cast<size_t>(g) * p.dc, p.ldv, p, b, u0, L, p.dc);
+  auto fetch = [&](int ch, int g) {
+    const int pad = ch == 0 ? pad0 : 0;
+    const ptrdiff_t u = static_cast<ptrdiff_t>(ch - c0) * CL;
+    if (kOut && (!kMany || g == 0)) sq.load(qb + u * qstep, qstep, pad, p.da);
+    sk.load(kb + u * kstep + g * p.da, kstep, pad, p.da);
+    sv.load(vb + u * vstep + g * p.dc, vstep, pad, p.dc);
   };
 
-  const int total = (c1 - c0) * (kMany ? p.gk : 1);
-  fetch(0);
-  for (int it = 0; it < total; ++it) {
-    const int g = kMany ? it % p.gk : 0, u0 = (c0 + (kMany ? it / p.gk : it)) * CL, L = min(CL, p.T - u0);
-    const bool first = g == 0, last = !kMany || g == p.gk - 1;
-    const int ni = (L + 15) / 16, nb = (L + 31) / 32;
+  int ch = c0, g = 0;
+  fetch(ch, g);
+  while (ch < c1) {
+    const int pad = ch == 0 ? pad0 : 0, u0 = ch * CL - pad0;
+    const bool first = !kMany || g == 0, last = !kMany || g == p.gk - 1;
     if (kOut && first) sq.template store<TL::QS, true>(lds.q);
     sk.template store<TL::QS, true>(lds.k);
     sv.template store<TL::VS, false>(lds.v);
     // bit i: a reset before the chunk's step i
-    bool flag = false;
-    if (p.reset && lane < L) {
+    uint64_t resets = 0;
+    if (p.reset) {
+      bool flag = false;
       const int u = u0 + lane;
-      if (!p.rev)
-        flag = p.reset[static_cast<size_t>(u) * p.B + b] != 0;
-      else if (u > 0)
-        flag = p.reset[static_cast<size_t>(p.T - u) * p.B + b] != 0;
+      if (lane < CL && u >= (p.rev ? 1 : 0)) flag = p.reset[static_cast<size_t>(p.rev ? p.T - u : u) * p.B + b] != 0;
+      resets = __ballot(flag);
     }
-    const uint64_t resets = __ballot(flag);
-    const int rl = resets ? 63 - __builtin_clzll(resets) : -1;  // r of the chunk's last step
-    auto last_reset = [&](int i) {
-      const uint64_t m = resets & (~0ull >> (63 - i));
-      return m ? 63 - __builtin_clzll(m) : -1;
-    };
+    const int rl = resets ? 63 - __builtin_clzll(resets) : -1;  // the last reset
+    int lr = -1;  // the last reset at or before step `lane`
+    if (resets) {
+      int x = 63 - lane;
+      asm volatile("" : "+v"(x));  // (else the mask is kept in registers from chunk to chunk)
+      const uint64_t m = resets & (~0ull >> x);
+      lr = m ? 63 - __builtin_clzll(m) : -1;
+    }
+    auto last_reset = [&](int ti) { return resets ? __shfl(lr, ti * 16 + l16) : -1; };  // of step 16 ti + l16
     __syncthreads();
-    if (it + 1 < total) fetch(it + 1);
+    int nch = ch, ng = g + 1;
+    if (!kMany || ng == p.gk) ++nch, ng = 0;
+    if (nch < c1) fetch(nch, ng);
 
     if (kOut) {  // p, 16 x 16 tiles at and below the diagonal, one after another to the waves
       constexpr int kTiles = NI * (NI + 1) / 2;
-      for (int x = wave; x < kTiles + NI / 2; x += 4) {
+      for (int x = wave; x < kTiles + NI / 2; x += WAVES) {
         int ti, tj;
         if (x < kTiles) {
           ti = x >= 6 ? 3 : x >= 3 ? 2 : x >= 1 ? 1 : 0;
@@ -287,169 +337,187 @@ __global__ void __launch_bounds__(256, 2) linattn_chunks(LinPass p, Split sp) {
           ti = (x - kTiles) * 2;
           tj = ti + 1;
         }
-        if (ti >= ni) continue;
         f32x4 s = {0, 0, 0, 0};
         const int i = ti * 16 + l16;
         if (tj <= ti) {
+          const char* kr = lds.k + (tj * 16 + l16) * TL::QS + ((g4 * 4 * ES) ^ M::swap(l16));
+          const char* qr = lds.q + i * TL::QS + ((g4 * 4 * ES) ^ M::swap(l16));
 #pragma unroll
-          for (int u = 0; u < NU; ++u) {
-            const Frag fk = M::rows(lds.k + (tj * 16 + l16) * TL::QS + u * 32 * ES + g4 * 8 * ES);
-            const Frag fq = M::rows(lds.q + i * TL::QS + u * 32 * ES + g4 * 8 * ES);
-            s = M::mma(fk, fq, s);
-          }
-          const int ri = last_reset(i);
-          const float f = p.oscale * p.kscale;
+          for (int u = 0; u < NU; ++u) s = M::mma(M::rows(kr + u * 32 * ES), M::rows(qr + u * 32 * ES), s);
+          const int ri = last_reset(ti);
+          const int d0 = i - tj * 16 - g4 * 4;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = tj * 16 + g4 * 4 + r;
-            s[r] = (j <= i && j >= ri) ? s[r] * (f * power(l2, max(i - j, 0))) : 0.0f;
-          }
+          for (int r = 0; r < 4; ++r)  // (a select: outside the mask the product may be anything)
+            s[r] = static_cast<unsigned>(d0 - r) <= static_cast<unsigned>(ri < 0 ? i : i - ri) ? s[r] * (pscale * power(l2, d0 - r)) : 0.0f;
         }
-        M::store4(lds.p + i * TL::PS + (tj >> 1) * 32 * ES + (g4 * 2 + (tj & 1)) * 4 * ES, s);
+        M::store4(lds.p + i * TL::PS + (tj * 16 + g4 * 4) * ES, s);
       }
       __syncthreads();
     }
 
     // the wave's columns of v
     Frag vf[NC][NB];
+    float odd = 0.0f;
+    auto read_v = [&](int c, int u) {
+      return M::template columns<TL::VS, false>(lds.v + u * 32 * TL::VS, (col0 + c * 16) * ES, lane);
+    };
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int u = 0; u < NB; ++u)
-        vf[c][u] = M::template columns<TL::VS, 4 * ES>(lds.v + u * 32 * TL::VS + (cw + c * 16) * ES, lane);
+      for (int u = 0; u < NB; ++u) {
+        vf[c][u] = read_v(c, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd = fmaf(M::get(vf[c][u], i), 0.0f, odd);
+      }
+    const bool any_odd = __any(!(odd == 0.0f));  // an infinity or NaN in them
 
     if (kOut) {
-      // an infinity or NaN in v may not meet the zeros of p: it is taken out of the product and added one by one
-      float odd = 0.0f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int u = 0; u < NB; ++u)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) odd = fmaf(M::get(vf[c][u], i), 0.0f, odd);
-      const bool any_odd = __any(!(odd == 0.0f));
-      Frag vp[NC][NB];
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-          vp[c][u] = vf[c][u];
-          if (any_odd) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (!(M::get(vf[c][u], i) * 0.0f == 0.0f)) M::set(vp[c][u], i, 0.0f);
-          }
-        }
-      Frag sf[NC][NU];
-      if (first) {
+      if (any_odd) {  // it may not meet the zeros of p: it is taken out of the product and added term by term
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int u = 0; u < NU; ++u)
+          for (int u = 0; u < NB; ++u) {
+            float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) M::set(sf[c][u], i, S[2 * u + (i >> 2)][c][i & 3]);
+            for (int i = 0; i < 8; ++i) x[i] = finite(M::get(vf[c][u], i)) ? M::get(vf[c][u], i) : 0.0f;
+            vf[c][u] = M::pack(x);
+          }
       }
+      Frag sf[NC][NU];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          const f32x4 x = S[2 * u][c], y = S[2 * u + 1][c];
+          const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+          sf[c][u] = M::pack(z);
+        }
+      int lrow = l16;
+      asm volatile("" : "+v"(lrow));
+      E* orow = ob + static_cast<ptrdiff_t>(ch - c0) * CL * ostep + lrow * ostep + col0 + g4 * 4;
+      const char* qr = lds.q + l16 * TL::QS + ((g4 * 4 * ES) ^ M::swap(l16));
+      const char* pr = lds.p + l16 * TL::PS + g4 * 4 * ES;
 #pragma unroll
       for (int ti = 0; ti < NI; ++ti) {
-        if (ti >= ni) break;
-        f32x4(&o)[NC] = acc[kMany ? ti : 0];
-        const int i = ti * 16 + l16, ri = last_reset(i);
+        if (ti * 16 + 16 <= pad) continue;
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 o[NC];
+        const int i = ti * 16 + l16;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c] = f32x4{0, 0, 0, 0};
         if (first) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] = f32x4{0, 0, 0, 0};
-#pragma unroll
           for (int u = 0; u < NU; ++u) {
-            const Frag fq = M::rows(lds.q + i * TL::QS + u * 32 * ES + g4 * 8 * ES);
+            const Frag fq = M::rows(qr + ti * 16 * TL::QS + u * 32 * ES);
 #pragma unroll
             for (int c = 0; c < NC; ++c) o[c] = M::mma(sf[c][u], fq, o[c]);
           }
-          const float f = p.oscale * power(l2, i + e);
+          const float f = p.oscale * power(l2, i - pad + e);
+          const bool carried = last_reset(ti) < 0;
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[c][r] = ri < 0 ? o[c][r] * f : 0.0f;
+            for (int r = 0; r < 4; ++r) o[c][r] = carried ? o[c][r] * f : 0.0f;
+        } else {
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c] = acc[kMany ? ti : 0][c];
         }
 #pragma unroll
         for (int u = 0; u < ti / 2 + 1; ++u) {
-          const Frag fp = M::rows(lds.p + i * TL::PS + u * 32 * ES + g4 * 8 * ES);
+          const Frag fp = M::rows(pr + ti * 16 * TL::PS + u * 32 * ES);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] = M::mma(vp[c][u], fp, o[c]);
+          for (int c = 0; c < NC; ++c) o[c] = M::mma(vf[c][u], fp, o[c]);
         }
-        if (any_odd) {
-#pragma unroll 1
-          for (int j = max(ri, 0); j <= i; ++j) {
-            const int q = (j >> 2) & 7;
-            const E pj = *reinterpret_cast<const E*>(lds.p + i * TL::PS + (j >> 5) * 32 * ES +
-                                                     (((q & 3) * 2 + (q >> 2)) * 4 + (j & 3)) * ES);
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const E vj = *reinterpret_cast<const E*>(lds.v + j * TL::VS + (cw + c * 16 + g4 * 4 + r) * ES);
-                const float x = elem<E>::to_f32(vj);
-                if (!(x * 0.0f == 0.0f)) o[c][r] = fmaf(elem<E>::to_f32(pj), x, o[c][r]);
-              }
-          }
-        }
-        if (last && i < L) {
-          const int t = p.rev ? p.T - 1 - (u0 + i) : u0 + i;
-          E* row = ob + (static_cast<size_t>(t) * p.B + b) * p.ldo;
+        if (kMany) {
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            const int col = cw + c * 16 + g4 * 4;
-            if (col < p.dc) M::store4(row + col, o[c]);
+            if (any_odd) o[c] += odd_terms<E>(lds, i, last_reset(ti), col0 + c * 16 + g4 * 4);
+            acc[ti][c] = o[c];
           }
         }
+        if (last && i >= pad) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (col0 + c * 16 + g4 * 4 < p.dc) M::store4(orow + ti * 16 * ostep + c * 16, o[c]);
+        }
       }
+      if (any_odd) {
+#pragma unroll 1
+        for (int x = kMany ? NI * NC : 0; x < NI * NC; ++x) {  // onto what this lane has just written
+          const int ti = x / NC, c = x % NC, i = ti * 16 + l16, ri = last_reset(ti);
+          if (i < pad || col0 + c * 16 + g4 * 4 >= p.dc) continue;
+          E* at = orow + ti * 16 * ostep + c * 16;
+          f32x4 o;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[r] = elem<E>::to_f32(at[r]);
+          M::store4(at, o + odd_terms<E>(lds, i, ri, col0 + c * 16 + g4 * 4));
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int u = 0; u < NB; ++u) vf[c][u] = read_v(c, u);
+      }
+    }
+
+    if (rl > 0) {  // a key that is cut off may hold anything, and may not meet the zeros of what enters
+      for (int x = tid; x < rl * (TL::QS / 16); x += BT) *reinterpret_cast<u32x4*>(lds.k + x * 16) = u32x4{0, 0, 0, 0};
+      __syncthreads();
     }
 
     // the state after the chunk
     if (first) {
-      const float f = power(l2, L);
+      if (resets) {
+        cut_any = true;
 #pragma unroll
-      for (int a = 0; a < NA; ++a)
+        for (int a = 0; a < NA; ++a)
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+          for (int c = 0; c < NC; ++c) S[a][c] = f32x4{0, 0, 0, 0};
+      } else {
+        const float f = uniform(power(l2, CL - pad));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[a][c][r] = rl < 0 ? S[a][c][r] * f : 0.0f;
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) S[a][c] *= f;
+      }
     }
-    cut_any = cut_any || rl >= 0;
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
-      if (u >= nb) break;
-      // what enters: in bf16 as a (hi, lo) pair, which keeps 16 bits of it
-      Frag hi[NC], lo[NC];
+      if (u * 32 + 32 <= pad) continue;
+      __builtin_amdgcn_sched_barrier(0);
+      // what enters, in bf16 as a sum of terms
+      Frag term[NC][M::TERMS];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int j = u * 32 + (i >> 2) * 16 + g4 * 4 + (i & 3);
-        const float w = p.kscale * power(l2, max(L - e - j, 0));
+      for (int c = 0; c < NC; ++c) {
+        float x[8];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const float x = j >= rl ? M::get(vf[c][u], i) * w : 0.0f;
-          M::set(hi[c], i, x);
-          if (ES == 2) {
-            const float y = M::get(hi[c], i);
-            M::set(lo[c], i, (y * 0.0f == 0.0f) ? x - y : 0.0f);
-          }
+        for (int i = 0; i < 8; ++i) {
+          const int tiles = NI - 1 - (2 * u + (i >> 2));
+          x[i] = (M::get(vf[c][u], i) * in[i & 3]) * (tiles == 0 ? 1.0f : tiles == 1 ? l16th : tiles == 2 ? l32 : l48);
+        }
+        if (rl > u * 32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = u * 32 + (i >> 2) * 16 + g4 * 4 + (i & 3) >= rl ? x[i] : 0.0f;
+        }
+        term[c][0] = M::pack(x);
+#pragma unroll
+        for (int t = 1; t < M::TERMS; ++t) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] -= M::get(term[c][t - 1], i);
+          term[c][t] = M::pack(x);
         }
       }
 #pragma unroll
       for (int a = 0; a < NA; ++a) {
-        Frag kf = M::template columns<TL::QS, 8 * ES>(
-            lds.k + u * 32 * TL::QS + (a >> 1) * 32 * ES + (a & 1) * 4 * ES, lane);
-        if (rl > u * 32) {
+        const Frag kf = M::template columns<TL::QS, true>(lds.k + u * 32 * TL::QS, a * 16 * ES, lane);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (u * 32 + (i >> 2) * 16 + g4 * 4 + (i & 3) < rl) M::set(kf, i, 0.0f);
-        }
+        for (int t = M::TERMS - 1; t >= 0; --t)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          S[a][c] = M::mma(kf, hi[c], S[a][c]);
-          if (ES == 2) S[a][c] = M::mma(kf, lo[c], S[a][c]);
-        }
+          for (int c = 0; c < NC; ++c) S[a][c] = M::mma(kf, term[c][t], S[a][c]);
       }
     }
     __syncthreads();
+    ch = nch;
+    g = ng;
   }
 
   if (kOut && sp.states) return;  // the scan has written the last state
@@ -459,28 +527,30 @@ __global__ void __launch_bounds__(256, 2) linattn_chunks(LinPass p, Split sp) {
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
-      for (int c = 0; c < NC; ++c) st[(a * NC + c) * 64 + lane] = S[a][c];
+      for (int c = 0; c < NC; ++c) st[(c * NA + a) * 64 + lane] = S[a][c];
     if (tid == 0)
       sp.keep[static_cast<size_t>(blockIdx.y) * p.B * p.nkv + bn] =
-          cut_any ? -1.0f : power(l2, min(p.T, c1 * CL) - c0 * CL);
+          cut_any ? -1.0f : power(l2, (c1 - c0) * CL - (c0 == 0 ? pad0 : 0));
     return;
   }
-  if (p.sT && (kMany || hq % p.gq == 0)) {
-    const bool cut = p.rev && p.reset && p.reset[b] != 0;
+  if (!p.sT || (!kMany && hq % p.gq != 0)) return;
+  const bool cut = p.rev && p.reset && p.reset[b] != 0;
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+  for (int c = 0; c < NC; ++c) {
+    const int col = col0 + c * 16 + l16;
+    if (col >= p.dc) continue;
+    float* sT = p.sT + sbase + (p.s0t ? col * p.da + g4 * 4 : g4 * 4 * p.dc + col);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int row = a * 16 + g4 * 4, col = cw + c * 16 + l16;
-        if (row >= p.da || col >= p.dc) continue;
-        const f32x4 x = cut ? f32x4{0, 0, 0, 0} : S[a][c];
-        if (p.s0t) {
-          *reinterpret_cast<f32x4*>(p.sT + sbase + static_cast<size_t>(col) * p.da + row) = x;
-        } else {
+    for (int a = 0; a < NA; ++a) {
+      if (a * 16 + g4 * 4 >= p.da) continue;
+      const f32x4 x = cut ? f32x4{0, 0, 0, 0} : S[a][c];
+      if (p.s0t) {
+        *reinterpret_cast<f32x4*>(sT + a * 16) = x;
+      } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) p.sT[sbase + static_cast<size_t>(row + r) * p.dc + col] = x[r];
-        }
+        for (int r = 0; r < 4; ++r) sT[(a * 16 + r) * p.dc] = x[r];
       }
+    }
   }
 }
 
@@ -489,12 +559,12 @@ __global__ void __launch_bounds__(256, 2) linattn_chunks(LinPass p, Split sp) {
 // column (one accumulator).
 template <int DA, int DC>
 __global__ void __launch_bounds__(256) linattn_scan(LinPass p, Split sp, int splits) {
-  constexpr int NA = DA / 16, NC = DC / 64, Q = DA * DC / 4;
+  constexpr int NA = DA / 16, Q = DA * DC / 4;
   const size_t idx = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
   const int states = p.B * p.nkv;
   const int bn = static_cast<int>(idx / Q), x = static_cast<int>(idx % Q);
-  const int lane = x & 63, tile = x >> 6, c = tile % NC, a = tile / NC % NA, wave = tile / (NC * NA);
-  const int row = a * 16 + (lane >> 4) * 4, col = wave * (DC / 4) + c * 16 + (lane & 15);
+  const int lane = x & 63, tile = x >> 6;
+  const int row = tile % NA * 16 + (lane >> 4) * 4, col = tile / NA * 16 + (lane & 15);
   const bool in = row < p.da && col < p.dc;
   const size_t at = static_cast<size_t>(bn) * p.da * p.dc;
   f32x4 X = {0, 0, 0, 0};
