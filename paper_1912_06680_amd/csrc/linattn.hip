@@ -94,6 +94,13 @@ template <> struct Mx<uint16_t> {
   static __device__ __forceinline__ float get(const Frag& f, int i) {
     return __uint_as_float((i & 1) ? f[i / 2] & 0xffff0000u : f[i / 2] << 16);
   }
+  // whether a value that is not finite went past: the largest magnitude's bits so far
+  typedef uint16_t Odd __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ void look(const Frag& f, Odd& odd) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd = __builtin_elementwise_max(odd, __builtin_bit_cast(Odd, f[i] & 0x7fff7fffu));
+  }
+  static __device__ __forceinline__ bool found(Odd odd) { return odd[0] >= 0x7f80 || odd[1] >= 0x7f80; }
   static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
     return Frag{f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]), f32x2_to_bf16x2(x[4], x[5]), f32x2_to_bf16x2(x[6], x[7])};
   }
@@ -131,6 +138,12 @@ template <> struct Mx<float> {
     return f;
   }
   static __device__ __forceinline__ float get(const Frag& f, int i) { return f.h[i >> 2][i & 3]; }
+  typedef float Odd;
+  static __device__ __forceinline__ void look(const Frag& f, Odd& odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) odd = fmaf(get(f, i), 0.0f, odd);
+  }
+  static __device__ __forceinline__ bool found(Odd odd) { return !(odd == 0.0f); }
   static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
     return {{f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]}}};
   }
@@ -168,10 +181,15 @@ struct Stage {
     const int c = threadIdx.x % U * PER;
     asm volatile("" : "+v"(row));  // the address is worked out anew for each chunk: kept, it would cost two registers
     const E* at = base + row * step + c;
+    if (pad == 0 && d == D) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      x[n] = u32x4{0, 0, 0, 0};
-      if (c < d && row + n * (BT / U) >= pad) x[n] = *reinterpret_cast<const u32x4*>(at + n * (BT / U) * step);
+      for (int n = 0; n < N; ++n) x[n] = *reinterpret_cast<const u32x4*>(at + n * (BT / U) * step);
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        x[n] = u32x4{0, 0, 0, 0};
+        if (c < d && row + n * (BT / U) >= pad) x[n] = *reinterpret_cast<const u32x4*>(at + n * (BT / U) * step);
+      }
     }
   }
   template <int STRIDE, bool SWAP>
@@ -207,12 +225,19 @@ struct Split {
   float* keep;      // [splits][B * nkv]: the factor on the state across the split, -1 where a reset cuts it off
 };
 
+// The passes of one launch: alike in T, B, nkv and gq, and in the kernel that runs them.
+struct Passes {
+  int count;
+  LinPass pass[3];
+  Split split[3];
+};
+
 // kOut: write the outputs; else only add up each split's own part of the state.
 // kMany: gk > 1, the outputs are sums over the group.
 // Where T is no multiple of CL the first chunk is short: it starts `pad` steps
 // before step 0, and those rows are zero and not written.
 template <typename E, int DA, int DC, bool kOut, bool kMany>
-__global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(LinPass p, Split sp) {
+__global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Passes ps) {
   typedef Mx<E> M;
   typedef typename M::Frag Frag;
   typedef Tiles<E, DA, DC> TL;
@@ -221,8 +246,12 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Li
   __shared__ TL lds;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (the passes of a call read the same rows: side by side, so that they find them in the caches)
+  const LinPass& p = ps.pass[blockIdx.x % ps.count];
+  const Split& sp = ps.split[blockIdx.x % ps.count];
+  const int block = blockIdx.x / ps.count;
   const int heads = kOut ? p.nkv * p.gq : p.nkv;
-  const int b = blockIdx.x / heads, hq = blockIdx.x % heads, n = kOut ? hq / p.gq : hq;
+  const int b = block / heads, hq = block % heads, n = kOut ? hq / p.gq : hq;
   const int chunks = (p.T + CL - 1) / CL;
   const int c0 = blockIdx.y * sp.chunks, c1 = min(chunks, c0 + sp.chunks);
   const int e = p.rev ? 0 : 1;
@@ -357,7 +386,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Li
 
     // the wave's columns of v
     Frag vf[NC][NB];
-    float odd = 0.0f;
+    typename M::Odd odd = {};
     auto read_v = [&](int c, int u) {
       return M::template columns<TL::VS, false>(lds.v + u * 32 * TL::VS, (col0 + c * 16) * ES, lane);
     };
@@ -366,10 +395,9 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Li
 #pragma unroll
       for (int u = 0; u < NB; ++u) {
         vf[c][u] = read_v(c, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) odd = fmaf(M::get(vf[c][u], i), 0.0f, odd);
+        M::look(vf[c][u], odd);
       }
-    const bool any_odd = __any(!(odd == 0.0f));  // an infinity or NaN in them
+    const bool any_odd = __any(M::found(odd));  // an infinity or NaN in them
 
     if (kOut) {
       if (any_odd) {  // it may not meet the zeros of p: it is taken out of the product and added term by term
@@ -413,11 +441,15 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Li
             for (int c = 0; c < NC; ++c) o[c] = M::mma(sf[c][u], fq, o[c]);
           }
           const float f = p.oscale * power(l2, i - pad + e);
-          const bool carried = last_reset(ti) < 0;
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+          for (int c = 0; c < NC; ++c) o[c] *= f;
+          if (resets) {
+            const bool carried = last_reset(ti) < 0;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[c][r] = carried ? o[c][r] * f : 0.0f;
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[c][r] = carried ? o[c][r] : 0.0f;
+          }
         } else {
 #pragma unroll
           for (int c = 0; c < NC; ++c) o[c] = acc[kMany ? ti : 0][c];
@@ -558,8 +590,10 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Li
 // state: X_0 = S0, X_{s+1} = keep_s X_s + part_s.  A thread takes 4 rows of a
 // column (one accumulator).
 template <int DA, int DC>
-__global__ void __launch_bounds__(256) linattn_scan(LinPass p, Split sp, int splits) {
+__global__ void __launch_bounds__(256) linattn_scan(Passes ps, int splits) {
   constexpr int NA = DA / 16, Q = DA * DC / 4;
+  const LinPass& p = ps.pass[blockIdx.y];
+  const Split& sp = ps.split[blockIdx.y];
   const size_t idx = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
   const int states = p.B * p.nkv;
   const int bn = static_cast<int>(idx / Q), x = static_cast<int>(idx % Q);
@@ -610,54 +644,82 @@ int plan_splits(o5_dtype dt, int T, int B, int nkv, int gq) {
   return std::max(1, std::min(want, chunks / 4));
 }
 
-size_t pass_workspace(o5_dtype dt, int T, int B, int nkv, int gq, int da, int dc) {
+// Workspace of any of a call's launches: `count` passes at most, each with as many splits as if it ran alone.
+size_t pass_workspace(o5_dtype dt, int T, int B, int nkv, int gq, int da, int dc, int count) {
   const int splits = plan_splits(dt, T, B, nkv, gq);
   if (splits == 1) return 0;
-  return align_up(static_cast<size_t>(splits) * B * nkv * (pad_head(da) * pad_head(dc) + 1) * sizeof(float));
+  const size_t floats = static_cast<size_t>(splits) * B * nkv * (pad_head(da) * pad_head(dc) + 1);
+  return align_up(floats, 64) * sizeof(float) * count;
+}
+
+size_t pass_floats(const LinPass& p, int splits) {
+  return static_cast<size_t>(splits) * p.B * p.nkv * (pad_head(p.da) * pad_head(p.dc) + 1);
+}
+
+template <typename E, int DA, int DC, bool kMany>
+void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
+  const LinPass& p = ps.pass[0];
+  const int chunks = (p.T + Mx<E>::CL - 1) / Mx<E>::CL;
+  const unsigned states = static_cast<unsigned>(p.B) * p.nkv;
+  const int per = (chunks + splits - 1) / splits, used = (chunks + per - 1) / per;
+  for (int i = 0; i < ps.count; ++i) {
+    ps.split[i] = {per, nullptr, nullptr};
+    if (splits > 1) {
+      ps.split[i].states = ws;
+      ps.split[i].keep = ws + static_cast<size_t>(used) * states * DA * DC;
+      ws += align_up(pass_floats(ps.pass[i], splits), 64);
+    }
+  }
+  if (splits > 1) {
+    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany>), dim3(states * ps.count, used), dim3(256), 0, s, ps);
+    hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
+  }
+  hipLaunchKernelGGL((linattn_chunks<E, DA, DC, true, kMany>), dim3(states * p.gq * ps.count, used), dim3(256), 0, s, ps);
 }
 
 template <typename E, int DA, int DC>
-void launch_chunks(o5_dtype dt, const LinPass& p, void* ws, hipStream_t s) {
-  const int splits = plan_splits(dt, p.T, p.B, p.nkv, p.gq);
-  const int chunks = (p.T + Mx<E>::CL - 1) / Mx<E>::CL;
-  const unsigned states = static_cast<unsigned>(p.B) * p.nkv;
-  Split sp = {chunks, nullptr, nullptr};
-  int used = 1;
-  if (splits > 1) {
-    sp.chunks = (chunks + splits - 1) / splits;
-    used = (chunks + sp.chunks - 1) / sp.chunks;
-    sp.states = static_cast<float*>(ws);
-    sp.keep = sp.states + static_cast<size_t>(used) * states * DA * DC;
-    if (p.gk > 1)
-      hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, true>), dim3(states, used), dim3(256), 0, s, p, sp);
-    else
-      hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, false>), dim3(states, used), dim3(256), 0, s, p, sp);
-    hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024)), dim3(256), 0, s, p, sp, used);
-  }
-  if (p.gk > 1)
-    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, true, true>), dim3(states * p.gq, used), dim3(256), 0, s, p, sp);
+void launch_many(Passes& ps, float* ws, int splits, hipStream_t s) {
+  if (ps.pass[0].gk > 1)
+    launch_chunks<E, DA, DC, true>(ps, ws, splits, s);
   else
-    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, true, false>), dim3(states * p.gq, used), dim3(256), 0, s, p, sp);
+    launch_chunks<E, DA, DC, false>(ps, ws, splits, s);
 }
 
 template <typename E>
-void launch_typed(o5_dtype dt, const LinPass& p, void* ws, hipStream_t s) {
-  const bool a = p.da <= 64, c = p.dc <= 64;
+void launch_typed(Passes& ps, float* ws, int splits, hipStream_t s) {
+  const bool a = ps.pass[0].da <= 64, c = ps.pass[0].dc <= 64;
   if (a && c)
-    launch_chunks<E, 64, 64>(dt, p, ws, s);
+    launch_many<E, 64, 64>(ps, ws, splits, s);
   else if (a)
-    launch_chunks<E, 64, 128>(dt, p, ws, s);
+    launch_many<E, 64, 128>(ps, ws, splits, s);
   else if (c)
-    launch_chunks<E, 128, 64>(dt, p, ws, s);
+    launch_many<E, 128, 64>(ps, ws, splits, s);
   else
-    launch_chunks<E, 128, 128>(dt, p, ws, s);
+    launch_many<E, 128, 128>(ps, ws, splits, s);
 }
 
-void launch_pass(o5_dtype dt, const LinPass& p, void* ws, hipStream_t s) {
-  if (dt == O5_BF16)
-    launch_typed<uint16_t>(dt, p, ws, s);
-  else
-    launch_typed<float>(dt, p, ws, s);
+// Whether one kernel runs both passes.
+bool alike(const LinPass& x, const LinPass& y) {
+  return pad_head(x.da) == pad_head(y.da) && pad_head(x.dc) == pad_head(y.dc) && x.gq == y.gq && x.gk == y.gk;
+}
+
+// Passes of one call in as few launches as they allow.
+void launch_passes(o5_dtype dt, const LinPass* p, int count, void* ws, hipStream_t s) {
+  bool done[3] = {};
+  for (int i = 0; i < count; ++i) {
+    if (done[i]) continue;
+    Passes ps = {};
+    for (int j = i; j < count; ++j)
+      if (!done[j] && alike(p[i], p[j])) {
+        ps.pass[ps.count++] = p[j];
+        done[j] = true;
+      }
+    const int splits = plan_splits(dt, p[i].T, p[i].B, p[i].nkv, p[i].gq * ps.count);
+    if (dt == O5_BF16)
+      launch_typed<uint16_t>(ps, static_cast<float*>(ws), splits, s);
+    else
+      launch_typed<float>(ps, static_cast<float*>(ws), splits, s);
+  }
 }
 
 // ----------------------------------------------------------- single token
@@ -785,7 +847,7 @@ using namespace o5;
 
 extern "C" size_t o5_linattn_fwd_workspace_bytes(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv) {
   if (check_sizes("o5_linattn_fwd_workspace_bytes", dt, T, B, nh, nkv, dk, dv) != O5_OK) return 0;
-  return std::max<size_t>(256, pass_workspace(dt, T, B, nkv, nh / nkv, dk, dv));
+  return std::max<size_t>(256, pass_workspace(dt, T, B, nkv, nh / nkv, dk, dv, 1));
 }
 
 extern "C" int o5_linattn_fwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv, const void* q, size_t ldq,
@@ -805,13 +867,13 @@ extern "C" int o5_linattn_fwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk
   O5_PTR(ws, "ws");
   const LinPass p = {q, k, v, o, ldq, ldk, ldv, ldo, decay, reset, S0, ST, T, B, nkv, nh / nkv, 1, dk, dv, scale, 1.0f,
                      false, false};
-  launch_pass(dt, p, ws, as_stream(stream));
+  launch_passes(dt, &p, 1, ws, as_stream(stream));
   return check_launch(fn);
 }
 
 extern "C" size_t o5_linattn_bwd_workspace_bytes(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv) {
   if (check_sizes("o5_linattn_bwd_workspace_bytes", dt, T, B, nh, nkv, dk, dv) != O5_OK) return 0;
-  return std::max<size_t>({256, pass_workspace(dt, T, B, nkv, nh / nkv, dv, dk), pass_workspace(dt, T, B, nkv, 1, dk, dv)});
+  return std::max<size_t>(256, pass_workspace(dt, T, B, nkv, 1, dk, dv, 3));
 }
 
 extern "C" int o5_linattn_bwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk, int dv, const void* q, size_t ldq,
@@ -838,13 +900,11 @@ extern "C" int o5_linattn_bwd(o5_dtype dt, int T, int B, int nh, int nkv, int dk
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
   const int G = nh / nkv;
-  const LinPass pq = {dout, v, k, dq, lddo, ldv, ldk, lddq, decay, reset, S0, nullptr, T, B, nkv, G, 1, dv, dk, scale,
-                      1.0f, true, false};
-  const LinPass pv = {k, q, dout, dval, ldk, ldq, lddo, lddv, decay, reset, dST, dS0, T, B, nkv, 1, G, dk, dv, 1.0f,
-                      scale, false, true};
-  const LinPass pk = {v, dout, q, dkey, ldv, lddo, ldq, lddk, decay, reset, dST, nullptr, T, B, nkv, 1, G, dv, dk, 1.0f,
-                      scale, true, true};
-  for (const LinPass* p : {&pq, &pv, &pk}) launch_pass(dt, *p, ws, as_stream(stream));
+  const LinPass p[3] = {
+      {dout, v, k, dq, lddo, ldv, ldk, lddq, decay, reset, S0, nullptr, T, B, nkv, G, 1, dv, dk, scale, 1.0f, true, false},
+      {k, q, dout, dval, ldk, ldq, lddo, lddv, decay, reset, dST, dS0, T, B, nkv, 1, G, dk, dv, 1.0f, scale, false, true},
+      {v, dout, q, dkey, ldv, lddo, ldq, lddk, decay, reset, dST, nullptr, T, B, nkv, 1, G, dv, dk, 1.0f, scale, true, true}};
+  launch_passes(dt, p, 3, ws, as_stream(stream));
   return check_launch(fn);
 }
 
