@@ -7,6 +7,8 @@
 // the gradients are dq_t = scale S_t do_t, dk_t = G_t v_t, dv_t = G_t^T k_t:
 // the same recurrence with (query, key, value) = (do, v, k) forward in time
 // on S^T, and (v, do, q) on G^T and (k, q, do) on G backward in time.
+#include <type_traits>
+
 #include "common.h"
 
 namespace o5 {
@@ -176,12 +178,13 @@ struct Stage {
   static_assert(N >= 1 && CL * U % BT == 0, "every thread takes whole units");
   u32x4 x[N];
   // `base`: row 0 of the chunk; `step`: elements between rows; rows before `pad` and columns from d on are zero
+  template <bool kFull>
   __device__ __forceinline__ void load(const E* base, ptrdiff_t step, int pad, int d) {
     int row = threadIdx.x / U;
     const int c = threadIdx.x % U * PER;
     asm volatile("" : "+v"(row));  // the address is worked out anew for each chunk: kept, it would cost two registers
     const E* at = base + row * step + c;
-    if (pad == 0 && d == D) {
+    if (kFull) {
 #pragma unroll
       for (int n = 0; n < N; ++n) x[n] = *reinterpret_cast<const u32x4*>(at + n * (BT / U) * step);
     } else {
@@ -315,32 +318,35 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
   StQ sq, sk;
   StV sv;
   bool cut_any = false;  // a reset in this split so far
-  f32x4 acc[kMany ? NI : 1][NC];
+  f32x4 o[NI][NC];  // the chunk's outputs, transposed
 
-  auto fetch = [&](int ch, int g) {
+  uint32_t flag = 0;  // of step `lane` of the chunk that is on its way: not 0 for a reset before it
+  const int r0 = p.rev ? 1 : 0;  // the first step that a reset can precede
+  auto fetch = [&](auto full, int ch, int g) {
+    constexpr bool kFull = decltype(full)::value;
     const int pad = ch == 0 ? pad0 : 0;
     const ptrdiff_t u = static_cast<ptrdiff_t>(ch - c0) * CL;
-    if (kOut && (!kMany || g == 0)) sq.load(qb + u * qstep, qstep, pad, p.da);
-    sk.load(kb + u * kstep + g * p.da, kstep, pad, p.da);
-    sv.load(vb + u * vstep + g * p.dc, vstep, pad, p.dc);
+    if (kOut && (!kMany || g == 0)) sq.template load<kFull>(qb + u * qstep, qstep, pad, p.da);
+    sk.template load<kFull>(kb + u * kstep + g * p.da, kstep, pad, p.da);
+    sv.template load<kFull>(vb + u * vstep + g * p.dc, vstep, pad, p.dc);
+    if (p.reset && (!kMany || g == 0)) {  // (looked at a chunk later: a branch on it here would wait for every load)
+      const int t = max(ch * CL - pad0 + min(lane, CL - 1), min(r0, p.T - 1));
+      flag = p.reset[static_cast<size_t>(p.rev && t > 0 ? p.T - t : t) * p.B + b];
+    }
   };
 
   int ch = c0, g = 0;
-  fetch(ch, g);
-  while (ch < c1) {
-    const int pad = ch == 0 ? pad0 : 0, u0 = ch * CL - pad0;
+  // kFull: no padded rows or columns, so that every access is unconditional and the waits for the next chunk's rows
+  // need not wait for this chunk's outputs too
+  auto chunk = [&](auto full) {
+    constexpr bool kFull = decltype(full)::value;
+    const int pad = !kFull && ch == 0 ? pad0 : 0;
     const bool first = !kMany || g == 0, last = !kMany || g == p.gk - 1;
     if (kOut && first) sq.template store<TL::QS, true>(lds.q);
     sk.template store<TL::QS, true>(lds.k);
     sv.template store<TL::VS, false>(lds.v);
-    // bit i: a reset before the chunk's step i
-    uint64_t resets = 0;
-    if (p.reset) {
-      bool flag = false;
-      const int u = u0 + lane;
-      if (lane < CL && u >= (p.rev ? 1 : 0)) flag = p.reset[static_cast<size_t>(p.rev ? p.T - u : u) * p.B + b] != 0;
-      resets = __ballot(flag);
-    }
+    uint64_t resets = 0;  // bit i: a reset before the chunk's step i
+    if (p.reset) resets = __ballot(flag != 0 && lane < CL && ch * CL - pad0 + lane >= r0);
     const int rl = resets ? 63 - __builtin_clzll(resets) : -1;  // the last reset
     int lr = -1;  // the last reset at or before step `lane`
     if (resets) {
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
     __syncthreads();
     int nch = ch, ng = g + 1;
     if (!kMany || ng == p.gk) ++nch, ng = 0;
-    if (nch < c1) fetch(nch, ng);
+    if (nch < c1) fetch(full, nch, ng);
 
     if (kOut) {  // p, 16 x 16 tiles at and below the diagonal, one after another to the waves
       constexpr int kTiles = NI * (NI + 1) / 2;
@@ -411,66 +417,75 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
             vf[c][u] = M::pack(x);
           }
       }
-      Frag sf[NC][NU];
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          const f32x4 x = S[2 * u][c], y = S[2 * u + 1][c];
-          const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-          sf[c][u] = M::pack(z);
-        }
-      int lrow = l16;
-      asm volatile("" : "+v"(lrow));
-      E* orow = ob + static_cast<ptrdiff_t>(ch - c0) * CL * ostep + lrow * ostep + col0 + g4 * 4;
       const char* qr = lds.q + l16 * TL::QS + ((g4 * 4 * ES) ^ M::swap(l16));
       const char* pr = lds.p + l16 * TL::PS + g4 * 4 * ES;
+      auto skip = [&](int ti) { return !kFull && ti * 16 + 16 <= pad; };
+      if (first) {
 #pragma unroll
-      for (int ti = 0; ti < NI; ++ti) {
-        if (ti * 16 + 16 <= pad) continue;
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 o[NC];
-        const int i = ti * 16 + l16;
+        for (int ti = 0; ti < NI; ++ti)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c] = f32x4{0, 0, 0, 0};
-        if (first) {
+          for (int c = 0; c < NC; ++c) o[ti][c] = f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int u = 0; u < NU; ++u) {
+        for (int u = 0; u < NU; ++u) {
+          __builtin_amdgcn_sched_barrier(0);
+          Frag sf[NC];
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const f32x4 x = S[2 * u][c], y = S[2 * u + 1][c];
+            const float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            sf[c] = M::pack(z);
+          }
+#pragma unroll
+          for (int ti = 0; ti < NI; ++ti) {
+            if (skip(ti)) continue;
             const Frag fq = M::rows(qr + ti * 16 * TL::QS + u * 32 * ES);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) o[c] = M::mma(sf[c][u], fq, o[c]);
+            for (int c = 0; c < NC; ++c) o[ti][c] = M::mma(sf[c], fq, o[ti][c]);
           }
-          const float f = p.oscale * power(l2, i - pad + e);
+        }
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] *= f;
+        for (int ti = 0; ti < NI; ++ti) {
+          const float f = p.oscale * power(l2, ti * 16 + l16 - pad + e);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[ti][c] *= f;
           if (resets) {
             const bool carried = last_reset(ti) < 0;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) o[c][r] = carried ? o[c][r] : 0.0f;
+              for (int r = 0; r < 4; ++r) o[ti][c][r] = carried ? o[ti][c][r] : 0.0f;
           }
-        } else {
-#pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] = acc[kMany ? ti : 0][c];
         }
+      }
 #pragma unroll
-        for (int u = 0; u < ti / 2 + 1; ++u) {
+      for (int u = 0; u < NB; ++u) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ti = 2 * u; ti < NI; ++ti) {
+          if (skip(ti)) continue;
           const Frag fp = M::rows(pr + ti * 16 * TL::PS + u * 32 * ES);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c] = M::mma(vf[c][u], fp, o[c]);
+          for (int c = 0; c < NC; ++c) o[ti][c] = M::mma(vf[c][u], fp, o[ti][c]);
         }
-        if (kMany) {
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (kMany && any_odd) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            if (any_odd) o[c] += odd_terms<E>(lds, i, last_reset(ti), col0 + c * 16 + g4 * 4);
-            acc[ti][c] = o[c];
-          }
-        }
-        if (last && i >= pad) {
+        for (int ti = 0; ti < NI; ++ti)
 #pragma unroll
           for (int c = 0; c < NC; ++c)
-            if (col0 + c * 16 + g4 * 4 < p.dc) M::store4(orow + ti * 16 * ostep + c * 16, o[c]);
+            o[ti][c] += odd_terms<E>(lds, ti * 16 + l16, last_reset(ti), col0 + c * 16 + g4 * 4);
+      }
+      int lrow = l16;
+      asm volatile("" : "+v"(lrow));
+      E* orow = ob + static_cast<ptrdiff_t>(ch - c0) * CL * ostep + lrow * ostep + col0 + g4 * 4;
+      if (last) {
+#pragma unroll
+        for (int ti = 0; ti < NI; ++ti) {
+          if (!kFull && ti * 16 + l16 < pad) continue;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (kFull || col0 + c * 16 + g4 * 4 < p.dc) M::store4(orow + ti * 16 * ostep + c * 16, o[ti][c]);
         }
       }
       if (any_odd) {
@@ -550,6 +565,20 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
     __syncthreads();
     ch = nch;
     g = ng;
+  };
+  const std::true_type full;
+  const std::false_type part;
+  if (p.da == DA && p.dc == DC) {
+    if (c0 == 0 && pad0 > 0) {
+      fetch(part, ch, g);
+      while (ch == 0 && ch < c1) chunk(part);
+    } else {
+      fetch(full, ch, g);
+    }
+    while (ch < c1) chunk(full);
+  } else {
+    fetch(part, ch, g);
+    while (ch < c1) chunk(part);
   }
 
   if (kOut && sp.states) return;  // the scan has written the last state
