@@ -152,10 +152,10 @@ template <> struct Mx<float> {
   static __device__ __forceinline__ void store4(void* p, f32x4 v) { *static_cast<f32x4*>(p) = v; }
 };
 
-// l^n for n > 0 (l2 = log2 l, -inf for l = 0) and n = 0; for other n any number.
-__device__ __forceinline__ float power(float l2, int n) {
-  return n == 0 ? 1.0f : __builtin_amdgcn_exp2f(l2 * static_cast<float>(n));
-}
+// log2 of a decay, finite for 0 too, so that l^0 is 1 and l^n 0 without a branch; and l^n for n >= 0 (for other n any
+// number).
+__device__ __forceinline__ float log2_decay(float l) { return fmaxf(log2f(l), -0x1p100f); }
+__device__ __forceinline__ float power(float l2, int n) { return __builtin_amdgcn_exp2f(l2 * static_cast<float>(n)); }
 __device__ __forceinline__ float uniform(float x) {
   return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
 }
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
   }
 
   // powers of the decay
-  const float l2 = uniform(log2f(p.decay[n]));
+  const float l2 = uniform(log2_decay(p.decay[n]));
   const float l16th = uniform(power(l2, 16)), l32 = uniform(power(l2, 32)), l48 = l16th * l32;
   float in[4];  // the factor on what enters the state from a chunk's last 16 steps
 #pragma unroll
@@ -379,11 +379,19 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
           const char* qr = lds.q + i * TL::QS + ((g4 * 4 * ES) ^ M::swap(l16));
 #pragma unroll
           for (int u = 0; u < NU; ++u) s = M::mma(M::rows(kr + u * 32 * ES), M::rows(qr + u * 32 * ES), s);
-          const int ri = last_reset(ti);
           const int d0 = i - tj * 16 - g4 * 4;
+          const float dl = l2 * static_cast<float>(d0);
 #pragma unroll
-          for (int r = 0; r < 4; ++r)  // (a select: outside the mask the product may be anything)
-            s[r] = static_cast<unsigned>(d0 - r) <= static_cast<unsigned>(ri < 0 ? i : i - ri) ? s[r] * (pscale * power(l2, d0 - r)) : 0.0f;
+          for (int r = 0; r < 4; ++r) s[r] *= pscale * __builtin_amdgcn_exp2f(fmaf(l2, static_cast<float>(-r), dl));
+          if (ti == tj) {  // (selects: outside the mask the product may be anything)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] = d0 >= r ? s[r] : 0.0f;
+          }
+          if (resets) {
+            const int ri = last_reset(ti) - tj * 16 - g4 * 4;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] = r >= ri ? s[r] : 0.0f;
+          }
         }
         M::store4(lds.p + i * TL::PS + (tj * 16 + g4 * 4) * ES, s);
       }
