@@ -7,8 +7,6 @@
 // the gradients are dq_t = scale S_t do_t, dk_t = G_t v_t, dv_t = G_t^T k_t:
 // the same recurrence with (query, key, value) = (do, v, k) forward in time
 // on S^T, and (v, do, q) on G^T and (k, q, do) on G backward in time.
-#include <type_traits>
-
 #include "common.h"
 
 namespace o5 {
@@ -239,7 +237,12 @@ struct Passes {
 // kMany: gk > 1, the outputs are sums over the group.
 // Where T is no multiple of CL the first chunk is short: it starts `pad` steps
 // before step 0, and those rows are zero and not written.
-template <typename E, int DA, int DC, bool kOut, bool kMany>
+// kFull: T is a multiple of CL and the state fills its tiles, so that every
+// access is unconditional and the waits for the next chunk's rows need not
+// wait for this chunk's outputs too (a kernel of its own: with both kinds of
+// chunk in one, registers spilled and T = 256, B = 128, 32 x 128 x 128 took 441
+// us instead of 423).
+template <typename E, int DA, int DC, bool kOut, bool kMany, bool kFull>
 __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Passes ps) {
   typedef Mx<E> M;
   typedef typename M::Frag Frag;
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
   for (int r = 0; r < 4; ++r) in[r] = p.kscale * power(l2, 16 - e - (g4 * 4 + r));
   const float pscale = p.oscale * p.kscale;
 
-  const int pad0 = chunks * CL - p.T;
+  const int pad0 = kFull ? 0 : chunks * CL - p.T;
   const ptrdiff_t dir = p.rev ? -p.B : p.B;
   const ptrdiff_t qstep = dir * static_cast<ptrdiff_t>(p.ldq), kstep = dir * static_cast<ptrdiff_t>(p.ldk);
   const ptrdiff_t vstep = dir * static_cast<ptrdiff_t>(p.ldv), ostep = dir * static_cast<ptrdiff_t>(p.ldo);
@@ -322,9 +325,8 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
 
   uint32_t flag = 0;  // of step `lane` of the chunk that is on its way: not 0 for a reset before it
   const int r0 = p.rev ? 1 : 0;  // the first step that a reset can precede
-  auto fetch = [&](auto full, int ch, int g) {
-    constexpr bool kFull = decltype(full)::value;
-    const int pad = ch == 0 ? pad0 : 0;
+  auto fetch = [&](int ch, int g) {
+    const int pad = !kFull && ch == 0 ? pad0 : 0;
     const ptrdiff_t u = static_cast<ptrdiff_t>(ch - c0) * CL;
     if (kOut && (!kMany || g == 0)) sq.template load<kFull>(qb + u * qstep, qstep, pad, p.da);
     sk.template load<kFull>(kb + u * kstep + g * p.da, kstep, pad, p.da);
@@ -336,10 +338,8 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
   };
 
   int ch = c0, g = 0;
-  // kFull: no padded rows or columns, so that every access is unconditional and the waits for the next chunk's rows
-  // need not wait for this chunk's outputs too
-  auto chunk = [&](auto full) {
-    constexpr bool kFull = decltype(full)::value;
+  fetch(ch, g);
+  while (ch < c1) {
     const int pad = !kFull && ch == 0 ? pad0 : 0;
     const bool first = !kMany || g == 0, last = !kMany || g == p.gk - 1;
     if (kOut && first) sq.template store<TL::QS, true>(lds.q);
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
     __syncthreads();
     int nch = ch, ng = g + 1;
     if (!kMany || ng == p.gk) ++nch, ng = 0;
-    if (nch < c1) fetch(full, nch, ng);
+    if (nch < c1) fetch(nch, ng);
 
     if (kOut) {  // p, 16 x 16 tiles at and below the diagonal, one after another to the waves
       constexpr int kTiles = NI * (NI + 1) / 2;
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
     }
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
-      if (u * 32 + 32 <= pad) continue;
+      if (!kFull && u * 32 + 32 <= pad) continue;
       __builtin_amdgcn_sched_barrier(0);
       // what enters, in bf16 as a sum of terms
       Frag term[NC][M::TERMS];
@@ -573,20 +573,6 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
     __syncthreads();
     ch = nch;
     g = ng;
-  };
-  const std::true_type full;
-  const std::false_type part;
-  if (p.da == DA && p.dc == DC) {
-    if (c0 == 0 && pad0 > 0) {
-      fetch(part, ch, g);
-      while (ch == 0 && ch < c1) chunk(part);
-    } else {
-      fetch(full, ch, g);
-    }
-    while (ch < c1) chunk(full);
-  } else {
-    fetch(part, ch, g);
-    while (ch < c1) chunk(part);
   }
 
   if (kOut && sp.states) return;  // the scan has written the last state
@@ -708,10 +694,13 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
     }
   }
   if (splits > 1) {
-    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany>), dim3(states * ps.count, used), dim3(256), 0, s, ps);
+    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany, false>), dim3(states * ps.count, used), dim3(256), 0, s, ps);
     hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
   }
-  hipLaunchKernelGGL((linattn_chunks<E, DA, DC, true, kMany>), dim3(states * p.gq * ps.count, used), dim3(256), 0, s, ps);
+  bool full = p.T % Mx<E>::CL == 0;
+  for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
+  auto kernel = full ? linattn_chunks<E, DA, DC, true, kMany, true> : linattn_chunks<E, DA, DC, true, kMany, false>;
+  hipLaunchKernelGGL(kernel, dim3(states * p.gq * ps.count, used), dim3(256), 0, s, ps);
 }
 
 template <typename E, int DA, int DC>
