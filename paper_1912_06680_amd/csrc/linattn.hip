@@ -70,7 +70,8 @@ template <> struct Mx<uint16_t> {
   static constexpr int PAD = 32;
   static __device__ __forceinline__ int swap(int row) { return (row & 8) * 2; }
   typedef u32x4 Frag;
-  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
+  // c + a b; where `upper`, the block's first 16 are zero and need not be multiplied
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, bool upper = false) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
   // 4 g + r and 16 + 4 g + r of a row, `at` pointing to its block's element 4 g
@@ -117,11 +118,13 @@ template <> struct Mx<float> {
   struct Frag {
     f32x4 h[2];
   };
-  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, bool upper = false) {
+    if (!upper) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.h[0][r], b.h[0][r], c, 0, 0, 0);
+    }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.h[h][r], b.h[h][r], c, 0, 0, 0);
+    for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.h[1][r], b.h[1][r], c, 0, 0, 0);
     return c;
   }
   static __device__ __forceinline__ Frag rows(const char* at) {
@@ -398,6 +401,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
       __syncthreads();
     }
 
+    auto upper = [&](int u) { return !kFull && u * 32 + 16 <= pad; };
     // the wave's columns of v
     Frag vf[NC][NB];
     typename M::Odd odd = {};
@@ -473,7 +477,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
           if (skip(ti)) continue;
           const Frag fp = M::rows(pr + ti * 16 * TL::PS + u * 32 * ES);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[ti][c] = M::mma(vf[c][u], fp, o[ti][c]);
+          for (int c = 0; c < NC; ++c) o[ti][c] = M::mma(vf[c][u], fp, o[ti][c], upper(u));
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(256, DA + DC == 128 ? 3 : 2) linattn_chunks(Pa
 #pragma unroll
         for (int t = M::TERMS - 1; t >= 0; --t)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) S[a][c] = M::mma(kf, term[c][t], S[a][c]);
+          for (int c = 0; c < NC; ++c) S[a][c] = M::mma(kf, term[c][t], S[a][c], upper(u));
       }
     }
     __syncthreads();
@@ -635,12 +639,23 @@ __global__ void __launch_bounds__(256) linattn_scan(Passes ps, int splits) {
   }
   f32x4* st = reinterpret_cast<f32x4*>(sp.states) + idx;
   const size_t stride = static_cast<size_t>(states) * Q;
-  for (int s = 0; s < splits; ++s) {
-    const f32x4 part = st[s * stride];
-    const float keep = sp.keep[static_cast<size_t>(s) * states + bn];
-    st[s * stride] = X;
+  // (8 splits' loads in flight together: 32 splits of 4 states took 11 us one after another)
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    f32x4 part[8];
+    float keep[8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) X[r] = keep < 0.0f ? part[r] : fmaf(keep, X[r], part[r]);
+    for (int i = 0; i < 8; ++i) {
+      const int s = min(s0 + i, splits - 1);
+      part[i] = st[s * stride];
+      keep[i] = sp.keep[static_cast<size_t>(s) * states + bn];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (s0 + i >= splits) break;
+      st[(s0 + i) * stride] = X;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) X[r] = keep[i] < 0.0f ? part[i][r] : fmaf(keep[i], X[r], part[i][r]);
+    }
   }
   if (in && p.sT) {
     if (p.rev && p.reset && p.reset[bn / p.nkv] != 0) X = f32x4{0, 0, 0, 0};
