@@ -678,14 +678,17 @@ int pad_head(int d) { return d <= 64 ? 64 : 128; }
 
 // Splits of the T steps: where the states and their query heads are too few
 // to fill the chip, so many that about 512 blocks (2 on each compute unit)
-// run, of 4 chunks at least.
+// run.  Split, a block goes through its chunks twice (the states, then the
+// outputs) and two more launches take about four chunks' time, so a sequence
+// of few chunks stays whole.
 int plan_splits(o5_dtype dt, int T, int B, int nkv, int gq) {
   const int cl = dt == O5_BF16 ? Mx<uint16_t>::CL : Mx<float>::CL;
   const int chunks = (T + cl - 1) / cl;
   const long long blocks = static_cast<long long>(B) * nkv * gq;
   if (blocks >= 256) return 1;
-  const int want = static_cast<int>((512 + blocks - 1) / blocks);
-  return std::max(1, std::min(want, chunks / 4));
+  const int want = std::min<int>(chunks, static_cast<int>((512 + blocks - 1) / blocks));
+  const int per = (chunks + want - 1) / want;
+  return chunks >= 2 * per + 4 ? (chunks + per - 1) / per : 1;
 }
 
 // Workspace of any of a call's launches: `count` passes at most, each with as many splits as if it ran alone.

@@ -179,8 +179,8 @@ def _p(t):
 
 
 def _stream(stream):
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # (the handle itself: 0.3 us a call, where building a torch.cuda.Stream for it takes 2.8)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
