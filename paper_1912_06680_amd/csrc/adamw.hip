@@ -15,13 +15,15 @@
 // below half a code (1/16), and nearest rounding would leave it where it is.
 // The chances come from a counter-based generator, so results repeat.
 #include "common.h"
+#include "reduce.h"
 
 namespace o5 {
 namespace {
 
 constexpr uint64_t kMagic = 0x316e616c7077616full;  // the plan's first word
 constexpr int kGroup = 256;                         // elements that share an exponent
-constexpr int kChunk = 2048;                        // elements of a block
+constexpr int kChunk = 1024;                        // elements of a block: 168M parameters with 8-bit moments and their
+                                                    // values took 847 us, with 2048 872 and with 4096 905
 constexpr int kLowM = 13, kLowV = 29;               // binades below the largest that keep 3 bits
 constexpr int kNanM = 0x7f, kNanV = 0xff;
 
@@ -83,7 +85,7 @@ __device__ __forceinline__ int exponent(float x) { return static_cast<int>(__flo
 // [-90, 126] every value of a code and every scale here is a normal number.
 __device__ __forceinline__ int group_exponent(float top) { return min(max(exponent(top), -90), 126); }
 
-__device__ __forceinline__ int shared_exponent(uint8_t e) { return max(static_cast<int>(e) - 127, -90); }
+__device__ __forceinline__ int shared_exponent(int e) { return max(e - 127, -90); }
 
 __device__ __forceinline__ float decode(uint32_t code, int a, int low) {
   const int field = code >> 3;
@@ -134,132 +136,233 @@ __device__ __forceinline__ void philox4x32_7(uint32_t (&c)[4], uint32_t k0, uint
   }
 }
 
-__device__ __forceinline__ float wave_top(float v) {
-#pragma unroll
-  for (int w = 32; w > 0; w >>= 1) v = fmaxf(v, __shfl_xor(v, w));
-  return v;
-}
-
 // ----------------------------------------------------------------- kernels
 
-__device__ __forceinline__ void load4(const float* p, size_t i, int n, float (&x)[4]) {
-  if (n == 4) {
-    const float4 v = *reinterpret_cast<const float4*>(p + i);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? p[i + j] : 0.0f;
-  }
+// Four elements from i on, as they are stored; the tensor's tail (n < 4 of
+// them) one by one.  The stream is touched once per step, hence the
+// non-temporal hints.
+template <typename V, typename T>
+__device__ __forceinline__ V load_run(const T* p, size_t i) {
+  return __builtin_nontemporal_load(reinterpret_cast<const V*>(p + i));
 }
-__device__ __forceinline__ void load4(const uint16_t* p, size_t i, int n, float (&x)[4]) {
-  if (n == 4) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p + i);
-    x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-    x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? bf16_bits_to_f32(p[i + j]) : 0.0f;
-  }
+template <typename V, typename T>
+__device__ __forceinline__ void store_run(T* p, size_t i, V v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<V*>(p + i));
 }
-__device__ __forceinline__ void store4(float* p, size_t i, int n, const float (&x)[4]) {
-  if (n == 4) {
-    *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <bool kFull>
+__device__ __forceinline__ f32x4 load4(const float* p, size_t i, int n) {
+  if (kFull || n == 4) return load_run<f32x4>(p, i);
+  f32x4 x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = j < n ? p[i + j] : 0.0f;
+  return x;
+}
+template <bool kFull>
+__device__ __forceinline__ u32x2 load4(const uint16_t* p, size_t i, int n) {
+  if (kFull || n == 4) return load_run<u32x2>(p, i);
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = j < n ? p[i + j] : 0;
+  return u32x2{w[0] | (w[1] << 16), w[2] | (w[3] << 16)};
+}
+template <bool kFull>
+__device__ __forceinline__ uint32_t load4(const uint8_t* p, size_t i, int n) {
+  if (kFull || n == 4) return load_run<uint32_t>(p, i);
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w |= (j < n ? static_cast<uint32_t>(p[i + j]) : 0) << (8 * j);
+  return w;
+}
+__device__ __forceinline__ float element(f32x4 x, int j) { return x[j]; }
+__device__ __forceinline__ float element(u32x2 x, int j) {
+  return __uint_as_float((j & 1) ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16);
+}
+
+template <bool kFull>
+__device__ __forceinline__ void store4(float* p, size_t i, int n, f32x4 x) {
+  if (kFull || n == 4) {
+    store_run(p, i, x);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (j < n) p[i + j] = x[j];
   }
 }
-__device__ __forceinline__ void store4(uint16_t* p, size_t i, int n, const float (&x)[4]) {
-  if (n == 4) {
-    *reinterpret_cast<uint2*>(p + i) = make_uint2(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]));
+template <bool kFull>
+__device__ __forceinline__ void store4(uint16_t* p, size_t i, int n, f32x4 x) {
+  if (kFull || n == 4) {
+    store_run(p, i, u32x2{f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3])});
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (j < n) p[i + j] = f32_to_bf16_bits(x[j]);
   }
 }
-__device__ __forceinline__ void load_codes(const uint8_t* p, size_t i, int n, uint32_t (&c)[4]) {
-  uint32_t w = 0;
-  if (n == 4) {
-    w = *reinterpret_cast<const uint32_t*>(p + i);
+template <bool kFull>
+__device__ __forceinline__ void store4(uint8_t* p, size_t i, int n, uint32_t w) {
+  if (kFull || n == 4) {
+    store_run(p, i, w);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (j < n) w |= static_cast<uint32_t>(p[i + j]) << (8 * j);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) c[j] = (w >> (8 * j)) & 0xff;
-}
-__device__ __forceinline__ void store_codes(uint8_t* p, size_t i, int n, const uint32_t (&c)[4]) {
-  if (n == 4) {
-    *reinterpret_cast<uint32_t*>(p + i) = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[i + j] = static_cast<uint8_t>(c[j]);
+      if (j < n) p[i + j] = static_cast<uint8_t>(w >> (8 * j));
   }
 }
 
 // How many of the four elements from i on the tensor has.
 __device__ __forceinline__ int count4(uint64_t n, size_t i) { return i >= n ? 0 : n - i < 4 ? static_cast<int>(n - i) : 4; }
 
+constexpr int kRuns = kChunk / 1024;  // of four elements, for a thread
+
+template <bool kFull, typename G>
+__device__ __forceinline__ void step32(const Tensor& t, const Consts& c, size_t i0, float lr, float keep) {
+  const G* gp = static_cast<const G*>(t.g);
+  float *mp = static_cast<float*>(t.m), *vp = static_cast<float*>(t.v);
+  f32x4 p[kRuns], m[kRuns], v[kRuns];
+  decltype(load4<true>(gp, 0, 4)) g[kRuns];
+  int n[kRuns];
+#pragma unroll
+  for (int k = 0; k < kRuns; ++k) {  // every load before the first use
+    const size_t i = i0 + k * 1024;
+    n[k] = kFull ? 4 : count4(t.n, i);
+    p[k] = load4<kFull>(t.p, i, n[k]);
+    g[k] = load4<kFull>(gp, i, n[k]);
+    m[k] = load4<kFull>(mp, i, n[k]);
+    v[k] = load4<kFull>(vp, i, n[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kRuns; ++k) {
+    const size_t i = i0 + k * 1024;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float pj = p[k][j], mj = m[k][j], vj = v[k][j];
+      update(c, lr, keep, element(g[k], j), pj, mj, vj);
+      p[k][j] = pj, m[k][j] = mj, v[k][j] = vj;
+    }
+    store4<kFull>(t.p, i, n[k], p[k]);
+    store4<kFull>(mp, i, n[k], m[k]);
+    store4<kFull>(vp, i, n[k], v[k]);
+    if (t.p16) store4<kFull>(t.p16, i, n[k], p[k]);
+  }
+}
+
+// A wave's run of 4 x 64 elements is one group.
+template <bool kFull, typename G>
+__device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Consts& c, size_t i0, float lr, float keep) {
+  const G* gp = static_cast<const G*>(t.g);
+  uint8_t *mp = static_cast<uint8_t*>(t.m), *vp = static_cast<uint8_t*>(t.v);
+  f32x4 p[kRuns];
+  decltype(load4<true>(gp, 0, 4)) g[kRuns];
+  uint32_t mc[kRuns], vc[kRuns];
+  int n[kRuns], am[kRuns], av[kRuns];
+#pragma unroll
+  for (int k = 0; k < kRuns; ++k) {
+    const size_t i = i0 + k * 1024, group = i / kGroup;
+    n[k] = kFull ? 4 : count4(t.n, i);
+    const bool any = kFull || group * kGroup < t.n;
+    p[k] = load4<kFull>(t.p, i, n[k]);
+    g[k] = load4<kFull>(gp, i, n[k]);
+    mc[k] = load4<kFull>(mp, i, n[k]);
+    vc[k] = load4<kFull>(vp, i, n[k]);
+    am[k] = any ? t.m_exp[group] : 127;
+    av[k] = any ? t.v_exp[group] : 127;
+  }
+#pragma unroll
+  for (int k = 0; k < kRuns; ++k) {
+    const size_t i = i0 + k * 1024, group = i / kGroup;
+    const int em = shared_exponent(am[k]), ev = shared_exponent(av[k]);
+    float m[4], v[4], tm = 0.0f, tv = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float pj = p[k][j];
+      m[j] = decode_m((mc[k] >> (8 * j)) & 0xff, em);
+      v[j] = decode_v((vc[k] >> (8 * j)) & 0xff, ev);
+      update(c, lr, keep, element(g[k], j), pj, m[j], v[j]);
+      p[k][j] = pj;
+      if (j >= n[k]) m[j] = v[j] = 0.0f;
+      tm = fmaxf(tm, finite(m[j]) ? fabsf(m[j]) : 0.0f);
+      tv = fmaxf(tv, finite(v[j]) ? v[j] : 0.0f);
+    }
+    const int nm = group_exponent(wave_max(tm)), nv = group_exponent(wave_max(tv));
+    uint32_t w[4] = {static_cast<uint32_t>(i / 4), static_cast<uint32_t>(i >> 34), c.step, index};
+    philox4x32_7(w, c.key0, c.key1);
+    uint32_t mo = 0, vo = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      mo |= encode_m(m[j], nm, static_cast<float>(w[j] & 0xffff) * 0x1p-16f) << (8 * j);
+      vo |= encode_v(v[j], nv, static_cast<float>(w[j] >> 16) * 0x1p-16f) << (8 * j);
+    }
+    store4<kFull>(t.p, i, n[k], p[k]);
+    store4<kFull>(mp, i, n[k], mo);
+    store4<kFull>(vp, i, n[k], vo);
+    if (t.p16) store4<kFull>(t.p16, i, n[k], p[k]);
+    if ((threadIdx.x & 63) == 0 && (kFull || group * kGroup < t.n)) {
+      t.m_exp[group] = static_cast<uint8_t>(nm + 127);
+      t.v_exp[group] = static_cast<uint8_t>(nv + 127);
+    }
+  }
+}
+
 __global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, Consts c) {
   const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
   const float lr = c.lr * t.lr_scale;
   const float keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(t.weight_decay));
-#pragma unroll
-  for (int k = 0; k < kChunk / 1024; ++k) {
-    const size_t i = static_cast<size_t>(ch.index) * kChunk + k * 1024 + threadIdx.x * 4;
-    const int n = count4(t.n, i);
-    float p[4], g[4], m[4], v[4];
-    load4(t.p, i, n, p);
+  const size_t i = static_cast<size_t>(ch.index) * kChunk + threadIdx.x * 4;
+  const bool full = (static_cast<size_t>(ch.index) + 1) * kChunk <= t.n;
+  if (t.bits == 32) {
     if (t.g_bf16)
-      load4(static_cast<const uint16_t*>(t.g), i, n, g);
+      full ? step32<true, uint16_t>(t, c, i, lr, keep) : step32<false, uint16_t>(t, c, i, lr, keep);
     else
-      load4(static_cast<const float*>(t.g), i, n, g);
-    if (t.bits == 32) {
-      load4(static_cast<const float*>(t.m), i, n, m);
-      load4(static_cast<const float*>(t.v), i, n, v);
+      full ? step32<true, float>(t, c, i, lr, keep) : step32<false, float>(t, c, i, lr, keep);
+  } else {
+    if (t.g_bf16)
+      full ? step8<true, uint16_t>(t, ch.tensor, c, i, lr, keep) : step8<false, uint16_t>(t, ch.tensor, c, i, lr, keep);
+    else
+      full ? step8<true, float>(t, ch.tensor, c, i, lr, keep) : step8<false, float>(t, ch.tensor, c, i, lr, keep);
+  }
+}
+
+template <bool kFull>
+__device__ __forceinline__ void moments(const Tensor& t, size_t i0, float* mo, float* vo) {
+  f32x4 m[kRuns], v[kRuns];
+  int n[kRuns];
+  if (t.bits == 32) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) update(c, lr, keep, g[j], p[j], m[j], v[j]);
-      store4(static_cast<float*>(t.m), i, n, m);
-      store4(static_cast<float*>(t.v), i, n, v);
-    } else {  // a wave holds one group
-      const size_t group = i / kGroup;
-      const bool any = group * kGroup < t.n;
-      uint32_t mc[4], vc[4];
-      load_codes(static_cast<const uint8_t*>(t.m), i, n, mc);
-      load_codes(static_cast<const uint8_t*>(t.v), i, n, vc);
-      const int am = any ? shared_exponent(t.m_exp[group]) : 0, av = any ? shared_exponent(t.v_exp[group]) : 0;
-      float tm = 0.0f, tv = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[j] = decode_m(mc[j], am);
-        v[j] = decode_v(vc[j], av);
-        update(c, lr, keep, g[j], p[j], m[j], v[j]);
-        if (j >= n) m[j] = v[j] = 0.0f;
-        tm = fmaxf(tm, finite(m[j]) ? fabsf(m[j]) : 0.0f);
-        tv = fmaxf(tv, finite(v[j]) ? v[j] : 0.0f);
-      }
-      const int em = group_exponent(wave_top(tm)), ev = group_exponent(wave_top(tv));
-      uint32_t w[4] = {static_cast<uint32_t>(i / 4), static_cast<uint32_t>(i >> 34), c.step, ch.tensor};
-      philox4x32_7(w, c.key0, c.key1);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        mc[j] = encode_m(m[j], em, static_cast<float>(w[j] & 0xffff) * 0x1p-16f);
-        vc[j] = encode_v(v[j], ev, static_cast<float>(w[j] >> 16) * 0x1p-16f);
-      }
-      store_codes(static_cast<uint8_t*>(t.m), i, n, mc);
-      store_codes(static_cast<uint8_t*>(t.v), i, n, vc);
-      if (any && (threadIdx.x & 63) == 0) {
-        t.m_exp[group] = static_cast<uint8_t>(em + 127);
-        t.v_exp[group] = static_cast<uint8_t>(ev + 127);
-      }
+    for (int k = 0; k < kRuns; ++k) {
+      const size_t i = i0 + k * 1024;
+      n[k] = kFull ? 4 : count4(t.n, i);
+      m[k] = load4<kFull>(static_cast<const float*>(t.m), i, n[k]);
+      v[k] = load4<kFull>(static_cast<const float*>(t.v), i, n[k]);
     }
-    store4(t.p, i, n, p);
-    if (t.p16) store4(t.p16, i, n, p);
+  } else {
+    uint32_t mc[kRuns], vc[kRuns];
+    int am[kRuns], av[kRuns];
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k) {
+      const size_t i = i0 + k * 1024, group = i / kGroup;
+      n[k] = kFull ? 4 : count4(t.n, i);
+      const bool any = kFull || group * kGroup < t.n;
+      mc[k] = load4<kFull>(static_cast<const uint8_t*>(t.m), i, n[k]);
+      vc[k] = load4<kFull>(static_cast<const uint8_t*>(t.v), i, n[k]);
+      am[k] = any ? t.m_exp[group] : 127;
+      av[k] = any ? t.v_exp[group] : 127;
+    }
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[k][j] = decode_m((mc[k] >> (8 * j)) & 0xff, shared_exponent(am[k]));
+        v[k][j] = decode_v((vc[k] >> (8 * j)) & 0xff, shared_exponent(av[k]));
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < kRuns; ++k) {
+    store4<kFull>(mo, i0 + k * 1024, n[k], m[k]);
+    store4<kFull>(vo, i0 + k * 1024, n[k], v[k]);
   }
 }
 
@@ -267,30 +370,11 @@ __global__ void __launch_bounds__(256) adamw_moments(const void* __restrict__ pl
                                                      float* __restrict__ mo, float* __restrict__ vo) {
   const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
-#pragma unroll
-  for (int k = 0; k < kChunk / 1024; ++k) {
-    const size_t i = static_cast<size_t>(ch.index) * kChunk + k * 1024 + threadIdx.x * 4;
-    const int n = count4(t.n, i);
-    float m[4], v[4];
-    if (t.bits == 32) {
-      load4(static_cast<const float*>(t.m), i, n, m);
-      load4(static_cast<const float*>(t.v), i, n, v);
-    } else {
-      const size_t group = i / kGroup;
-      const bool any = group * kGroup < t.n;
-      uint32_t mc[4], vc[4];
-      load_codes(static_cast<const uint8_t*>(t.m), i, n, mc);
-      load_codes(static_cast<const uint8_t*>(t.v), i, n, vc);
-      const int am = any ? shared_exponent(t.m_exp[group]) : 0, av = any ? shared_exponent(t.v_exp[group]) : 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[j] = decode_m(mc[j], am);
-        v[j] = decode_v(vc[j], av);
-      }
-    }
-    store4(mo, t.at + i, n, m);
-    store4(vo, t.at + i, n, v);
-  }
+  const size_t i = static_cast<size_t>(ch.index) * kChunk + threadIdx.x * 4;
+  if ((static_cast<size_t>(ch.index) + 1) * kChunk <= t.n)
+    moments<true>(t, i, mo + t.at, vo + t.at);
+  else
+    moments<false>(t, i, mo + t.at, vo + t.at);
 }
 
 #define O5_TRY(expr)              \

@@ -14,6 +14,12 @@ namespace o5 {
 namespace {
 
 constexpr int kMaxWidth = 8192;
+// Blocks that walk the rows.  Two on each compute unit read fastest in the
+// forward pass (32768 x 4096 in bf16: 257 us, 276 with one, 262 with three and
+// four; 40000 x 512: 33, 43, 33); the backward pass has more of a row in flight
+// and sums to write for each block: one (391 us, 423 with two; 40000 x 512:
+// 62 and 59).
+constexpr int kFwdBlocks = 512, kBwdBlocks = 256;
 
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
@@ -74,76 +80,101 @@ struct NormFwd {
   float eps;
 };
 
-// TR threads of a block of max(256, TR) take a row, 8 elements each in NJ runs.
+// A row's operands on their way from memory: the next row's are in flight
+// while one is worked on.
+template <typename X, typename E, int NJ>
+struct FwdRow {
+  Run8<X> x[NJ];
+  Run8<E> u[NJ], gate[NJ];
+};
+
+// TR threads of a block of max(256, TR) take a row, 8 elements each in NJ
+// runs, and walk the rows with the gains in registers.
 template <typename X, typename E, int TR, int NJ>
 __global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_fwd(NormFwd p) {
   constexpr int BT = TR < 256 ? 256 : TR;
   __shared__ float red[BT / 64];
-  const int row = blockIdx.x * (BT / TR) + threadIdx.x / TR, t = threadIdx.x % TR;
-  const bool in = row < p.N;
-  const size_t base = static_cast<size_t>(in ? row : 0) * p.D, gbase = static_cast<size_t>(in ? row : 0) * p.ldg;
+  const int group = blockIdx.x * (BT / TR) + threadIdx.x / TR, groups = gridDim.x * (BT / TR), t = threadIdx.x % TR;
   const float inv = 1.0f / static_cast<float>(p.D);
-  float x[NJ][8];
   bool on[NJ];
+  float wr[NJ][8], wp[NJ][8];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int c = (t + j * TR) * 8;
-    on[j] = in && c < p.D;
-    Run8<X> r;
-    if (on[j]) r.load(p.x, base + c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[j][i] = on[j] ? r[i] : 0.0f;
-  }
-  if (p.u) {
-    float u[NJ][8], ss = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      Run8<E> r;
-      if (on[j]) r.load(p.u, base + (t + j * TR) * 8);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        u[j][i] = on[j] ? r[i] : 0.0f;
-        ss = fmaf(u[j][i], u[j][i], ss);
-      }
+    on[j] = c < p.D;
+    Run8<float> a = {}, b = {}, w = {};
+    if (on[j] && p.u) {
+      a.load(p.w_post, c);
+      b.load(p.rho, c);
     }
-    const float r = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
-    if (p.r_post && t == 0 && in) p.r_post[row] = r;
+    if (on[j] && p.w_pre) w.load(p.w_pre, c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      wr[j][i] = a[i] * b[i];
+      wp[j][i] = w[i];
+    }
+  }
+  auto fetch = [&](int row, FwdRow<X, E, NJ>& r) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      if (!on[j]) continue;
       const int c = (t + j * TR) * 8;
-      Run8<float> w, rho;
-      Run8<E> g;
-      w.load(p.w_post, c);
-      rho.load(p.rho, c);
-      if (p.gate) g.load(p.gate, gbase + c);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float y = u[j][i] * r * (w[i] * rho[i]);
-        if (p.gate) y *= sigmoid_f(g[i]);
-        x[j][i] += y;
-      }
-      store8<X>(p.xo, base + c, x[j]);
+      r.x[j] = {};
+      r.u[j] = {};
+      r.gate[j] = {};
+      if (row >= p.N || !on[j]) continue;
+      r.x[j].load(p.x, static_cast<size_t>(row) * p.D + c);
+      if (p.u) r.u[j].load(p.u, static_cast<size_t>(row) * p.D + c);
+      if (p.gate) r.gate[j].load(p.gate, static_cast<size_t>(row) * p.ldg + c);
     }
-  }
-  if (p.w_pre) {
-    float ss = 0.0f;
+  };
+  const int rounds = (p.N + groups - 1) / groups;
+  FwdRow<X, E, NJ> next;
+  fetch(group, next);
+  for (int k = 0; k < rounds; ++k) {
+    const int row = group + k * groups;
+    const bool in = row < p.N;
+    const size_t base = static_cast<size_t>(row) * p.D;
+    const FwdRow<X, E, NJ> r = next;
+    if (k + 1 < rounds) fetch(row + groups, next);
+    float x[NJ][8];
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[j][i], x[j][i], ss);
-    const float r = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
-    if (p.r_pre && t == 0 && in) p.r_pre[row] = r;
+      for (int i = 0; i < 8; ++i) x[j][i] = r.x[j][i];
+    if (p.u) {
+      float ss = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      if (!on[j]) continue;
-      const int c = (t + j * TR) * 8;
-      Run8<float> w;
-      w.load(p.w_pre, c);
-      float y[8];
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = x[j][i] * r * w[i];
-      store8<E>(p.n, base + c, y);
+        for (int i = 0; i < 8; ++i) ss = fmaf(r.u[j][i], r.u[j][i], ss);
+      const float ru = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
+      if (p.r_post && t == 0 && in) p.r_post[row] = ru;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float y = r.u[j][i] * ru * wr[j][i];
+          if (p.gate) y *= sigmoid_f(r.gate[j][i]);
+          x[j][i] += y;
+        }
+        if (in && on[j]) store8<X>(p.xo, base + (t + j * TR) * 8, x[j]);
+      }
+    }
+    if (p.w_pre) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[j][i], x[j][i], ss);
+      const float rx = 1.0f / sqrtf(row_sum<TR>(ss, red) * inv + p.eps);
+      if (p.r_pre && t == 0 && in) p.r_pre[row] = rx;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[j][i] * rx * wp[j][i];
+        if (in && on[j]) store8<E>(p.n, base + (t + j * TR) * 8, y);
+      }
     }
   }
 }
@@ -153,125 +184,167 @@ struct NormBwd {
   const float *w_post, *rho, *w_pre, *r_post, *r_pre;
   const void *dxo, *dn;
   void *dx, *du, *dgate;
-  float *part;  // [blocks * rows per block][2][D]: the row groups' column sums for dw_pre, and for drho and dw_post
+  float *part;  // [blocks][2][D]: the blocks' column sums for dw_pre, and for drho and dw_post
   int N, D;
   size_t ldg, lddg;
 };
 
-// The rows' gradients, and each row group's sums over its rows:
+template <typename X, typename E, int NJ>
+struct BwdRow {
+  Run8<X> dxo[NJ], x[NJ];
+  Run8<E> dn[NJ], u[NJ], gate[NJ];
+  float r_pre, r_post;
+};
+
+// The rows' gradients, and each block's sums over its rows:
 //   a = dn w_pre,  d = dx' + r_x' (a - x' r_x'^2 mean(a x')),  dx = d
 //   s = sigmoid(gate), y = u r_u:  dgate = d y w_post rho s (1 - s),
 //   a = d s w_post rho,  du = r_u (a - y mean(a y))
 //   dw_pre = sum dn x' r_x',  drho = w_post sum d s y,  dw_post = rho sum d s y
+// Every operand of the next row is in flight while a row is worked on, and
+// the gains stay in registers (read again for each row they were half as many
+// bytes as the row itself).
 template <typename X, typename E, int TR, int NJ>
 __global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_bwd(NormBwd p) {
-  constexpr int BT = TR < 256 ? 256 : TR;
+  constexpr int BT = TR < 256 ? 256 : TR, ROWS = BT / TR;
   __shared__ float red[BT / 64];
-  const int group = blockIdx.x * (BT / TR) + threadIdx.x / TR, groups = gridDim.x * (BT / TR), t = threadIdx.x % TR;
+  const int group = blockIdx.x * ROWS + threadIdx.x / TR, groups = gridDim.x * ROWS, t = threadIdx.x % TR;
   const float inv = 1.0f / static_cast<float>(p.D);
-  float spre[NJ][8] = {}, spost[NJ][8] = {};
-  const int rounds = (p.N + groups - 1) / groups;
-  for (int k = 0; k < rounds; ++k) {
-    const int row = group + k * groups;
+  float spre[NJ][8] = {}, spost[NJ][8] = {}, wr[NJ][8], wp[NJ][8];
+  bool on[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int c = (t + j * TR) * 8;
+    on[j] = c < p.D;
+    Run8<float> a = {}, b = {}, w = {};
+    if (on[j] && p.u) {
+      a.load(p.w_post, c);
+      b.load(p.rho, c);
+    }
+    if (on[j] && p.w_pre) w.load(p.w_pre, c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      wr[j][i] = a[i] * b[i];
+      wp[j][i] = w[i];
+    }
+  }
+  auto fetch = [&](int row, BwdRow<X, E, NJ>& r) {  // (zeros beyond the rows and columns)
     const bool in = row < p.N;
-    const size_t base = static_cast<size_t>(in ? row : 0) * p.D;
-    float d[NJ][8];
-    bool on[NJ];
+    const size_t base = static_cast<size_t>(row) * p.D;
+    r.r_pre = in && p.w_pre ? p.r_pre[row] : 0.0f;
+    r.r_post = in && p.u ? p.r_post[row] : 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int c = (t + j * TR) * 8;
-      on[j] = in && c < p.D;
-      Run8<X> r;
-      if (on[j]) r.load(p.dxo, base + c);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) d[j][i] = on[j] ? r[i] : 0.0f;
+      r.dxo[j] = {};
+      r.x[j] = {};
+      r.dn[j] = {};
+      r.u[j] = {};
+      r.gate[j] = {};
+      if (!in || !on[j]) continue;
+      r.dxo[j].load(p.dxo, base + c);
+      if (p.w_pre) {
+        r.x[j].load(p.x, base + c);
+        r.dn[j].load(p.dn, base + c);
+      }
+      if (p.u) r.u[j].load(p.u, base + c);
+      if (p.gate) r.gate[j].load(p.gate, static_cast<size_t>(row) * p.ldg + c);
     }
-    if (p.w_pre) {
-      float a[NJ][8], x[NJ][8], dot = 0.0f;
-      const float r = in ? p.r_pre[row] : 0.0f;
+  };
+  const int rounds = (p.N + groups - 1) / groups;
+  BwdRow<X, E, NJ> next;
+  fetch(group, next);
+  for (int k = 0; k < rounds; ++k) {
+    const int row = group + k * groups;
+    const bool in = row < p.N;
+    const size_t base = static_cast<size_t>(row) * p.D;
+    const BwdRow<X, E, NJ> q = next;
+    if (k + 1 < rounds) fetch(row + groups, next);
+    float d[NJ][8];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int c = (t + j * TR) * 8;
-        Run8<X> xr;
-        Run8<E> nr;
-        Run8<float> w;
-        if (on[j]) {
-          xr.load(p.x, base + c);
-          nr.load(p.dn, base + c);
-          w.load(p.w_pre, c);
-        }
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[j][i] = q.dxo[j][i];
+    if (p.w_pre) {
+      const float r = q.r_pre;
+      float dot = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          x[j][i] = on[j] ? xr[i] : 0.0f;
-          const float dn = on[j] ? nr[i] : 0.0f;
-          a[j][i] = on[j] ? dn * w[i] : 0.0f;
-          dot = fmaf(a[j][i], x[j][i], dot);
-          spre[j][i] = fmaf(dn, x[j][i] * r, spre[j][i]);
+          dot = fmaf(q.dn[j][i] * wp[j][i], q.x[j][i], dot);
+          spre[j][i] = fmaf(q.dn[j][i], q.x[j][i] * r, spre[j][i]);
         }
-      }
       const float m = row_sum<TR>(dot, red) * inv * (r * r);
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[j][i] += r * (a[j][i] - x[j][i] * m);
+        for (int i = 0; i < 8; ++i) d[j][i] += r * (q.dn[j][i] * wp[j][i] - q.x[j][i] * m);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
-      if (on[j]) store8<X>(p.dx, base + (t + j * TR) * 8, d[j]);
+      if (in && on[j]) store8<X>(p.dx, base + (t + j * TR) * 8, d[j]);
     if (p.u) {
-      float a[NJ][8], y[NJ][8], dot = 0.0f;
-      const float r = in ? p.r_post[row] : 0.0f;
+      const float r = q.r_post;
+      float dot = 0.0f;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int c = (t + j * TR) * 8;
-        Run8<E> ur, gr;
-        Run8<float> w, rho;
-        if (on[j]) {
-          ur.load(p.u, base + c);
-          w.load(p.w_post, c);
-          rho.load(p.rho, c);
-          if (p.gate) gr.load(p.gate, static_cast<size_t>(row) * p.ldg + c);
-        }
         float dg[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          y[j][i] = on[j] ? ur[i] * r : 0.0f;
-          const float wr = on[j] ? w[i] * rho[i] : 0.0f;
-          float ds = d[j][i];
+          const float y = q.u[j][i] * r;
           if (p.gate) {
-            const float s = on[j] ? sigmoid_f(gr[i]) : 0.0f;
-            dg[i] = ds * y[j][i] * wr * s * (1.0f - s);
-            ds *= s;
+            const float s = sigmoid_f(q.gate[j][i]);
+            dg[i] = d[j][i] * y * wr[j][i] * s * (1.0f - s);
+            d[j][i] *= s;
           }
-          spost[j][i] = fmaf(ds, y[j][i], spost[j][i]);
-          a[j][i] = ds * wr;
-          dot = fmaf(a[j][i], y[j][i], dot);
+          spost[j][i] = fmaf(d[j][i], y, spost[j][i]);
+          d[j][i] *= wr[j][i];
+          dot = fmaf(d[j][i], y, dot);
         }
-        if (p.gate && on[j]) store8<E>(p.dgate, static_cast<size_t>(row) * p.lddg + c, dg);
+        if (p.gate && in && on[j]) store8<E>(p.dgate, static_cast<size_t>(row) * p.lddg + (t + j * TR) * 8, dg);
       }
       const float m = row_sum<TR>(dot, red) * inv;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        if (!on[j]) continue;
         float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = r * (a[j][i] - y[j][i] * m);
-        store8<E>(p.du, base + (t + j * TR) * 8, o);
+        for (int i = 0; i < 8; ++i) o[i] = r * (d[j][i] - q.u[j][i] * r * m);
+        if (in && on[j]) store8<E>(p.du, base + (t + j * TR) * 8, o);
       }
     }
   }
-  float* part = p.part + static_cast<size_t>(group) * 2 * p.D;
+  float* part = p.part + static_cast<size_t>(blockIdx.x) * 2 * p.D;
+  if (ROWS == 1) {
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int c = (t + j * TR) * 8;
-    if (c >= p.D) continue;
-    if (p.w_pre) store8<float>(part, c, spre[j]);
-    if (p.u) store8<float>(part + p.D, c, spost[j]);
+    for (int j = 0; j < NJ; ++j) {
+      const int c = (t + j * TR) * 8;
+      if (!on[j]) continue;
+      if (p.w_pre) store8<float>(part, c, spre[j]);
+      if (p.u) store8<float>(part + p.D, c, spost[j]);
+    }
+  } else {  // the block's row groups first, in order
+    constexpr int WIDTH = TR * NJ * 8;
+    __shared__ alignas(16) float sums[ROWS == 1 ? 1 : ROWS][ROWS == 1 ? 8 : WIDTH];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) store8<float>(sums[threadIdx.x / TR], (t + j * TR) * 8, a == 0 ? spre[j] : spost[j]);
+      __syncthreads();
+      if (a == 0 ? p.w_pre == nullptr : p.u == nullptr) continue;
+      for (int c = threadIdx.x; c < p.D; c += BT) {
+        float s = 0.0f;
+#pragma unroll
+        for (int g = 0; g < ROWS; ++g) s += sums[g][c];
+        part[a * p.D + c] = s;
+      }
+    }
   }
 }
 
-// dw_pre, drho and dw_post from the row groups' sums: a block takes 64 columns
-// of one of the two sums, wave w adds the groups w, w + 16, ... in order, and
+// dw_pre, drho and dw_post from the blocks' sums: a block takes 64 columns of
+// one of the two sums, wave w adds the blocks w, w + 16, ... in order, and
 // the 16 waves' sums are added in order.
 __global__ void __launch_bounds__(1024) resnorm_columns(int groups, int D, const float* __restrict__ part,
                                                         const float* __restrict__ w_post,
@@ -301,25 +374,19 @@ __global__ void __launch_bounds__(1024) resnorm_columns(int groups, int D, const
 // Threads of a row: 8 or 16 elements each.
 int row_threads(int D) { return D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
 
-// Row groups that walk the N rows in the backward pass.
-int bwd_blocks(int N, int D) {
+int row_blocks(int N, int D, int most) {
   const int tr = row_threads(D), per = tr < 256 ? 256 / tr : 1;
-  return std::min((N + per - 1) / per, 512);
-}
-int bwd_groups(int N, int D) {
-  const int tr = row_threads(D);
-  return bwd_blocks(N, D) * (tr < 256 ? 256 / tr : 1);
+  return std::min((N + per - 1) / per, most);
 }
 
 template <typename X, typename E>
 void launch_fwd(const NormFwd& p, hipStream_t s) {
-  const int tr = row_threads(p.D), bt = tr < 256 ? 256 : tr, per = bt / tr;
-  const dim3 grid(static_cast<unsigned>((p.N + per - 1) / per));
+  const int tr = row_threads(p.D), bt = tr < 256 ? 256 : tr;
   auto k = tr == 64    ? (p.D <= 512 ? resnorm_fwd<X, E, 64, 1> : resnorm_fwd<X, E, 64, 2>)
            : tr == 128 ? resnorm_fwd<X, E, 128, 2>
            : tr == 256 ? resnorm_fwd<X, E, 256, 2>
                        : resnorm_fwd<X, E, 512, 2>;
-  hipLaunchKernelGGL(k, grid, dim3(bt), 0, s, p);
+  hipLaunchKernelGGL(k, dim3(row_blocks(p.N, p.D, kFwdBlocks)), dim3(bt), 0, s, p);
 }
 
 template <typename X, typename E>
@@ -329,7 +396,7 @@ void launch_bwd(const NormBwd& p, hipStream_t s) {
            : tr == 128 ? resnorm_bwd<X, E, 128, 2>
            : tr == 256 ? resnorm_bwd<X, E, 256, 2>
                        : resnorm_bwd<X, E, 512, 2>;
-  hipLaunchKernelGGL(k, dim3(bwd_blocks(p.N, p.D)), dim3(bt), 0, s, p);
+  hipLaunchKernelGGL(k, dim3(row_blocks(p.N, p.D, kBwdBlocks)), dim3(bt), 0, s, p);
 }
 
 int check_common(const char* fn, o5_dtype xt, o5_dtype dt, int N, int D) {
@@ -393,7 +460,7 @@ extern "C" int o5_resnorm_fwd(o5_dtype xt, o5_dtype dt, int N, int D, const void
 
 extern "C" size_t o5_resnorm_bwd_workspace_bytes(o5_dtype xt, o5_dtype dt, int N, int D) {
   if (check_common("o5_resnorm_bwd_workspace_bytes", xt, dt, N, D) != O5_OK) return 0;
-  return static_cast<size_t>(bwd_groups(N, D)) * 2 * D * sizeof(float);
+  return static_cast<size_t>(row_blocks(N, D, kBwdBlocks)) * 2 * D * sizeof(float);
 }
 
 extern "C" int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo, const void* u, const void* gate,
@@ -441,7 +508,7 @@ extern "C" int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void
   else
     launch_bwd<float, float>(p, as_stream(stream));
   const dim3 grid((D + 63) / 64, (u ? 1 : 0) + (w_pre ? 1 : 0));
-  hipLaunchKernelGGL(resnorm_columns, grid, dim3(1024), 0, as_stream(stream), bwd_groups(N, D), D,
+  hipLaunchKernelGGL(resnorm_columns, grid, dim3(1024), 0, as_stream(stream), row_blocks(N, D, kBwdBlocks), D,
                      static_cast<const float*>(ws), w_post, rho, w_pre ? dw_pre : nullptr, drho, dw_post);
   return check_launch(fn);
 }
