@@ -238,9 +238,11 @@ struct Passes {
 
 // Column tiles of a wave: two where the state's accumulators would else need 8 waves of more registers than they can
 // have (128 x 128 with one tile spills: 543 us against 423 at T = 256, B = 128, 32 heads).
-constexpr int tile_columns(int da, int dc) { return da == 128 && dc == 128 ? 2 : 1; }
-constexpr int block_threads(int da, int dc) { return dc / 16 / tile_columns(da, dc) * 64; }
-constexpr int waves_per_simd(int da, int dc) { return block_threads(da, dc) == 512 ? 4 : da + dc == 128 ? 3 : 2; }
+constexpr int tile_columns(int da, int dc, bool many) { return (da == 128 || many) && dc == 128 ? 2 : 1; }
+constexpr int block_threads(int da, int dc, bool many) { return dc / 16 / tile_columns(da, dc, many) * 64; }
+constexpr int waves_per_simd(int da, int dc, bool many) {
+  return block_threads(da, dc, many) == 512 ? 4 : da + dc == 128 ? 3 : 2;
+}
 
 // kOut: write the outputs; else only add up each split's own part of the state.
 // kMany: gk > 1, the outputs are sums over the group.
@@ -252,11 +254,11 @@ constexpr int waves_per_simd(int da, int dc) { return block_threads(da, dc) == 5
 // chunk in one, registers spilled and T = 256, B = 128, 32 x 128 x 128 took 441
 // us instead of 423).
 template <typename E, int DA, int DC, bool kOut, bool kMany, bool kFull>
-__global__ void __launch_bounds__(block_threads(DA, DC), waves_per_simd(DA, DC)) linattn_chunks(Passes ps) {
+__global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(DA, DC, kMany)) linattn_chunks(Passes ps) {
   typedef Mx<E> M;
   typedef typename M::Frag Frag;
   typedef Tiles<E, DA, DC> TL;
-  constexpr int NC = tile_columns(DA, DC), WAVES = DC / 16 / NC, BT = WAVES * 64;
+  constexpr int NC = tile_columns(DA, DC, kMany), WAVES = DC / 16 / NC, BT = WAVES * 64;
   constexpr int CL = M::CL, ES = sizeof(E), NI = CL / 16, NB = CL / 32, NA = DA / 16, NU = DA / 32;
   __shared__ TL lds;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
@@ -718,13 +720,13 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
     }
   }
   if (splits > 1) {
-    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany, false>), dim3(states * ps.count, used), dim3(block_threads(DA, DC)), 0, s, ps);
+    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany, false>), dim3(states * ps.count, used), dim3(block_threads(DA, DC, kMany)), 0, s, ps);
     hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
   }
   bool full = p.T % Mx<E>::CL == 0;
   for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
   auto kernel = full ? linattn_chunks<E, DA, DC, true, kMany, true> : linattn_chunks<E, DA, DC, true, kMany, false>;
-  hipLaunchKernelGGL(kernel, dim3(states * p.gq * ps.count, used), dim3(block_threads(DA, DC)), 0, s, ps);
+  hipLaunchKernelGGL(kernel, dim3(states * p.gq * ps.count, used), dim3(block_threads(DA, DC, kMany)), 0, s, ps);
 }
 
 template <typename E, int DA, int DC>
