@@ -521,7 +521,7 @@ int o5_surgery_fold_input(int D, int H, int A1, int Dk, const float* E,
  *   o_{t,h} = scale S_t^T q_{t,h}
  *
  * dt       type of q, k, v, o and of dout, dq, dk, dv.
- * T, B     steps and samples, >= 1, T*B below 2^31.   nh: query heads, a
+ * T, B     steps and samples, >= 1, T*B below 2^30.   nh: query heads, a
  *          multiple of nkv, the key/value and state heads; B*nh below 2^24.
  * dk, dv   widths of a key (and query) and of a value, multiples of 8 in
  *          8..128.
@@ -534,7 +534,10 @@ int o5_surgery_fold_input(int D, int H, int A1, int Dk, const float* E,
  * S0       [B, nkv, dk, dv] fp32, the states before the first step, or NULL
  *          (= 0).   ST: out, the states after the last step, or NULL.
  * reset    [T, B] uint8 or NULL (no resets): nonzero cuts the carried state
- *          off before step t, whatever it held, infinities and NaN too.
+ *          off before step t, whatever it held, infinities and NaN too.  A
+ *          value that is not finite reaches the steps that the recurrence
+ *          carries it to and no other (there, and in the states, an infinity
+ *          may show as NaN).
  * ws       scratch of o5_linattn_*_workspace_bytes(...) bytes.
  *
  * o5_linattn_bwd differentiates J = sum_t <dout_t, o_t> + <dST, S_{T-1}>:
