@@ -262,7 +262,11 @@ constexpr int waves_per_simd(int da, int dc, bool many) {
 }
 
 // kOut: write the outputs; else only add up each split's own part of the state.
-// kMany: gk > 1, the outputs are sums over the group.
+// kLoop: what a block takes in turn within a chunk: kAlone, one query head and
+// one key/value head; kManyKeys, the gk key/value heads of a state, whose outputs
+// are summed; kGroupQueries, the gq query heads of a state, which then stages the keys
+// and values and updates the state once for all of them.
+enum Loop { kAlone, kManyKeys, kGroupQueries };
 // Where T is no multiple of CL the first chunk is short: it starts `pad` steps
 // before step 0, and those rows are zero and not written.
 // kFull: T is a multiple of CL and the state fills its tiles, so that every
@@ -270,8 +274,10 @@ constexpr int waves_per_simd(int da, int dc, bool many) {
 // wait for this chunk's outputs too (a kernel of its own: with both kinds of
 // chunk in one, registers spilled and T = 256, B = 128, 32 x 128 x 128 took 441
 // us instead of 423).
-template <typename E, int DA, int DC, bool kOut, bool kMany, bool kFull>
-__global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(DA, DC, kMany)) linattn_chunks(Passes ps) {
+template <typename E, int DA, int DC, bool kOut, Loop kLoop, bool kFull>
+__global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), waves_per_simd(DA, DC, kLoop == kManyKeys))
+    linattn_chunks(Passes ps) {
+  constexpr bool kMany = kLoop == kManyKeys, kGroup = kLoop == kGroupQueries;
   typedef Mx<E> M;
   typedef typename M::Frag Frag;
   typedef Tiles<E, DA, DC> TL;
@@ -284,8 +290,9 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
   const LinPass& p = ps.pass[blockIdx.x % ps.count];
   const Split& sp = ps.split[blockIdx.x % ps.count];
   const int block = blockIdx.x / ps.count;
-  const int heads = kOut ? p.nkv * p.gq : p.nkv;
-  const int b = block / heads, hq = block % heads, n = kOut ? hq / p.gq : hq;
+  const int heads = kOut && !kGroup ? p.nkv * p.gq : p.nkv;
+  const int b = block / heads, n = kOut && !kGroup ? block % heads / p.gq : block % heads;
+  const int hq = kGroup ? n * p.gq : block % heads;  // the block's (first) query head
   const int chunks = (p.T + CL - 1) / CL;
   const int c0 = blockIdx.y * sp.chunks, c1 = min(chunks, c0 + sp.chunks);
   const int e = p.rev ? 0 : 1;
@@ -356,10 +363,12 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
   auto fetch = [&](int ch, int g) {
     const int pad = !kFull && ch == 0 ? pad0 : 0;
     const ptrdiff_t u = static_cast<ptrdiff_t>(ch - c0) * CL;
-    if (kOut && (!kMany || g == 0)) sq.template load<kFull>(qb + u * qstep, qstep, pad, p.da);
-    sk.template load<kFull>(kb + u * kstep + g * p.da, kstep, pad, p.da);
-    sv.template load<kFull>(vb + u * vstep + g * p.dc, vstep, pad, p.dc);
-    if (p.reset && (!kMany || g == 0)) {  // (looked at a chunk later: a branch on it here would wait for every load)
+    if (kOut && (!kMany || g == 0)) sq.template load<kFull>(qb + u * qstep + (kGroup ? g * p.da : 0), qstep, pad, p.da);
+    if (!kGroup || g == 0) {
+      sk.template load<kFull>(kb + u * kstep + (kMany ? g * p.da : 0), kstep, pad, p.da);
+      sv.template load<kFull>(vb + u * vstep + (kMany ? g * p.dc : 0), vstep, pad, p.dc);
+    }
+    if (p.reset && g == 0) {  // (looked at a chunk later: a branch on it here would wait for every load)
       const int t = max(ch * CL - pad0 + min(lane, CL - 1), min(r0, p.T - 1));
       flag = p.reset[static_cast<size_t>(p.rev && t > 0 ? p.T - t : t) * p.B + b];
     }
@@ -369,10 +378,12 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
   fetch(ch, g);
   while (ch < c1) {
     const int pad = !kFull && ch == 0 ? pad0 : 0;
-    const bool first = !kMany || g == 0, last = !kMany || g == p.gk - 1;
+    const bool first = !kMany || g == 0, last = !kMany || g == p.gk - 1;  // of the outputs' sums
     if (kOut && first) sq.template store<TL::QS, true>(lds.q);
-    sk.template store<TL::QS, true>(lds.k);
-    sv.template store<TL::VS, false>(lds.v);
+    if (!kGroup || g == 0) {
+      sk.template store<TL::QS, true>(lds.k);
+      sv.template store<TL::VS, false>(lds.v);
+    }
     uint64_t resets = 0;  // bit i: a reset before the chunk's step i
     if (p.reset) resets = __ballot(flag != 0 && lane < CL && ch * CL - pad0 + lane >= r0);
     const int rl = resets ? 63 - __builtin_clzll(resets) : -1;  // the last reset
@@ -386,7 +397,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
     auto last_reset = [&](int ti) { return resets ? __shfl(lr, ti * 16 + l16) : -1; };  // of step 16 ti + l16
     __syncthreads();
     int nch = ch, ng = g + 1;
-    if (!kMany || ng == p.gk) ++nch, ng = 0;
+    if (ng == (kMany ? p.gk : kGroup ? p.gq : 1)) ++nch, ng = 0;
     if (nch < c1) fetch(nch, ng);
 
     if (kOut) {  // p, 16 x 16 tiles at and below the diagonal, one after another to the waves
@@ -515,7 +526,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
       }
       int lrow = l16;
       asm volatile("" : "+v"(lrow));
-      E* orow = ob + static_cast<ptrdiff_t>(ch - c0) * CL * ostep + lrow * ostep + col0 + g4 * 4;
+      E* orow = ob + static_cast<ptrdiff_t>(ch - c0) * CL * ostep + lrow * ostep + (kGroup ? g * p.dc : 0) + col0 + g4 * 4;
       if (last) {
 #pragma unroll
         for (int ti = 0; ti < NI; ++ti) {
@@ -543,60 +554,62 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
       }
     }
 
-    if (rl > 0) {  // a key that is cut off may hold anything, and may not meet the zeros of what enters
-      for (int x = tid; x < rl * (TL::QS / 16); x += BT) *reinterpret_cast<u32x4*>(lds.k + x * 16) = u32x4{0, 0, 0, 0};
-      __syncthreads();
-    }
+    if (!kGroup || g == p.gq - 1) {
+      if (rl > 0) {  // a key that is cut off may hold anything, and may not meet the zeros of what enters
+        for (int x = tid; x < rl * (TL::QS / 16); x += BT) *reinterpret_cast<u32x4*>(lds.k + x * 16) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+      }
 
-    // the state after the chunk
-    if (first) {
-      if (resets) {
-        cut_any = true;
+      // the state after the chunk
+      if (first) {
+        if (resets) {
+          cut_any = true;
 #pragma unroll
-        for (int a = 0; a < NA; ++a)
+          for (int a = 0; a < NA; ++a)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) S[a][c] = f32x4{0, 0, 0, 0};
-      } else {
-        const float f = uniform(power(l2, CL - pad));
+            for (int c = 0; c < NC; ++c) S[a][c] = f32x4{0, 0, 0, 0};
+        } else {
+          const float f = uniform(power(l2, CL - pad));
 #pragma unroll
-        for (int a = 0; a < NA; ++a)
+          for (int a = 0; a < NA; ++a)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) S[a][c] *= f;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < NB; ++u) {
-      if (!kFull && u * 32 + 32 <= pad) continue;
-      __builtin_amdgcn_sched_barrier(0);
-      // what enters, in bf16 as a sum of terms
-      Frag term[NC][M::TERMS];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int tiles = NI - 1 - (2 * u + (i >> 2));
-          x[i] = (M::get(vf[c][u], i) * in[i & 3]) * (tiles == 0 ? 1.0f : tiles == 1 ? l16th : tiles == 2 ? l32 : l48);
-        }
-        if (rl > u * 32) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = u * 32 + (i >> 2) * 16 + g4 * 4 + (i & 3) >= rl ? x[i] : 0.0f;
-        }
-        term[c][0] = M::pack(x);
-#pragma unroll
-        for (int t = 1; t < M::TERMS; ++t) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] -= M::get(term[c][t - 1], i);
-          term[c][t] = M::pack(x);
+            for (int c = 0; c < NC; ++c) S[a][c] *= f;
         }
       }
 #pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        const Frag kf = M::template columns<TL::QS, true>(lds.k + u * 32 * TL::QS, a * 16 * ES, lane);
+      for (int u = 0; u < NB; ++u) {
+        if (!kFull && u * 32 + 32 <= pad) continue;
+        __builtin_amdgcn_sched_barrier(0);
+        // what enters, in bf16 as a sum of terms
+        Frag term[NC][M::TERMS];
 #pragma unroll
-        for (int t = M::TERMS - 1; t >= 0; --t)
+        for (int c = 0; c < NC; ++c) {
+          float x[8];
 #pragma unroll
-          for (int c = 0; c < NC; ++c) S[a][c] = M::mma(kf, term[c][t], S[a][c], upper(u));
+          for (int i = 0; i < 8; ++i) {
+            const int tiles = NI - 1 - (2 * u + (i >> 2));
+            x[i] = (M::get(vf[c][u], i) * in[i & 3]) * (tiles == 0 ? 1.0f : tiles == 1 ? l16th : tiles == 2 ? l32 : l48);
+          }
+          if (rl > u * 32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = u * 32 + (i >> 2) * 16 + g4 * 4 + (i & 3) >= rl ? x[i] : 0.0f;
+          }
+          term[c][0] = M::pack(x);
+#pragma unroll
+          for (int t = 1; t < M::TERMS; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] -= M::get(term[c][t - 1], i);
+            term[c][t] = M::pack(x);
+          }
+        }
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+          const Frag kf = M::template columns<TL::QS, true>(lds.k + u * 32 * TL::QS, a * 16 * ES, lane);
+#pragma unroll
+          for (int t = M::TERMS - 1; t >= 0; --t)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[a][c] = M::mma(kf, term[c][t], S[a][c], upper(u));
+        }
       }
     }
     __syncthreads();
@@ -617,7 +630,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kMany), waves_per_simd(D
           cut_any ? -1.0f : power(l2, (c1 - c0) * CL - (c0 == 0 ? pad0 : 0));
     return;
   }
-  if (!p.sT || (!kMany && hq % p.gq != 0)) return;
+  if (!p.sT || hq % p.gq != 0) return;
   const bool cut = p.rev && p.reset && p.reset[b] != 0;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -722,8 +735,10 @@ size_t pass_floats(const LinPass& p, int splits) {
   return static_cast<size_t>(splits) * p.B * p.nkv * (pad_head(p.da) * pad_head(p.dc) + 1);
 }
 
-template <typename E, int DA, int DC, bool kMany>
+template <typename E, int DA, int DC, Loop kLoop>
 void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
+  constexpr bool kMany = kLoop == kManyKeys;
+  constexpr int threads = block_threads(DA, DC, kMany);
   const LinPass& p = ps.pass[0];
   const int chunks = (p.T + Mx<E>::CL - 1) / Mx<E>::CL;
   const unsigned states = static_cast<unsigned>(p.B) * p.nkv;
@@ -737,39 +752,53 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
     }
   }
   if (splits > 1) {
-    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kMany, false>), dim3(states * ps.count, used), dim3(block_threads(DA, DC, kMany)), 0, s, ps);
+    constexpr Loop kParts = kMany ? kManyKeys : kAlone;
+    hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kParts, false>), dim3(states * ps.count, used), dim3(threads), 0, s, ps);
     hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
   }
   bool full = p.T % Mx<E>::CL == 0;
   for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
-  auto kernel = full ? linattn_chunks<E, DA, DC, true, kMany, true> : linattn_chunks<E, DA, DC, true, kMany, false>;
-  hipLaunchKernelGGL(kernel, dim3(states * p.gq * ps.count, used), dim3(block_threads(DA, DC, kMany)), 0, s, ps);
+  auto kernel = full ? linattn_chunks<E, DA, DC, true, kLoop, true> : linattn_chunks<E, DA, DC, true, kLoop, false>;
+  const unsigned blocks = states * (kLoop == kGroupQueries ? 1 : p.gq) * ps.count;
+  hipLaunchKernelGGL(kernel, dim3(blocks, used), dim3(threads), 0, s, ps);
 }
 
 template <typename E, int DA, int DC>
-void launch_many(Passes& ps, float* ws, int splits, hipStream_t s) {
+void launch_loop(Passes& ps, float* ws, int splits, bool group, hipStream_t s) {
   if (ps.pass[0].gk > 1)
-    launch_chunks<E, DA, DC, true>(ps, ws, splits, s);
+    launch_chunks<E, DA, DC, kManyKeys>(ps, ws, splits, s);
+  else if (group)
+    launch_chunks<E, DA, DC, kGroupQueries>(ps, ws, splits, s);
   else
-    launch_chunks<E, DA, DC, false>(ps, ws, splits, s);
+    launch_chunks<E, DA, DC, kAlone>(ps, ws, splits, s);
 }
 
 template <typename E>
-void launch_typed(Passes& ps, float* ws, int splits, hipStream_t s) {
+void launch_typed(Passes& ps, float* ws, int splits, bool group, hipStream_t s) {
   const bool a = ps.pass[0].da <= 64, c = ps.pass[0].dc <= 64;
   if (a && c)
-    launch_many<E, 64, 64>(ps, ws, splits, s);
+    launch_loop<E, 64, 64>(ps, ws, splits, group, s);
   else if (a)
-    launch_many<E, 64, 128>(ps, ws, splits, s);
+    launch_loop<E, 64, 128>(ps, ws, splits, group, s);
   else if (c)
-    launch_many<E, 128, 64>(ps, ws, splits, s);
+    launch_loop<E, 128, 64>(ps, ws, splits, group, s);
   else
-    launch_many<E, 128, 128>(ps, ws, splits, s);
+    launch_loop<E, 128, 128>(ps, ws, splits, group, s);
 }
 
 // Whether one kernel runs both passes.
 bool alike(const LinPass& x, const LinPass& y) {
   return pad_head(x.da) == pad_head(y.da) && pad_head(x.dc) == pad_head(y.dc) && x.gq == y.gq && x.gk == y.gk;
+}
+
+// Whether a block takes a state's query heads in turn: where the states alone
+// give each compute unit 2 blocks.  Forward, 256 steps of bf16, us by block a
+// head -> block a state: 512 states of 64 x 64, 2 heads each 39.9 -> 35.0; 1024 of
+// 128 x 128, 4 heads 297 -> 209; fp32, 100 steps, 386 -> 257.  With 256 states the
+// chip is half empty: 64 x 64, 2 heads 24.2 -> 28.4, 4 heads 38.3 -> 43.9; and 4
+// states over T = 10007, split further in the heads' place, take 62 for 54.
+bool group_queries(const LinPass& p, int count) {
+  return p.gq > 1 && static_cast<long long>(p.B) * p.nkv * count >= 512;
 }
 
 // Passes of one call in as few launches as they allow.
@@ -784,10 +813,11 @@ void launch_passes(o5_dtype dt, const LinPass* p, int count, void* ws, hipStream
         done[j] = true;
       }
     const int splits = plan_splits(dt, p[i].T, p[i].B, p[i].nkv, p[i].gq * ps.count);
+    const bool group = group_queries(p[i], ps.count);  // (so many states are not split)
     if (dt == O5_BF16)
-      launch_typed<uint16_t>(ps, static_cast<float*>(ws), splits, s);
+      launch_typed<uint16_t>(ps, static_cast<float*>(ws), splits, group, s);
     else
-      launch_typed<float>(ps, static_cast<float*>(ws), splits, s);
+      launch_typed<float>(ps, static_cast<float*>(ws), splits, group, s);
   }
 }
 

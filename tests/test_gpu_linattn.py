@@ -225,6 +225,67 @@ def test_what_a_reset_cuts_off_may_hold_anything(bf16):
         assert_close(name, np.where(fine, host(x), 0), np.where(fine, y, 0), TOL_STATE if name == "dS0" else TOL_OUT[bf16])
 
 
+#        T    B   nh nkv dk  dv  resets fused: 512 states and more, with several query heads each
+GROUPS = [
+    (64, 256, 4, 2, 64, 64, 0.02, False),
+    (65, 128, 12, 4, 64, 128, 0.05, True),
+    (128, 128, 8, 4, 128, 128, 0.02, False),
+    (47, 513, 3, 1, 40, 72, 0.1, True),
+    (1, 300, 8, 2, 128, 64, 0.5, False),
+]
+
+
+def of_samples(c, at):
+    """The inputs of some samples, which depend on no others."""
+    r = c.ref()
+    for name in ("q", "k", "v", "reset"):
+        r[name] = r[name][:, at]
+    r["S0"] = r["S0"][at]
+    return r
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shape", GROUPS, ids=lambda s: "x".join(map(str, s[:6])))
+def test_many_states_with_shared_heads(bf16, shape):
+    need_gpu()
+    banner(f"linattn many states with shared heads bf16={bf16} {shape}")
+    c = Case(bf16, *shape, seed=9)
+    B = shape[1]
+    at = [0, 1, B // 2, B - 1]
+    o, ST = c.fwd()
+    ref_o, states = linattn_fwd(**of_samples(c, at))
+    assert_close("o", host(o)[:, at], ref_o, TOL_OUT[bf16])
+    assert_close("ST", host(ST)[at], states[-1], TOL_STATE)
+    ref = linattn_bwd(dout=host(c.do)[:, at], dST=host(c.dST)[at], **of_samples(c, at))
+    for name, x, y in zip(("dq", "dk", "dv", "dS0"), c.bwd(), ref):
+        x = host(x)[at] if name == "dS0" else host(x)[:, at]
+        assert_close(name, x, y, TOL_STATE if name == "dS0" else TOL_OUT[bf16])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_many_states_and_inputs_that_are_not_finite(bf16):
+    """What is cut off reaches nothing, and what is not, exactly the recurrence's outputs, of each query head."""
+    need_gpu()
+    banner(f"linattn many states, non-finite inputs bf16={bf16}")
+    c = Case(bf16, 100, 256, 6, 2, 64, 64, resets=0, seed=10)
+    c.reset = torch.zeros((100, 256), dtype=torch.uint8, device="cuda")
+    c.reset[0, 0] = c.reset[40, 1] = c.reset[90, 1] = c.reset[33, 255] = 1
+    c.S0[0] = float("nan")
+    c.v[30, 1, 3] = float("inf")
+    c.v[95, 1, 5] = float("nan")
+    c.k[20, 255, 7] = float("nan")
+    at = [0, 1, 2, 255]
+    o, ST = c.fwd()
+    with np.errstate(invalid="ignore"):
+        ref_o, states = linattn_fwd(**of_samples(c, at))
+    fine = np.isfinite(ref_o)
+    o = host(o)[:, at]
+    assert 0 < np.sum(~fine) < fine.size
+    assert np.array_equal(np.isfinite(o), fine)
+    assert_close("o", np.where(fine, o, 0), np.where(fine, ref_o, 0), TOL_OUT[bf16])
+    assert np.array_equal(np.isfinite(host(ST)[at]), np.isfinite(states[-1]))
+
+
 def test_another_stream_and_a_graph():
     """The calls run on the stream that is current, and replay from a graph."""
     need_gpu()
