@@ -28,6 +28,12 @@ method computes, written so that it can be checked against the paper by eye:
                 deviation (appendix "Reward Weights"; Table "Hyperparameters").
 * ``adam``   -- Adam with the per-parameter gradient clip to +-5 sqrt(v)
                 (subsection "Optimizing the Policy"; Table "Hyperparameters").
+* ``linattn`` -- linear attention with a decay for each head and resets, its
+                gradient by the adjoint recurrence.
+* ``resnorm`` -- RMS norms before and after a block with its gate and residual
+                scale, forward and backward.
+* ``adamw``  -- AdamW over a tensor, its moments in 32 bits or in 8 bits with a
+                shared exponent and stochastic rounding (Philox4x32-7).
 * ``philox`` -- Philox4x64-10 counter-based generator and Gumbel-max action
                 sampling (sampling an action each timestep, subsection
                 "Playing Dota using AI").

@@ -306,6 +306,11 @@ __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Con
   }
 }
 
+// A block takes a chunk, a thread four consecutive elements, so that a wave
+// holds one group of 256 and the new exponent is one reduction within it.  HBM-
+// bound: 168M parameters with bf16 gradients, 8-bit moments and bf16 copies, 16
+// bytes each, 541 to 615 us, 5.0 to 4.4 TB/s; 5.3M with 32-bit moments 27 us, 5.9 TB/s
+// (partly from the caches).
 __global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, Consts c) {
   const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
@@ -366,6 +371,8 @@ __device__ __forceinline__ void moments(const Tensor& t, size_t i0, float* mo, f
   }
 }
 
+// The moments as they are stored, in fp32.  HBM-bound: 168M of 8 bits 272 to 280
+// us, 6.0 TB/s, most of it written.
 __global__ void __launch_bounds__(256) adamw_moments(const void* __restrict__ plan, uint32_t tensors,
                                                      float* __restrict__ mo, float* __restrict__ vo) {
   const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];

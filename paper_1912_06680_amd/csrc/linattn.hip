@@ -48,8 +48,8 @@ __device__ __forceinline__ float ld(const void* p, size_t i) {
 //   p_ij = oscale kscale l^(i-j) q_i . k_j
 //   S' = (r_{L-1} < 0) l^L S + sum_{j >= r_{L-1}} kscale l^(L-e-j) k_j v_j^T
 //
-// A block of 4 waves takes one state and runs through its chunks; each wave
-// owns a quarter of the state's columns in its accumulators.  Products are
+// A block of 4 or 8 waves takes one state and runs through its chunks; each wave
+// owns 16 or 32 of the state's columns in its accumulators.  Products are
 // formed transposed (o^T = S^T q^T + v^T p^T), so that the accumulators of S
 // are, as they lie, operands of the next product.
 //
@@ -65,7 +65,11 @@ __device__ __forceinline__ float ld(const void* p, size_t i) {
 // the last state written), and nearly as much by issue, per chunk and wave about
 // 1,000 vector and 150 matrix instructions of 4 and 16 cycles.  With both from
 // the L2 that shape takes 279 us, its memory traffic alone 343, together 377 to
-// 425 (4.3 to 3.8 TB/s; a copy runs at 5.1).
+// 440 on different cards (4.3 to 3.7 TB/s; a copy runs at 5.1).  The backward
+// pass reads each row array where a pass needs it, 12 row arrays moved for the
+// 7 of the call: T = 256, B = 64, 16 x 128 x 128 takes 230 to 250 us.  One
+// sequence (T = 10007, 4 states of 64 x 128, 16 query heads, 32 splits) is bound
+// by the latency of a chunk, five of them a block: 50 us, 37 of it the outputs.
 //
 // The reduction index of every product runs in blocks of 32; of a block, lane
 // group g = lane / 16 holds 4 g + r and 16 + 4 g + r (r = 0..3), which is how
@@ -653,7 +657,8 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), wav
 
 // The state before each split, in place of the split's own part, and the last
 // state: X_0 = S0, X_{s+1} = keep_s X_s + part_s.  A thread takes 4 rows of a
-// column (one accumulator).
+// column (one accumulator).  Bound by its loads' latency: 32 splits of 4 states
+// of 64 x 128 5.6 us.
 template <int DA, int DC>
 __global__ void __launch_bounds__(256) linattn_scan(Passes ps, int splits) {
   constexpr int NA = DA / 16, Q = DA * DC / 4;
