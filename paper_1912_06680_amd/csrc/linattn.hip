@@ -558,7 +558,11 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), wav
       }
     }
 
-    if (!kGroup || g == p.gq - 1) {
+    // Where no one takes the state after the last chunk, that chunk has no update (backward, 2 samples of T = 2048 in
+    // splits, 16 query heads on 4 states of 128 x 128: 116 -> 103 us; fp32, T = 16, B = 256, 16 on 8 of 64 x 64: 77 -> 75).
+    // Not in the kernel of most registers, which the branch costs more: T = 256, B = 64, 16 x 128 x 128: 231 -> 239.
+    const bool update = (kFull && DA + DC == 256) || ch + 1 < c1 || !kOut || (p.sT && !sp.states && hq == n * p.gq);
+    if ((!kGroup || g == p.gq - 1) && update) {
       if (rl > 0) {  // a key that is cut off may hold anything, and may not meet the zeros of what enters
         for (int x = tid; x < rl * (TL::QS / 16); x += BT) *reinterpret_cast<u32x4*>(lds.k + x * 16) = u32x4{0, 0, 0, 0};
         __syncthreads();
@@ -634,7 +638,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), wav
           cut_any ? -1.0f : power(l2, (c1 - c0) * CL - (c0 == 0 ? pad0 : 0));
     return;
   }
-  if (!p.sT || hq % p.gq != 0) return;
+  if (!p.sT || hq != n * p.gq) return;
   const bool cut = p.rev && p.reset && p.reset[b] != 0;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -761,7 +765,8 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
     hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kParts, false>), dim3(states * ps.count, used), dim3(threads), 0, s, ps);
     hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
   }
-  bool full = p.T % Mx<E>::CL == 0;
+  // (kFull's kernel of 128 x 128 has every update; in splits the last one's is worth more than kFull)
+  bool full = p.T % Mx<E>::CL == 0 && (DA + DC < 256 || splits == 1);
   for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
   auto kernel = full ? linattn_chunks<E, DA, DC, true, kLoop, true> : linattn_chunks<E, DA, DC, true, kLoop, false>;
   const unsigned blocks = states * (kLoop == kGroupQueries ? 1 : p.gq) * ps.count;
