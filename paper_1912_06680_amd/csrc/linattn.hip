@@ -253,6 +253,7 @@ struct Split {
 // The passes of one launch: alike in T, B, nkv and gq, and in the kernel that runs them.
 struct Passes {
   int count;
+  unsigned first;  // the call's block that is block 0 of this launch, a multiple of count
   LinPass pass[3];
   Split split[3];
 };
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), wav
   // (the passes of a call read the same rows: side by side, so that they find them in the caches)
   const LinPass& p = ps.pass[blockIdx.x % ps.count];
   const Split& sp = ps.split[blockIdx.x % ps.count];
-  const int block = blockIdx.x / ps.count;
+  const int block = (ps.first + blockIdx.x) / ps.count;
   const int heads = kOut && !kGroup ? p.nkv * p.gq : p.nkv;
   const int b = block / heads, n = kOut && !kGroup ? block % heads / p.gq : block % heads;
   const int hq = kGroup ? n * p.gq : block % heads;  // the block's (first) query head
@@ -769,8 +770,12 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
   bool full = p.T % Mx<E>::CL == 0 && (DA + DC < 256 || splits == 1);
   for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
   auto kernel = full ? linattn_chunks<E, DA, DC, true, kLoop, true> : linattn_chunks<E, DA, DC, true, kLoop, false>;
+  // A launch holds fewer than 2^32 threads in a dimension (with more the grid wraps and the rest is never run, without an
+  // error), so that more blocks go out in several.  (Split sequences have fewer than 256 states and heads.)
   const unsigned blocks = states * (kLoop == kGroupQueries ? 1 : p.gq) * ps.count;
-  hipLaunchKernelGGL(kernel, dim3(blocks, used), dim3(threads), 0, s, ps);
+  const unsigned most = 0xffffffffu / threads / ps.count * ps.count;
+  for (ps.first = 0; ps.first < blocks; ps.first += most)
+    hipLaunchKernelGGL(kernel, dim3(std::min(blocks - ps.first, most), used), dim3(threads), 0, s, ps);
 }
 
 template <typename E, int DA, int DC>
