@@ -311,8 +311,9 @@ __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Con
 // bound: 168M parameters with bf16 gradients, 8-bit moments and bf16 copies, 16
 // bytes each, 541 to 615 us, 5.0 to 4.4 TB/s; 5.3M with 32-bit moments 27 us, 5.9 TB/s
 // (partly from the caches).
-__global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, Consts c) {
-  const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];
+__global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, uint32_t first,
+                                                    Consts c) {
+  const Chunk ch = chunks_of(plan, tensors)[first + blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
   const float lr = c.lr * t.lr_scale;
   const float keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(t.weight_decay));
@@ -373,15 +374,24 @@ __device__ __forceinline__ void moments(const Tensor& t, size_t i0, float* mo, f
 
 // The moments as they are stored, in fp32.  HBM-bound: 168M of 8 bits 272 to 280
 // us, 6.0 TB/s, most of it written.
-__global__ void __launch_bounds__(256) adamw_moments(const void* __restrict__ plan, uint32_t tensors,
+__global__ void __launch_bounds__(256) adamw_moments(const void* __restrict__ plan, uint32_t tensors, uint32_t first,
                                                      float* __restrict__ mo, float* __restrict__ vo) {
-  const Chunk ch = chunks_of(plan, tensors)[blockIdx.x];
+  const Chunk ch = chunks_of(plan, tensors)[first + blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
   const size_t i = static_cast<size_t>(ch.index) * kChunk + threadIdx.x * 4;
   if ((static_cast<size_t>(ch.index) + 1) * kChunk <= t.n)
     moments<true>(t, i, mo + t.at, vo + t.at);
   else
     moments<false>(t, i, mo + t.at, vo + t.at);
+}
+
+// A launch holds fewer than 2^32 threads in a dimension (with more the grid
+// wraps and the rest is never run, without an error), so that a plan of more
+// chunks goes out in several: launch(first chunk, blocks).
+template <class F>
+void launch_chunks(uint32_t chunks, F&& launch) {
+  constexpr uint32_t kMost = 0xffffffffu / 256;
+  for (uint32_t first = 0; first < chunks; first += kMost) launch(first, std::min(chunks - first, kMost));
 }
 
 #define O5_TRY(expr)              \
@@ -481,7 +491,9 @@ extern "C" int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp 
   c.key0 = static_cast<uint32_t>(seed);
   c.key1 = static_cast<uint32_t>(seed >> 32);
   c.step = static_cast<uint32_t>(step);
-  hipLaunchKernelGGL(adamw_kernel, dim3(h->chunks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, c);
+  launch_chunks(h->chunks, [&](uint32_t first, uint32_t blocks) {
+    hipLaunchKernelGGL(adamw_kernel, dim3(blocks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, first, c);
+  });
   return check_launch(fn);
 }
 
@@ -491,6 +503,8 @@ extern "C" int o5_adamw_moments(const void* plan, const void* plan_dev, float* m
   O5_PTR(m, "m");
   O5_PTR(v, "v");
   const Header* h = static_cast<const Header*>(plan);
-  hipLaunchKernelGGL(adamw_moments, dim3(h->chunks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, m, v);
+  launch_chunks(h->chunks, [&](uint32_t first, uint32_t blocks) {
+    hipLaunchKernelGGL(adamw_moments, dim3(blocks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, first, m, v);
+  });
   return check_launch(fn);
 }

@@ -3,7 +3,7 @@
 HIP takes no launch of 2^32 threads or more in a dimension, so that such a
 call goes out in several.  Every element of the outputs is compared, those on
 both sides of a launch's end among them.  Tolerances as in test_gpu_linattn
-(bf16 outputs 1e-2 of the largest)."""
+(bf16 outputs 1e-2 of the largest) and test_gpu_operators_large."""
 import pytest
 import torch
 
@@ -69,3 +69,32 @@ def test_linattn_step_of_16_million_states():
         ref = 0.5 + ka[:, :, None] * va[:, None, :]
         assert torch.allclose(S[a:a + (1 << 22), 0], ref, rtol=1e-6, atol=1e-6)
         _near(o[a:a + (1 << 22)], (qa[:, :, None] * ref).sum(1))
+
+
+def test_adamw_more_chunks_than_a_launch():
+    """2^34 + 3079 elements, 8-bit moments: the first step from zero moments moves every parameter by the learning rate, and
+    every moment is the gradient's, to the eighth that a code resolves."""
+    need_gpu()
+    banner("adamw, 2^34 + 3079 elements")
+    n = (1 << 34) + 3 * 1024 + 7
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    me, ve = (torch.zeros((n + 255) // 256, dtype=torch.uint8, device="cuda") for _ in range(2))
+    t = [o5.adamw_tensor(p, g, m, v, me, ve)]
+    plan = torch.empty(o5.o5_adamw_plan_bytes(t), dtype=torch.uint8)
+    o5.o5_adamw_plan(t, plan)
+    plan_dev = plan.cuda()
+    o5.o5_adamw_step(plan, plan_dev, 1e-2, 0.9, 0.999, 1e-8, 0.0, 0, 1)
+    for a in range(0, n, 1 << 30):
+        assert torch.all((p[a:a + (1 << 30)] + 1e-2).abs_() <= 1e-6), a
+    # (the values of the moments need the moments and their exponents alone)
+    size = (n + 255) // 256 * 256
+    del p, g
+    torch.cuda.empty_cache()
+    mo, vo = torch.zeros(size, device="cuda"), torch.zeros(size, device="cuda")
+    o5.o5_adamw_moments(plan, plan_dev, mo, vo)
+    for x, value in ((mo, 0.05), (vo, 2.5e-4)):
+        for a in range(0, n, 1 << 30):
+            assert torch.all((x[a:min(n, a + (1 << 30))] / value - 1).abs_() <= 0.125), a
+    del m, v, me, ve, mo, vo, x
+    torch.cuda.empty_cache()
