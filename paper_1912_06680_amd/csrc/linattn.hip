@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(block_threads(DA, DC, kLoop == kManyKeys), wav
 
     // Where no one takes the state after the last chunk, that chunk has no update (backward, 2 samples of T = 2048 in
     // splits, 16 query heads on 4 states of 128 x 128: 116 -> 103 us; fp32, T = 16, B = 256, 16 on 8 of 64 x 64: 77 -> 75).
-    // Not in the kernel of most registers, which the branch costs more: T = 256, B = 64, 16 x 128 x 128: 231 -> 239.
+    // Not in the kernel of most registers, which the branch costs more where the state is taken (full_kernel).
     const bool update = (kFull && DA + DC == 256) || ch + 1 < c1 || !kOut || (p.sT && !sp.states && hq == n * p.gq);
     if ((!kGroup || g == p.gq - 1) && update) {
       if (rl > 0) {  // a key that is cut off may hold anything, and may not meet the zeros of what enters
@@ -745,6 +745,27 @@ size_t pass_floats(const LinPass& p, int splits) {
   return static_cast<size_t>(splits) * p.B * p.nkv * (pad_head(p.da) * pad_head(p.dc) + 1);
 }
 
+// Whether a launch takes the kernel of whole chunks.  That of 128 x 128 updates
+// the state after every chunk, the last one too; where no pass takes that state
+// and it is one of at most 4 updates, the other kernel, which leaves it out, is
+// faster.  us, whole chunks -> the other, 16 heads of one or of four to a state:
+// backward, one chunk, bf16 143 -> 136 and 179 -> 152, fp32 176 -> 150 and 224 ->
+// 170; four chunks, bf16 106.8 -> 107.2 and 178 -> 170, fp32 151 -> 146 and 238 ->
+// 226; eight, bf16 107 -> 113 and 222 -> 219, fp32 151 and 252 both.  Where the
+// state is taken the kernel of whole chunks stays (forward, one to eight chunks,
+// bf16 0 to 9 % and fp32 0 to 5 % faster).  A sequence in splits has no one to take its
+// last update, whatever its length.
+template <typename E, int DA, int DC>
+bool full_kernel(const Passes& ps, int chunks, int splits) {
+  if (ps.pass[0].T % Mx<E>::CL != 0) return false;
+  bool taken = false;
+  for (int i = 0; i < ps.count; ++i) {
+    if (ps.pass[i].da != DA || ps.pass[i].dc != DC) return false;
+    taken = taken || ps.pass[i].sT != nullptr;
+  }
+  return DA + DC < 256 || (splits == 1 && (taken || chunks > 4));
+}
+
 template <typename E, int DA, int DC, Loop kLoop>
 void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
   constexpr bool kMany = kLoop == kManyKeys;
@@ -766,10 +787,7 @@ void launch_chunks(Passes& ps, float* ws, int splits, hipStream_t s) {
     hipLaunchKernelGGL((linattn_chunks<E, DA, DC, false, kParts, false>), dim3(states * ps.count, used), dim3(threads), 0, s, ps);
     hipLaunchKernelGGL((linattn_scan<DA, DC>), dim3(states * (DA * DC / 1024), ps.count), dim3(256), 0, s, ps, used);
   }
-  // (kFull's kernel of 128 x 128 has every update; in splits the last one's is worth more than kFull)
-  bool full = p.T % Mx<E>::CL == 0 && (DA + DC < 256 || splits == 1);
-  for (int i = 0; i < ps.count; ++i) full = full && ps.pass[i].da == DA && ps.pass[i].dc == DC;
-  auto kernel = full ? linattn_chunks<E, DA, DC, true, kLoop, true> : linattn_chunks<E, DA, DC, true, kLoop, false>;
+  auto kernel = full_kernel<E, DA, DC>(ps, chunks, splits) ? linattn_chunks<E, DA, DC, true, kLoop, true> : linattn_chunks<E, DA, DC, true, kLoop, false>;
   // A launch holds fewer than 2^32 threads in a dimension (with more the grid wraps and the rest is never run, without an
   // error), so that more blocks go out in several.  (Split sequences have fewer than 256 states and heads.)
   const unsigned blocks = states * (kLoop == kGroupQueries ? 1 : p.gq) * ps.count;
