@@ -5,18 +5,22 @@ own parts of the state, a scan, a launch for the outputs) of one or of several c
 first of them short where the length is no multiple.  The sizes below pick each of these; the number of splits is read off
 the workspace, so that a size cannot leave its way unnoticed.
 
-Tolerances as in test_gpu_linattn, whose docstring derives them."""
+Tolerances (max|Y - ref| / max|ref|): outputs as in test_gpu_linattn, whose docstring derives them.  States: what enters
+one keeps 24 bits and is summed in fp32; a chunk adds to it in 7 roundings at most (6 products of three terms and the
+decay), so that the 64 chunks which a state of decay 1 - 2^-12 remembers are a random walk of 450 steps of at most 2^-24,
+21 x 2^-24 = 1.2e-6 at the outside.  (Operands of 16 bits leave 2.4e-6.)"""
 import numpy as np
 import pytest
 import torch
 
 from oracle.linattn import linattn_bwd, linattn_fwd
 from paper_1912_06680_amd import o5
-from tests.gpu_util import assert_close, banner, host, need_gpu
+from tests.gpu_util import assert_close, banner, dev_f32, host, need_gpu
 from tests.test_gpu_linattn import TOL_OUT, TOL_STATE, Case
 
 pytestmark = pytest.mark.gpu
 
+TOL_24 = 1.2e-6
 NAMES = ("dq", "dk", "dv", "dS0")
 
 
@@ -153,3 +157,25 @@ def test_inputs_that_are_not_finite(shape, decay, bf16):
     c.do[T - 80, b, n * (nh // nkv) * dv + 4] = float("inf")  # back to step T / 3
     c.do[5, b, n * (nh // nkv) * dv] = float("nan")         # back to the first step and dS0
     _backward(c, {(b, n), other})
+
+
+@pytest.mark.parametrize("T,B,splits", [(6000, 1, 94), (2048, 256, 1), (2052, 256, 1)])
+def test_states_keep_24_bits_in_bf16(T, B, splits):
+    """A state that remembers thousands of steps, summed in one block and across splits, is as exact as an fp32 sum."""
+    need_gpu()
+    banner(f"linattn states of long sequences T={T} B={B}")
+    c = Case(True, T, B, 1, 1, 64, 64, resets=0, seed=15)
+    c.decay = dev_f32(np.array([1.0 - 2.0 ** -12]))
+    assert _splits(c) == splits
+    _forward(c, ((B - 1, 0),), TOL_24)
+    _backward(c, ((B - 1, 0),), TOL_24)
+
+
+@pytest.mark.parametrize("shape", UNSPLIT + SPLIT, ids=lambda s: "x".join(map(str, s[:6])))
+def test_states_keep_24_bits_everywhere(shape):
+    need_gpu()
+    *size, picks, _ = shape
+    banner(f"linattn states {size}")
+    c = Case(True, *size, resets=0.004, seed=16)
+    _forward(c, picks[:1], TOL_24)
+    _backward(c, picks[:1], TOL_24)
