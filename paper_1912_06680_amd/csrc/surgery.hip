@@ -41,6 +41,16 @@ static Shape5 shape5(int D, int H, int A1) {
   return s;
 }
 
+// A launch holds fewer than 2^32 threads in a dimension (with more the grid
+// wraps and the rest is never run, without an error), so that a larger vector
+// goes out in several: launch(first thread, grid), blocks of 256.
+template <class F>
+static void launch_threads(size_t threads, F&& launch) {
+  constexpr size_t kMost = 0xffffffffu / 256 * size_t{256};
+  for (size_t first = 0; first < threads; first += kMost)
+    launch(first, dim3(static_cast<unsigned>((std::min(threads - first, kMost) + 255) / 256)));
+}
+
 constexpr int64_t kNew = -1;   // element takes a new random value
 constexpr int64_t kZero = -2;  // element is zero
 
@@ -79,11 +89,11 @@ __device__ __forceinline__ int64_t widen_source(I e, const Shape5& o, const Shap
 }
 
 template <typename I>
-__global__ void __launch_bounds__(256) widen_kernel(Shape5 o, Shape5 n, const float* __restrict__ p_old,
+__global__ void __launch_bounds__(256) widen_kernel(size_t first, Shape5 o, Shape5 n, const float* __restrict__ p_old,
                                                     const float* __restrict__ m_old, const float* __restrict__ v_old,
                                                     float* __restrict__ p_new, float* __restrict__ m_new,
                                                     float* __restrict__ v_new, float scale, uint64_t seed) {
-  const size_t t = static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  const size_t t = first + static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   const size_t e0 = t * 4;
   if (e0 >= n.total) return;
   uint64_t w0 = t, w1 = 0, w2 = 0, w3 = 0;
@@ -130,11 +140,11 @@ __device__ __forceinline__ size_t fold_source(size_t e, const Shape5& o, const S
   return o.wh + (e - n.wh);  // Wh, b, Wp, bp keep their order and sizes
 }
 
-__global__ void __launch_bounds__(256) fold_copy(Shape5 o, Shape5 n, const float* __restrict__ p_old,
+__global__ void __launch_bounds__(256) fold_copy(size_t first, Shape5 o, Shape5 n, const float* __restrict__ p_old,
                                                  const float* __restrict__ m_old, const float* __restrict__ v_old,
                                                  float* __restrict__ p_new, float* __restrict__ m_new,
                                                  float* __restrict__ v_new) {
-  const size_t e = static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  const size_t e = first + static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (e >= n.total) return;
   const size_t src = fold_source(e, o, n);
   p_new[e] = p_old[src];
@@ -193,14 +203,11 @@ extern "C" int o5_surgery_widen(int D, int H, int A1, int D2, int H2, const floa
   O5_PTR(m_new, "m_new");
   O5_PTR(v_new, "v_new");
   const Shape5 o = shape5(D, H, A1), n = shape5(D2, H2, A1);
-  const size_t threads = (n.total + 3) / 4;
-  const dim3 grid(static_cast<unsigned>((threads + 255) / 256));
-  if (n.total < (size_t{1} << 32))
-    hipLaunchKernelGGL(widen_kernel<uint32_t>, grid, dim3(256), 0, as_stream(stream), o, n, p_old, m_old, v_old,
-                       p_new, m_new, v_new, scale, seed);
-  else
-    hipLaunchKernelGGL(widen_kernel<uint64_t>, grid, dim3(256), 0, as_stream(stream), o, n, p_old, m_old, v_old,
-                       p_new, m_new, v_new, scale, seed);
+  auto kernel = n.total < (size_t{1} << 32) ? widen_kernel<uint32_t> : widen_kernel<uint64_t>;
+  launch_threads((n.total + 3) / 4, [&](size_t first, dim3 grid) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, as_stream(stream), first, o, n, p_old, m_old, v_old, p_new, m_new,
+                       v_new, scale, seed);
+  });
   return check_launch("o5_surgery_widen");
 }
 
@@ -219,8 +226,9 @@ extern "C" int o5_surgery_fold_input(int D, int H, int A1, int Dk, const float* 
   O5_PTR(v_new, "v_new");
   const Shape5 o = shape5(D, H, A1), n = shape5(Dk, H, A1);
   hipStream_t s = as_stream(stream);
-  hipLaunchKernelGGL(fold_copy, dim3(static_cast<unsigned>((n.total + 255) / 256)), dim3(256), 0, s, o, n, p_old,
-                     m_old, v_old, p_new, m_new, v_new);
+  launch_threads(n.total, [&](size_t first, dim3 grid) {
+    hipLaunchKernelGGL(fold_copy, grid, dim3(256), 0, s, first, o, n, p_old, m_old, v_old, p_new, m_new, v_new);
+  });
   hipLaunchKernelGGL(fold_bias, dim3(static_cast<unsigned>(H)), dim3(256), 0, s, o, n, Dk, p_old, E, p_new);
   return check_launch("o5_surgery_fold_input");
 }
