@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(256) obs_finalize(int Do, int nchunks, const C
 }
 
 template <typename E>
-__global__ void __launch_bounds__(256) obs_apply(size_t total4, int Do, const float* __restrict__ obs,
+__global__ void __launch_bounds__(256) obs_apply(size_t first, size_t total4, int Do, const float* __restrict__ obs,
                                                  const float* __restrict__ mean_f, const float* __restrict__ rstd_f,
                                                  float clip, E* __restrict__ o) {
-  const size_t i = static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;  // 4 consecutive elements
+  const size_t i = first + static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;  // 4 consecutive elements
   if (i >= total4) return;
   const int j = static_cast<int>((i * 4) % Do);
   const float4 x = reinterpret_cast<const float4*>(obs)[i];
@@ -306,13 +306,18 @@ extern "C" int o5_obs_normalize(o5_dtype dt, int N, int Do, const float* obs, do
   hipLaunchKernelGGL(obs_stats, dim3(cdiv(Do, 1024), w.nchunks), dim3(256), 0, s, N, Do, obs, part);
   hipLaunchKernelGGL(obs_finalize, dim3(cdiv(Do, 64)), dim3(256), 0, s, Do, w.nchunks, part, stats, eps, mean_f, rstd_f);
   const size_t total4 = static_cast<size_t>(N) * Do / 4;
-  const dim3 grid(static_cast<unsigned>((total4 + 255) / 256));
-  if (dt == O5_BF16)
-    hipLaunchKernelGGL(obs_apply<uint16_t>, grid, dim3(256), 0, s, total4, Do, obs, mean_f, rstd_f, clip,
-                       static_cast<uint16_t*>(o));
-  else
-    hipLaunchKernelGGL(obs_apply<float>, grid, dim3(256), 0, s, total4, Do, obs, mean_f, rstd_f, clip,
-                       static_cast<float*>(o));
+  // A launch holds fewer than 2^32 threads in a dimension (with more the grid wraps and the rest is never run, without an
+  // error), so that more observations go out in several.
+  constexpr size_t kMost = 0xffffffffu / 256 * size_t{256};
+  for (size_t first = 0; first < total4; first += kMost) {
+    const dim3 grid(static_cast<unsigned>((std::min(total4 - first, kMost) + 255) / 256));
+    if (dt == O5_BF16)
+      hipLaunchKernelGGL(obs_apply<uint16_t>, grid, dim3(256), 0, s, first, total4, Do, obs, mean_f, rstd_f, clip,
+                         static_cast<uint16_t*>(o));
+    else
+      hipLaunchKernelGGL(obs_apply<float>, grid, dim3(256), 0, s, first, total4, Do, obs, mean_f, rstd_f, clip,
+                         static_cast<float*>(o));
+  }
   ktimer_end(kSiteObsNorm, s);
   return check_launch("o5_obs_normalize");
 }
