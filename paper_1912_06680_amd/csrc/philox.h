@@ -33,8 +33,9 @@ __device__ __forceinline__ void philox4x64_10(uint64_t& c0, uint64_t& c1, uint64
   }
 }
 
-// U in (0, 1) from the top 24 bits of a word: ((word >> 40) + 1/2) / 2^24,
-// exact in fp32.
+// U in (0, 1] from the top 24 bits of a word: ((word >> 40) + 1/2) / 2^24 rounded
+// to fp32, which is exact below 1/2 (above it 25 bits are needed) and 1 for the
+// largest word.
 __device__ __forceinline__ float philox_uniform24(uint64_t word) {
   return (static_cast<float>(word >> 40) + 0.5f) * 5.9604644775390625e-08f;  // 2^-24
 }

@@ -84,7 +84,8 @@ __global__ void __launch_bounds__(kSampleWaves * 64) gumbel_sample_rows(
       philox4x64_10(c0, c1, c2, c3, seed, 0ull);
       const int w = idx[i] & 3;
       const uint64_t word = w == 0 ? c0 : w == 1 ? c1 : w == 2 ? c2 : c3;
-      score[i] = z[i] - logf(-logf(philox_uniform24(word)));
+      // (-ln U of the largest U, 1 - 2^-25, which rounds to 1 in fp32; else that logit won whatever the others are)
+      score[i] = z[i] - logf(fmaxf(-logf(philox_uniform24(word)), 0x1p-25f));
     }
   }
   const auto wave_min = [](float v) { return wave_reduce(v, INFINITY, [](float x, float y) { return fminf(x, y); }); };
