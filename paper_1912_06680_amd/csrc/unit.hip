@@ -198,25 +198,34 @@ UnitWs unit_ws(o5_dtype dt, int N, int H, int nk, int d, bool loss, bool one_pas
   return w;
 }
 
+// A launch holds fewer than 2^32 threads in a dimension (with more the grid
+// wraps and the rest is never run, without an error), so that more rows go out
+// in several.  (Rows that unit_dq takes are too wide for so many.)
+template <typename E>
+static void launch_logits(int N, int nk, int d, const float* q, const float* bq, const E* emb, float* z, hipStream_t s) {
+  constexpr int kMost = 0xffffffffu / 256;
+  for (int n = 0; n < N; n += kMost)
+    hipLaunchKernelGGL(unit_logits<E>, dim3(std::min(N - n, kMost)), dim3(256), 0, s, nk, d,
+                       q + static_cast<size_t>(n) * d, bq, emb + static_cast<size_t>(n) * nk * d,
+                       z + static_cast<size_t>(n) * nk);
+}
+
 void unit_forward(o5_dtype dt, int N, int H, int nk, const o5_unit_head& u, const void* h, char* ws, const UnitWs& w,
                   hipStream_t s) {
   float* q = reinterpret_cast<float*>(ws + w.q);
   float* zext = reinterpret_cast<float*>(ws + w.zext);
   const int d = w.d;
   const GemmPlan plan = plan_gemm(dt == O5_BF16, N, d, H, Split::kOne);
-  const dim3 grid(N);
   if (dt == O5_BF16) {
     KRows2<uint16_t> al{static_cast<const uint16_t*>(h), nullptr, nullptr, H, 0, H, H, N};
     KRows2<uint16_t> bl{static_cast<const uint16_t*>(u.Wq), nullptr, nullptr, H, 0, H, H, d};
     run_gemm(plan, al, bl, EpiStoreF32{q, d, 0}, N, d, H, s);
-    hipLaunchKernelGGL(unit_logits<uint16_t>, grid, dim3(256), 0, s, nk, d, q, u.bq,
-                       static_cast<const uint16_t*>(u.E), zext);
+    launch_logits(N, nk, d, q, u.bq, static_cast<const uint16_t*>(u.E), zext, s);
   } else {
     KRows2<float> al{static_cast<const float*>(h), nullptr, nullptr, H, 0, H, H, N};
     KRows2<float> bl{static_cast<const float*>(u.Wq), nullptr, nullptr, H, 0, H, H, d};
     run_gemm(plan, al, bl, EpiStoreF32{q, d, 0}, N, d, H, s);
-    hipLaunchKernelGGL(unit_logits<float>, grid, dim3(256), 0, s, nk, d, q, u.bq, static_cast<const float*>(u.E),
-                       zext);
+    launch_logits(N, nk, d, q, u.bq, static_cast<const float*>(u.E), zext, s);
   }
 }
 
