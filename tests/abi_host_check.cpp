@@ -5,6 +5,7 @@
 // last line "abi_host_check: all N checks passed" mean that every check held
 // and the sanitizers reported nothing (they abort the process on a report).
 #include <climits>
+#include <cmath>
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
@@ -40,6 +41,7 @@ static void check_strings() {
   EXPECT(o5_ktimer_read(-1, &ms, &n) != O5_OK);
   EXPECT(o5_ktimer_read(1 << 20, &ms, &n) != O5_OK);
   EXPECT(o5_ktimer_enable(0) == O5_OK);
+  EXPECT(o5_ktimer_enable_sites(0) == O5_OK);
 }
 
 static void check_gae() {
@@ -220,12 +222,134 @@ static void check_adam_surgery_misc() {
   EXPECT(o5_prelstm_bwd(O5_BF16, 2, 10, 64, 64, P(), F(), P(), F(), F(), nullptr, 0, nullptr) == O5_E_WORKSPACE);
 }
 
+// The parallel recurrent core: linear attention, the norms around a block, AdamW over many tensors.
+static void check_linattn() {
+  for (int dt = 0; dt < 2; ++dt) {
+    const o5_dtype d = static_cast<o5_dtype>(dt);
+    const size_t need = o5_linattn_fwd_workspace_bytes(d, 1000, 2, 8, 4, 64, 128);
+    const size_t bneed = o5_linattn_bwd_workspace_bytes(d, 1000, 2, 8, 4, 64, 128);
+    EXPECT(need > 256 && bneed >= need);
+    const auto fwd = [&](int T, int nh, const void* q, size_t ldq, float scale, const float* S0, void* o, void* ws, size_t n) {
+      return o5_linattn_fwd(d, T, 2, nh, 4, 64, 128, q, ldq, P(), 256, P(), 512, F(), scale, S0, U8(), o, 1024, F(), ws, n, nullptr);
+    };
+    EXPECT(fwd(0, 8, P(), 512, 1.0f, F(), P(), P(), need) == O5_E_SHAPE);
+    EXPECT(fwd(INT_MAX, 8, P(), 512, 1.0f, F(), P(), P(), need) == O5_E_SHAPE);
+    EXPECT(fwd(1000, 6, P(), 512, 1.0f, F(), P(), P(), need) == O5_E_SHAPE);
+    EXPECT(fwd(1000, 8, P(), 504, 1.0f, F(), P(), P(), need) == O5_E_SHAPE);
+    EXPECT(fwd(1000, 8, P(), SIZE_MAX - 7, 1.0f, F(), P(), P(), need) == O5_E_SHAPE);
+    EXPECT(fwd(1000, 8, nullptr, 512, 1.0f, F(), P(), P(), need) == O5_E_NULL);
+    EXPECT(fwd(1000, 8, P(0x1002), 512, 1.0f, F(), P(), P(), need) == O5_E_ALIGN);
+    EXPECT(fwd(1000, 8, P(), 512, INFINITY, F(), P(), P(), need) == O5_E_ARG);
+    EXPECT(fwd(1000, 8, P(), 512, 1.0f, F(0x1004), P(), P(), need) == O5_E_ALIGN);
+    EXPECT(fwd(1000, 8, P(), 512, 1.0f, nullptr, nullptr, P(), need) == O5_E_NULL);
+    EXPECT(fwd(1000, 8, P(), 512, 1.0f, nullptr, P(), nullptr, need) == O5_E_WORKSPACE);
+    EXPECT(fwd(1000, 8, P(), 512, 1.0f, nullptr, P(), P(), need - 1) == O5_E_WORKSPACE);
+    const auto bwd = [&](const void* dout, size_t lddq, void* dk, const float* dST, size_t n) {
+      return o5_linattn_bwd(d, 1000, 2, 8, 4, 64, 128, P(), 512, P(), 256, P(), 512, F(), 1.0f, nullptr, nullptr, dout, 1024, dST,
+                            P(), lddq, dk, 256, P(), 512, F(), P(), n, nullptr);
+    };
+    EXPECT(bwd(nullptr, 512, P(), F(), bneed) == O5_E_NULL);
+    EXPECT(bwd(P(), 510, P(), F(), bneed) == O5_E_SHAPE);
+    EXPECT(bwd(P(), 512, nullptr, F(), bneed) == O5_E_NULL);
+    EXPECT(bwd(P(), 512, P(), F(0x1008), bneed) == O5_E_ALIGN);
+    EXPECT(bwd(P(), 512, P(), nullptr, bneed - 1) == O5_E_WORKSPACE);
+    EXPECT(o5_linattn_step(d, 2, 8, 4, 64, 128, P(), 512, P(), 256, P(), 512, F(), 1.0f, nullptr, nullptr, P(), 1024, nullptr) ==
+           O5_E_NULL);
+    EXPECT(o5_linattn_step(d, -2, 8, 4, 64, 128, P(), 512, P(), 256, P(), 512, F(), 1.0f, nullptr, F(), P(), 1024, nullptr) ==
+           O5_E_SHAPE);
+    const int big[] = {INT_MIN, -1, 0, 1, 8, 128, 136, 65536, (1 << 24) - 1, 1 << 30, INT_MAX};
+    for (int T : big)
+      for (int B : big)
+        for (int nh : big)
+          for (int nkv : {-1, 0, 1, 8, INT_MAX}) {
+            (void)o5_linattn_fwd_workspace_bytes(d, T, B, nh, nkv, 64, 128);
+            (void)o5_linattn_bwd_workspace_bytes(d, T, B, nh, nkv, 8, T);
+            ++g_checks;
+          }
+  }
+  EXPECT(o5_linattn_fwd_workspace_bytes(static_cast<o5_dtype>(9), 1, 1, 1, 1, 8, 8) == 0);
+}
+
+static void check_resnorm() {
+  const o5_dtype t = O5_BF16;
+  const auto fwd = [&](o5_dtype dt, int N, int D, const void* u, const void* gate, size_t ldg, const float* w_pre, float eps) {
+    return o5_resnorm_fwd(t, dt, N, D, P(), u, gate, ldg, F(), F(), w_pre, eps, P(), P(), nullptr, F(0x1008), nullptr);
+  };
+  EXPECT(fwd(O5_F32, 4, 64, P(), P(), 64, F(), 1e-6f) == O5_E_DTYPE);
+  EXPECT(fwd(t, 0, 64, P(), P(), 64, F(), 1e-6f) == O5_E_SHAPE);
+  EXPECT(fwd(t, INT_MAX, INT_MAX, P(), P(), 64, F(), 1e-6f) == O5_E_SHAPE);
+  EXPECT(fwd(t, 4, 64, P(), P(), 60, F(), 1e-6f) == O5_E_SHAPE);
+  EXPECT(fwd(t, 4, 64, P(), P(), SIZE_MAX - 7, F(), 1e-6f) == O5_E_SHAPE);
+  EXPECT(fwd(t, 4, 64, nullptr, P(), 64, F(), 1e-6f) == O5_E_ARG);
+  EXPECT(fwd(t, 4, 64, nullptr, nullptr, 0, nullptr, 1e-6f) == O5_E_ARG);
+  EXPECT(fwd(t, 4, 64, P(), P(), 64, F(), NAN) == O5_E_ARG);
+  EXPECT(fwd(t, 4, 64, P(), P(), 64, F(), 1e-6f) == O5_E_ALIGN);  // (r_pre above)
+  const size_t need = o5_resnorm_bwd_workspace_bytes(t, t, 4, 64);
+  EXPECT(need > 0);
+  const auto bwd = [&](const float* r_post, void* dgate, size_t lddg, void* ws, size_t n) {
+    return o5_resnorm_bwd(t, t, 4, 64, P(), P(), P(), 64, F(), F(), F(), r_post, F(), P(), P(), P(), P(), dgate, lddg, F(), F(),
+                          F(), ws, n, nullptr);
+  };
+  EXPECT(bwd(nullptr, P(), 64, P(), need) == O5_E_NULL);
+  EXPECT(bwd(F(), nullptr, 64, P(), need) == O5_E_NULL);
+  EXPECT(bwd(F(), P(), 56, P(), need) == O5_E_SHAPE);
+  EXPECT(bwd(F(), P(), 64, nullptr, need) == O5_E_WORKSPACE);
+  EXPECT(bwd(F(), P(), 64, P(), need - 1) == O5_E_WORKSPACE);
+  for (int N : {INT_MIN, -1, 0, 1, 1 << 20, (1 << 30) - 1, 1 << 30, INT_MAX})
+    for (int D : {INT_MIN, -8, 0, 4, 8, 8192, 8200, INT_MAX}) {
+      (void)o5_resnorm_bwd_workspace_bytes(O5_F32, t, N, D);
+      ++g_checks;
+    }
+}
+
+static void check_adamw() {
+  const auto tensor = [](size_t n, int bits) {
+    return o5_adamw_tensor{n, F(), P(), P(), P(), U8(), U8(), nullptr, 1.0f, 0.0f, O5_F32, bits};
+  };
+  EXPECT(o5_adamw_plan_bytes(1, nullptr) == 0);
+  EXPECT(o5_adamw_plan_bytes(-1, nullptr) == 0);
+  // plans in heap buffers of exactly their size, with whole and partial chunks: a byte past the end is reported
+  for (size_t n : {size_t{1}, size_t{1023}, size_t{1024}, size_t{1025}, size_t{1000003}})
+    for (int count : {1, 3, 100}) {
+      o5_adamw_tensor* t = new o5_adamw_tensor[count];
+      for (int i = 0; i < count; ++i) t[i] = tensor(n + i, i % 2 ? 8 : 32);
+      const size_t bytes = o5_adamw_plan_bytes(count, t);
+      EXPECT(bytes > 0);
+      char* plan = new char[bytes];
+      EXPECT(o5_adamw_plan(count, t, plan, bytes) == O5_OK);
+      EXPECT(o5_adamw_plan(count, t, plan, bytes - 1) == O5_E_WORKSPACE);
+      EXPECT(o5_adamw_plan(count, t, plan + 1, bytes) == O5_E_ALIGN);
+      const o5_adam_hp hp{1e-3f, 0.9f, 0.999f, 1e-8f, 5.0f};
+      EXPECT(o5_adamw_step(plan, nullptr, hp, 1, 1, nullptr) == O5_E_NULL);
+      EXPECT(o5_adamw_step(plan, P(), hp, 1, 0, nullptr) == O5_E_ARG);
+      EXPECT(o5_adamw_step(plan, P(), o5_adam_hp{NAN, 0.9f, 0.999f, 1e-8f, 5.0f}, 1, 1, nullptr) == O5_E_ARG);
+      EXPECT(o5_adamw_moments(plan, P(), nullptr, F(), nullptr) == O5_E_NULL);
+      std::memset(plan, 0, 16);
+      EXPECT(o5_adamw_step(plan, P(), hp, 1, 1, nullptr) == O5_E_ARG);
+      EXPECT(o5_adamw_moments(plan, P(), F(), F(), nullptr) == O5_E_ARG);
+      delete[] plan;
+      delete[] t;
+    }
+  o5_adamw_tensor bad[4] = {tensor(0, 32), tensor(SIZE_MAX, 32), tensor(10, 16), tensor(10, 8)};
+  bad[3].v_exp = nullptr;
+  for (const o5_adamw_tensor& b : bad) {
+    char plan[64];
+    EXPECT(o5_adamw_plan_bytes(1, &b) == 0);
+    EXPECT(o5_adamw_plan(1, &b, plan, sizeof plan) != O5_OK);
+  }
+  const o5_adamw_tensor huge[3] = {tensor((size_t{1} << 40) - 1, 8), tensor((size_t{1} << 40) - 1, 8), tensor((size_t{1} << 40) - 1, 8)};
+  EXPECT(o5_adamw_plan_bytes(3, huge) == 0);
+}
+
 int main() {
   check_strings();
   check_gae();
   check_lstm();
   check_heads_and_sampler();
   check_adam_surgery_misc();
+  check_linattn();
+  check_resnorm();
+  check_adamw();
   if (g_fail) {
     std::printf("abi_host_check: %d of %d checks failed\n", g_fail, g_checks);
     return 1;
