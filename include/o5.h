@@ -520,7 +520,15 @@ int o5_surgery_fold_input(int D, int H, int A1, int Dk, const float* E,
  *   S_t = d_n (1 - reset[t,b]) S_{t-1} + k_t v_t^T        (S_{-1} = S0)
  *   o_{t,h} = scale S_t^T q_{t,h}
  *
- * dt       type of q, k, v, o and of dout, dq, dk, dv.
+ * dt       type of q, k, v, o and of dout, dq, dk, dv.  Products add up in
+ *          fp32, and states and their gradients are as exact as an fp32 sum.
+ *          In bf16 o5_linattn_fwd and _bwd round two operands of an output's
+ *          products to bf16, as q, k and v are: the scores q_i . k_j of nearby
+ *          steps and the carried state (_bwd alike, G for the state).  An
+ *          output or gradient is then up to 2.5e-3 off in the 2-norm, where
+ *          its own rounding alone makes up to 1.8e-3.  o5_linattn_step rounds
+ *          its output alone, so that a token and the same step of a sequence
+ *          differ by about 2.6e-3.  In O5_F32 nothing is rounded to fewer bits.
  * T, B     steps and samples, >= 1, T*B below 2^30.   nh: query heads, a
  *          multiple of nkv, the key/value and state heads; B*nh below 2^24.
  * dk, dv   widths of a key (and query) and of a value, multiples of 8 in
@@ -628,10 +636,11 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
  *   m = b1 m + (1-b1) g';   mh = m / (1 - b1^step)
  *   p = (1 - lr wd) p - lr mh / (sqrt(vh) + eps)     (lr: hp.lr * lr_scale)
  *
- * A tensor: n elements (1..2^40-1); p [n] fp32, updated in place; g [n] of
- * type g_dt; p_bf16 out [n], a bf16 copy of the new p, or NULL; lr_scale and
- * weight_decay >= 0.  bits = 32: m, v [n] fp32, in place (m_exp, v_exp
- * unused).  bits = 8: m, v [n] bytes and m_exp, v_exp, one byte for each 256
+ * A tensor: n elements (1..2^40-1; together, in runs of 1024 of which a
+ * tensor's last may be partial, fewer than 2^31 runs); p [n] fp32, updated in
+ * place; g [n] of type g_dt; p_bf16 out [n], a bf16 copy of the new p, or NULL;
+ * lr_scale and weight_decay >= 0.  bits = 32: m, v [n] fp32, in place (m_exp,
+ * v_exp unused).  bits = 8: m, v [n] bytes and m_exp, v_exp, one byte for each 256
  * elements (the last may be partial; no alignment needed), start from zeros
  * everywhere.  With a = max(exp - 127, -90) and e, f the code's exponent field and its 3
  * mantissa bits, a code stands for
