@@ -86,7 +86,16 @@ class AdamwTensor(ctypes.Structure):
 
 def adamw_tensor(p, g, m, v, m_exp=None, v_exp=None, p_bf16=None, lr_scale=1.0, weight_decay=0.0):
     """An o5_adamw_tensor over torch tensors (keep the tensors alive while the plan is used): g's type by its dtype,
-    moments in 8 bits where m is a tensor of bytes."""
+    moments in 8 bits where m is a tensor of bytes.  Refuses tensors that the kernels would read as what they are not."""
+    n = p.numel()
+    state = torch.uint8 if m.dtype == torch.uint8 else torch.float32
+    groups = (n + 255) // 256 if state == torch.uint8 else 0
+    for name, t, dtypes, least in (("p", p, (torch.float32,), n), ("g", g, (torch.float32, torch.bfloat16), n),
+                                   ("m", m, (state,), n), ("v", v, (state,), n), ("m_exp", m_exp, (torch.uint8,), groups),
+                                   ("v_exp", v_exp, (torch.uint8,), groups), ("p_bf16", p_bf16, (torch.bfloat16,), n)):
+        if t is not None and (t.dtype not in dtypes or t.numel() < least or not t.is_contiguous()):
+            raise ValueError(f"adamw_tensor: {name} must be contiguous, of {' or '.join(map(str, dtypes))} and of at least "
+                             f"{least} elements, not {t.dtype} {tuple(t.shape)}")
     return AdamwTensor(p.numel(), _p(p), _p(g), _p(m), _p(v), _p(m_exp), _p(v_exp), _p(p_bf16), float(lr_scale),
                        float(weight_decay), O5_BF16 if g.dtype == torch.bfloat16 else O5_F32,
                        8 if m.dtype == torch.uint8 else 32)
