@@ -59,7 +59,10 @@ __device__ __forceinline__ float ld(const void* p, size_t i) {
 // factor (24 bits), so that a state after 10,000 steps is as exact as one summed
 // in fp32 (1.2e-7 of its size at T = 256, 2.3e-7 at T = 10007; with two terms
 // 2.4e-6, and T = 256, B = 128, 32 x 128 x 128 takes 5 % less).  fp32 runs on
-// fp32 matrix instructions throughout, with chunks of 32 steps.
+// fp32 matrix instructions throughout, with chunks of 32 steps.  The rounded
+// operands leave bf16 outputs 2.35e-3 off in the 2-norm, 1.65e-3 of it their own
+// rounding; as two bf16 terms each they would leave 1.66e-3, at 8 to 18 % more time
+// (that shape 377 -> 409 us; states of 64 x 128 spill and take twice as long).
 //
 // Bound: by bytes in the limit (q, k, v read once, o written once, S0 read and
 // the last state written), and nearly as much by issue, per chunk and wave about
@@ -69,7 +72,9 @@ __device__ __forceinline__ float ld(const void* p, size_t i) {
 // pass reads each row array where a pass needs it, 12 row arrays moved for the
 // 7 of the call: T = 256, B = 64, 16 x 128 x 128 takes 230 to 250 us.  One
 // sequence (T = 10007, 4 states of 64 x 128, 16 query heads, 32 splits) is bound
-// by the latency of a chunk, five of them a block: 50 us, 37 of it the outputs.
+// by the latency of a chunk, five of them a block, and by work done over: 50 us,
+// 37 of it the outputs, where each of a state's four query heads repeats its
+// updates, and 11 the splits' states, 128 blocks on 256 compute units.
 //
 // The reduction index of every product runs in blocks of 32; of a block, lane
 // group g = lane / 16 holds 4 g + r and 16 + 4 g + r (r = 0..3), which is how
@@ -259,7 +264,9 @@ struct Passes {
 };
 
 // Column tiles of a wave: two where the state's accumulators would else need 8 waves of more registers than they can
-// have (128 x 128 with one tile spills: 543 us against 423 at T = 256, B = 128, 32 heads).
+// have (128 x 128 with one tile spills: 543 us against 423 at T = 256, B = 128, 32 heads).  With two, the bf16 kernels of
+// 128 x 128 hold all 256 registers and spill a few more: 1 (kAlone), 3 (kGroupQueries) and 15 (kManyKeys) with whole
+// chunks, 2 in kManyKeys without.
 constexpr int tile_columns(int da, int dc, bool many) { return (da == 128 || many) && dc == 128 ? 2 : 1; }
 constexpr int block_threads(int da, int dc, bool many) { return dc / 16 / tile_columns(da, dc, many) * 64; }
 constexpr int waves_per_simd(int da, int dc, bool many) {
@@ -722,7 +729,10 @@ int pad_head(int d) { return d <= 64 ? 64 : 128; }
 // to fill the chip, so many that about 512 blocks (2 on each compute unit)
 // run.  Split, a block goes through its chunks twice (the states, then the
 // outputs) and two more launches take about four chunks' time, so a sequence
-// of few chunks stays whole.
+// of few chunks stays whole.  Chunks are what is counted: where a block takes gk
+// heads in each (dk and dv of shared states) it is gk times as long, and a short
+// sequence of few states stays whole all the same (backward, T = 256, B = 8, 4
+// states of 64 x 64 with 4 heads each: 66 us, its bytes 3.6).
 int plan_splits(o5_dtype dt, int T, int B, int nkv, int gq) {
   const int cl = dt == O5_BF16 ? Mx<uint16_t>::CL : Mx<float>::CL;
   const int chunks = (T + cl - 1) / cl;

@@ -14,11 +14,16 @@ namespace o5 {
 namespace {
 
 constexpr int kMaxWidth = 8192;
-// Blocks that walk the rows.  Two on each compute unit read fastest in the
-// forward pass (32768 x 4096 in bf16: 257 us, 276 with one, 262 with three and
-// four; 40000 x 512: 33, 43, 33); the backward pass has more of a row in flight
-// and sums to write for each block: one (391 us, 423 with two; 40000 x 512:
-// 62 and 59).
+// Blocks that walk the rows: two on each compute unit in the forward pass, one
+// in the backward pass, which has more of a row in flight and sums to write for
+// each block.  us, two / one, forward: the norm before alone, 32768 x 4096 in
+// bf16, 91 / 130; with block and gate 4096 x 4096 27.6 / 32.5, 40000 x 1032 91 /
+// 136, 40000 x 512 32 / 43, in fp32 61 / 61, 157 / 152 and 79 / 76.  One is
+// faster where block and gate come with many wide rows: 32768 x 4096 260 / 231,
+// in fp32 514 / 474; 2048 x 8192 32 / 28.  Backward with block and gate, one / two:
+// 16384 x 4096 202 / 217, in fp32 400 / 404, fp32 with bf16 blocks 267 / 289; 40000
+// x 512 63 / 62, 122 / 129 and 87 / 90.  Two are faster for rows of few lanes: 40000
+// x 256 54 / 39, 69 / 63 and 55 / 44; 40000 x 64 53 / 37, 56 / 40 and 54 / 38.
 constexpr int kFwdBlocks = 512, kBwdBlocks = 256;
 
 typedef float f4_t __attribute__((ext_vector_type(4)));
@@ -90,7 +95,7 @@ struct FwdRow {
 
 // TR threads of a block of max(256, TR) take a row, 8 elements each in NJ
 // runs, and walk the rows with the gains in registers.  HBM-bound: 32768 x 4096
-// in bf16 257 us, 5.2 TB/s; 60 x 1024 4 us, a row's latency.
+// in bf16 260 us, 5.2 TB/s, in fp32 504 to 514; 60 x 1024 4 us, a row's latency.
 template <typename X, typename E, int TR, int NJ>
 __global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_fwd(NormFwd p) {
   constexpr int BT = TR < 256 ? 256 : TR;
@@ -204,8 +209,10 @@ struct BwdRow {
 //   dw_pre = sum dn x' r_x',  drho = w_post sum d s y,  dw_post = rho sum d s y
 // Every operand of the next row is in flight while a row is worked on, and
 // the gains stay in registers (read again for each row they were half as many
-// bytes as the row itself).  HBM-bound: 32768 x 4096 in bf16 390 us, 5.5 TB/s;
-// 5003 x 1000 in fp32 and bf16 19.5 us, 4.6 TB/s.
+// bytes as the row itself).  HBM-bound: 32768 x 4096 in bf16 390 us, 5.5 TB/s,
+// in fp32 782 us; 5003 x 1000 in fp32 and bf16 19.5 us, 4.6 TB/s.  The fp32 forms
+// above 1024 columns hold 256 registers, one wave a SIMD, and that of 4104 to 8192
+// spills 14 more (8192 x 8192: 424 us, 5.1 TB/s).
 template <typename X, typename E, int TR, int NJ>
 __global__ void __launch_bounds__(TR < 256 ? 256 : TR) resnorm_bwd(NormBwd p) {
   constexpr int BT = TR < 256 ? 256 : TR, ROWS = BT / TR;
@@ -374,7 +381,9 @@ __global__ void __launch_bounds__(1024) resnorm_columns(int groups, int D, const
   }
 }
 
-// Threads of a row: 8 or 16 elements each.
+// Threads of a row: 8 or 16 elements each, but a wave at least, most of whose
+// lanes have nothing where the row is narrow (40000 x 64 in bf16: 25 us forward and
+// 53 backward, where the bytes take 5 and 8).
 int row_threads(int D) { return D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
 
 int row_blocks(int N, int D, int most) {

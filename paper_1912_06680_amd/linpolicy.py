@@ -37,6 +37,9 @@ class LinPolicy:
     """Parameters, buffers and call sequence for segments of T steps of B environments.
 
     D: width, a multiple of 64; heads: of D / heads, a multiple of 8 up to 128; head_sizes: of the action heads.
+
+    self.S0 holds the blocks' states before the segments, zeros at first.  To train on the segments that follow, copy
+    self.ST into it, with zeros where the last step's `dones` is set: a segment's resets begin at its second step.
     """
 
     def __init__(self, T, B, D, layers, heads, head_sizes, dtype="bf16", bits=8, seed=0, lr=5e-5, weight_decay=0.01,

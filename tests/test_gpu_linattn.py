@@ -4,8 +4,8 @@ Tolerances (max|Y - ref| / max|ref| per output): in fp32 an output is a sum of
 up to a few hundred products of both signs, each rounded to 2^-24: 2e-5 holds
 300 of them.  In bf16 an output is rounded to 2^-9 and so are, as operands of
 its products, the scores and the carried state: 3 x 2^-9 < 1e-2.  The states
-and their gradients stay in fp32 and their operands keep 16 bits: 2^-16 of each
-product, 2e-5."""
+and their gradients stay in fp32 and what enters them keeps 24 bits: 2e-5 as for
+an output in fp32 (test_gpu_linattn_paths holds them to 1.2e-6)."""
 import numpy as np
 import pytest
 import torch

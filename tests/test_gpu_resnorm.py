@@ -5,7 +5,7 @@ up to 8192 terms added in trees of at most 32 terms in a row, and from products
 and square roots rounded to 2^-24 each, the gate from a reciprocal and an
 exponential of about 1 ulp: 1e-5.  A bf16 output is rounded to 2^-9 of itself:
 4e-3 with the terms above.  Column sums add the rows of a group in order, at
-most N / 512 + 1 of them, and then the groups: 2e-5 at the sizes here."""
+most N / 256 + 1 of them, and then the groups: 2e-5 at the sizes here."""
 import numpy as np
 import pytest
 import torch
