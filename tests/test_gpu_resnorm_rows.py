@@ -1,7 +1,7 @@
 """GPU: the fused norms where a block walks several rows of more than 2048 columns, against their definition in fp64.
 
 From 2049 columns on a row takes a whole block, 512 blocks in the forward pass and 256 in the backward pass, so that these
-shapes walk 2 to 5 rows a block, the last round with blocks that have none: the next row's operands in flight, the sums
+shapes walk 2 to 5 rows a block, at the last of them some blocks with none: the next row's operands in flight, the sums
 over a row used again for the next, the column sums carried over the rows.
 
 Tolerances as in test_gpu_resnorm: fp32 1e-5 and bf16 4e-3 of the largest; a column sum adds at most N / 256 + 1 rows in
