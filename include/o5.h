@@ -582,6 +582,69 @@ int o5_linattn_step(o5_dtype dt, int B, int nh, int nkv, int dk, int dv,
                     size_t ldo, void* stream);
 
 /* ------------------------------------------------------------------------
+ * o5_gatedrec_fwd / _bwd / _step -- a linear recurrence of which every channel
+ * keeps as much of its state, and takes in as much, as two gates of the same
+ * step say: a recurrent core with a state of D numbers whose steps need no
+ * product with the state.  Per sample b and channel d:
+ *
+ *   log a_t = -c softplus(lam_d) sigmoid(r_t),  beta_t = sqrt(1 - a_t^2)
+ *   h_t = a_t (1 - reset[t,b]) h_{t-1} + beta_t sigmoid(i_t) x_t
+ *                                                            (h_{-1} = h0)
+ *
+ * dt       type of x, r, i, h and of dh, dx, dr, di, rounded once each; the
+ *          states and every step between are fp32.
+ * T, B     steps and samples, >= 1, T*B below 2^30.   D: channels, a multiple
+ *          of 8 in 8..65536.
+ * x, r, i  row t*B + b at x + (t*B + b)*ldx; row strides ld* in elements:
+ *          multiples of 8, at least D and below 2^31, so that x, r and i may
+ *          be parts of one wider buffer.   h: the same.
+ * lam      [D] fp32, finite (not checked).   c: > 0 and finite.
+ * h0       [B, D] fp32, the states before the first step, or NULL (= 0).
+ *          hT: out, the states after the last step, or NULL.
+ * reset    [T, B] uint8 or NULL (no resets): nonzero cuts the carried state
+ *          off before step t, whatever it held, infinities and NaN too.  A
+ *          value that is not finite reaches the later steps of its channel
+ *          up to a reset and no others (there an infinity may show as NaN).
+ * marks    out fp32, o5_gatedrec_marks_bytes(T, B, D) bytes: what
+ *          o5_gatedrec_bwd needs of the states (one in every 16 steps), or
+ *          NULL for inference.
+ * ws       scratch of o5_gatedrec_*_workspace_bytes(...) bytes.
+ *
+ * o5_gatedrec_bwd differentiates J = sum_t <dh_t, h_t> + <dhT, h_{T-1}> on
+ * the inputs and marks of a forward call:
+ *
+ *   G_t = dh_t + a_{t+1} (1 - reset[t+1,b]) G_{t+1}   (dhT joins at t = T-1)
+ *
+ * dx, dr, di  out, rows as x (and may each have its own stride).
+ * dlam     out [D] fp32, the sum over steps and samples in a fixed order.
+ * dhT, dh0 [B, D] fp32 or NULL (= 0; not wanted).
+ * Where a gate is so far closed that a_t rounds to 1 the gradients are the
+ * limits, which are 0.
+ *
+ * o5_gatedrec_step is one step (T = 1) that updates the states S [B, D] in
+ * place.
+ * ------------------------------------------------------------------------ */
+size_t o5_gatedrec_marks_bytes(int T, int B, int D);
+size_t o5_gatedrec_fwd_workspace_bytes(o5_dtype dt, int T, int B, int D);
+int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, size_t ldx,
+                    const void* r, size_t ldr, const void* i, size_t ldi,
+                    const float* lam, float c, const float* h0,
+                    const uint8_t* reset, void* h, size_t ldh, float* hT,
+                    float* marks, void* ws, size_t ws_bytes, void* stream);
+size_t o5_gatedrec_bwd_workspace_bytes(o5_dtype dt, int T, int B, int D);
+int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, size_t ldx,
+                    const void* r, size_t ldr, const void* i, size_t ldi,
+                    const float* lam, float c, const float* marks,
+                    const uint8_t* reset, const void* dh, size_t lddh,
+                    const float* dhT, void* dx, size_t lddx, void* dr,
+                    size_t lddr, void* di, size_t lddi, float* dlam, float* dh0,
+                    void* ws, size_t ws_bytes, void* stream);
+int o5_gatedrec_step(o5_dtype dt, int B, int D, const void* x, size_t ldx,
+                     const void* r, size_t ldr, const void* i, size_t ldi,
+                     const float* lam, float c, const uint8_t* reset, float* S,
+                     void* h, size_t ldh, void* stream);
+
+/* ------------------------------------------------------------------------
  * o5_resnorm_fwd / _bwd -- the RMS norms after one block and before the next
  * around a residual stream, fused with the block's gate and its residual
  * scale; one pass over the rows:

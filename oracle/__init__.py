@@ -30,6 +30,8 @@ method computes, written so that it can be checked against the paper by eye:
                 (subsection "Optimizing the Policy"; Table "Hyperparameters").
 * ``linattn`` -- linear attention with a decay for each head and resets, its
                 gradient by the adjoint recurrence.
+* ``gatedrec`` -- a linear recurrence whose decay and input are gated by the
+                input, with resets, and its gradient.
 * ``resnorm`` -- RMS norms before and after a block with its gate and residual
                 scale, forward and backward.
 * ``adamw``  -- AdamW over a tensor, its moments in 32 bits or in 8 bits with a

@@ -31,6 +31,8 @@ EXPORTED = (
     "o5_policy_sample_workspace_bytes", "o5_policy_sample", "o5_policy_sample_static",
     "o5_linattn_fwd_workspace_bytes", "o5_linattn_fwd", "o5_linattn_bwd_workspace_bytes", "o5_linattn_bwd",
     "o5_linattn_step",
+    "o5_gatedrec_marks_bytes", "o5_gatedrec_fwd_workspace_bytes", "o5_gatedrec_fwd", "o5_gatedrec_bwd_workspace_bytes",
+    "o5_gatedrec_bwd", "o5_gatedrec_step",
     "o5_resnorm_fwd", "o5_resnorm_bwd_workspace_bytes", "o5_resnorm_bwd",
     "o5_adamw_plan_bytes", "o5_adamw_plan", "o5_adamw_step", "o5_adamw_moments",
     "o5_f32_to_bf16",
@@ -142,6 +144,13 @@ _SIGS = {
     "o5_linattn_bwd": (_i, [_i] * 7 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp] + [_vp, _sz] * 3
                        + [_vp, _vp, _sz, _vp]),
     "o5_linattn_step": (_i, [_i] * 6 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp]),
+    "o5_gatedrec_marks_bytes": (_sz, [_i] * 3),
+    "o5_gatedrec_fwd_workspace_bytes": (_sz, [_i] * 4),
+    "o5_gatedrec_fwd": (_i, [_i] * 4 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz] + [_vp] * 3 + [_sz, _vp]),
+    "o5_gatedrec_bwd_workspace_bytes": (_sz, [_i] * 4),
+    "o5_gatedrec_bwd": (_i, [_i] * 4 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp] + [_vp, _sz] * 3 + [_vp] * 3
+                        + [_sz, _vp]),
+    "o5_gatedrec_step": (_i, [_i] * 3 + [_vp, _sz] * 3 + [_vp, _f] + [_vp] * 2 + [_vp, _sz, _vp]),
     "o5_resnorm_fwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 3 + [_f] + [_vp] * 5),
     "o5_resnorm_bwd_workspace_bytes": (_sz, [_i] * 4),
     "o5_resnorm_bwd": (_i, [_i] * 4 + [_vp] * 3 + [_sz] + [_vp] * 10 + [_sz] + [_vp] * 4 + [_sz, _vp]),
@@ -402,6 +411,38 @@ def o5_linattn_step(dt, B, nh, nkv, dk, dv, q, ldq, k, ldk, v, ldv, decay, scale
     _check("o5_linattn_step", lib().o5_linattn_step(
         dt, B, nh, nkv, dk, dv, _p(q), ldq, _p(k), ldk, _p(v), ldv, _p(decay), float(scale), _p(reset), _p(S),
         _p(o), ldo, _stream(stream)))
+
+
+def o5_gatedrec_marks_bytes(T, B, D):
+    return lib().o5_gatedrec_marks_bytes(T, B, D)
+
+
+def o5_gatedrec_fwd_workspace_bytes(dt, T, B, D):
+    return lib().o5_gatedrec_fwd_workspace_bytes(dt, T, B, D)
+
+
+def o5_gatedrec_fwd(dt, T, B, D, x, ldx, r, ldr, i, ldi, lam, c, h0, reset, h, ldh, hT, marks, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_gatedrec_fwd", lib().o5_gatedrec_fwd(
+        dt, T, B, D, _p(x), ldx, _p(r), ldr, _p(i), ldi, _p(lam), float(c), _p(h0), _p(reset), _p(h), ldh, _p(hT),
+        _p(marks), wp, wn, _stream(stream)))
+
+
+def o5_gatedrec_bwd_workspace_bytes(dt, T, B, D):
+    return lib().o5_gatedrec_bwd_workspace_bytes(dt, T, B, D)
+
+
+def o5_gatedrec_bwd(dt, T, B, D, x, ldx, r, ldr, i, ldi, lam, c, marks, reset, dh, lddh, dhT, dx, lddx, dr, lddr, di, lddi,
+                    dlam, dh0, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_gatedrec_bwd", lib().o5_gatedrec_bwd(
+        dt, T, B, D, _p(x), ldx, _p(r), ldr, _p(i), ldi, _p(lam), float(c), _p(marks), _p(reset), _p(dh), lddh, _p(dhT),
+        _p(dx), lddx, _p(dr), lddr, _p(di), lddi, _p(dlam), _p(dh0), wp, wn, _stream(stream)))
+
+
+def o5_gatedrec_step(dt, B, D, x, ldx, r, ldr, i, ldi, lam, c, reset, S, h, ldh, stream=None):
+    _check("o5_gatedrec_step", lib().o5_gatedrec_step(
+        dt, B, D, _p(x), ldx, _p(r), ldr, _p(i), ldi, _p(lam), float(c), _p(reset), _p(S), _p(h), ldh, _stream(stream)))
 
 
 def o5_resnorm_fwd(xt, dt, N, D, x, u, gate, ldg, w_post, rho, w_pre, eps, xo, n, r_post, r_pre, stream=None):
