@@ -361,6 +361,55 @@ int o5_ppo_loss_grad(o5_dtype dt, int N, int H, int K, const int* head_sizes,
                      void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * o5_ppo_logits_grad -- the loss of o5_ppo_loss_grad and its gradient on logits
+ * that the caller has, for heads of any width (a unit, an item or a token out of
+ * many), with a weight for each row and a penalty on the divergence from a
+ * reference policy:
+ *
+ *   p_k = softmax(z_k), q_k = softmax(ref_k), over the available logits;
+ *   logpi = sum_k m_k log p_k[a_k];  r = exp(logpi - logp_old)
+ *   L = sum_n w_n ( -min(r A, clip(r, 1-eps, 1+eps) A) + vf_coef (V - R)^2
+ *       - ent_coef sum_k m_k S(p_k) + kl_coef sum_k m_k KL(p_k || q_k) )
+ *
+ * dt       type of logits, ref and dlogits.   N: rows, 1..2^30-1.   K: heads, 1..8.
+ *          head_sizes: host [K], each >= 1, with A = their sum <= 2^24.
+ * logits   row n at logits + n*ldl: the K heads' A logits, then, where ret is
+ *          given, the value.   ref: the reference policy's A logits, rows of
+ *          stride ldr, or NULL (no divergence).   dlogits: out, dL/dlogits,
+ *          rows of stride ldd; columns from A (A + 1 with ret) on stay as they are.
+ *          Strides in elements: at least the columns, below 2^31 (any number:
+ *          no row needs an alignment).
+ * act      [N, K] int32.   logp_old, adv [N] fp32.   ret: [N] fp32, value
+ *          targets, or NULL: there is no value column and no value loss.
+ * weight   [N] fp32, or NULL: 1/N for every row.  A row of weight 0 is padding:
+ *          nothing else of it is used, and its gradient, logp and kl are 0.
+ * head_mask [N, K] and avail [N, A] uint8 or NULL, as for o5_ppo_loss_grad:
+ *          what an unavailable logit holds in logits and ref reaches nothing,
+ *          a head without an available logit above -infinity adds nothing,
+ *          and an unavailable or impossible action (not in 0 <= a < n_k) has
+ *          log-probability -inf.  A logit of -infinity has probability 0 and
+ *          adds nothing; where the reference alone excludes a choice, KL is
+ *          infinite and the row's gradient is not finite.
+ * hp, kl_coef  as above (kl_coef is not used without ref).
+ * stats    out [9] fp32: total, pg, vf, ent, clipfrac, approx_kl, ratio as for
+ *          o5_ppo_loss_grad with the weights in place of the mean, nonfinite
+ *          (the number of rows of a weight other than 0 whose loss is not
+ *          finite), kl.
+ * logp, kl out [N] fp32 = logpi and sum_k m_k KL (0 without ref), or NULL.
+ * ws       scratch of o5_ppo_logits_grad_workspace_bytes(...) bytes.
+ * ------------------------------------------------------------------------ */
+size_t o5_ppo_logits_grad_workspace_bytes(o5_dtype dt, int N, int K,
+                                          const int* head_sizes);
+int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_sizes,
+                       const void* logits, size_t ldl, const void* ref,
+                       size_t ldr, const int32_t* act, const float* logp_old,
+                       const float* adv, const float* ret, const float* weight,
+                       const uint8_t* head_mask, const uint8_t* avail,
+                       o5_ppo_hp hp, float kl_coef, float* stats, float* logp,
+                       float* kl, void* dlogits, size_t ldd, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * The heads' gradient in factored form (bf16 only; the same loss and
  * gradient as o5_ppo_loss_grad, appendix "Neural Network Architecture" and
  * subsection "Optimizing the Policy").  dL/dh is a product of a narrow
@@ -690,9 +739,10 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
                    void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
- * o5_adamw_plan / _step / _moments -- AdamW over many tensors in one launch,
- * with the per-parameter clip of o5_adam_step, decay of the weights apart from
- * the gradient, and moments in 32 bits or in 8:
+ * o5_adamw_plan / _step / _moments / _grad_norm / _step_clipped -- AdamW over
+ * many tensors in one launch, with the per-parameter clip of o5_adam_step, decay
+ * of the weights apart from the gradient, moments in 32 bits or in 8, and a clip
+ * of all gradients to a global norm:
  *
  *   v = b2 v + (1-b2) g^2;  vh = v / (1 - b2^step)
  *   g' = clamp(g, -clip_k sqrt(vh), clip_k sqrt(vh))     (clip_k <= 0: g' = g)
@@ -719,10 +769,21 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
  *
  * o5_adamw_plan  writes into `plan` (host, 16-byte aligned, bytes >=
  *          o5_adamw_plan_bytes, which is 0 for invalid tensors) what the
- *          other two calls need of count tensors (host array; 1..2^20).  The
+ *          other calls need of count tensors (host array; 1..2^20).  The
  *          caller copies those bytes to device memory once and passes both,
  *          and keeps the tensors where they are while the plan is used.
  * o5_adamw_step  one step; hp as for o5_adam_step; step >= 1.
+ * o5_adamw_grad_norm  the norm over the gradients of all of the plan's
+ *          tensors, sqrt(sum g^2) summed in 64 bits, and the factor min(1,
+ *          max_norm / norm) (max_norm > 0, infinity for the norm alone) that
+ *          clips them to max_norm: clip out [2] fp32 = (norm, factor).  The
+ *          factor is 0 where the norm is not finite, as with an infinity or a
+ *          NaN in any gradient, and positive otherwise.  The gradients stay
+ *          as they are.  ws: scratch of
+ *          o5_adamw_grad_norm_workspace_bytes(plan) bytes (0 for no plan).
+ * o5_adamw_step_clipped  o5_adamw_step on clip[1] g in place of g (clip from
+ *          device memory, as o5_adamw_grad_norm left it); where clip[1] is 0 the step
+ *          is left out: p, p_bf16 and the moments stay as they are.
  * o5_adamw_moments  the values of the moments, as a checkpoint holds them: m,
  *          v out, fp32; tensor k starts at the sum of the earlier tensors'
  *          n, each rounded up to 256 (the gaps are not written).
@@ -747,6 +808,12 @@ int o5_adamw_plan(int count, const o5_adamw_tensor* tensors, void* plan,
                   size_t bytes);
 int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp hp,
                   uint64_t seed, int step, void* stream);
+size_t o5_adamw_grad_norm_workspace_bytes(const void* plan);
+int o5_adamw_grad_norm(const void* plan, const void* plan_dev, float max_norm,
+                       float* clip, void* ws, size_t ws_bytes, void* stream);
+int o5_adamw_step_clipped(const void* plan, const void* plan_dev,
+                          o5_adam_hp hp, const float* clip, uint64_t seed,
+                          int step, void* stream);
 int o5_adamw_moments(const void* plan, const void* plan_dev, float* m,
                      float* v, void* stream);
 

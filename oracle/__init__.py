@@ -17,6 +17,8 @@ method computes, written so that it can be checked against the paper by eye:
                 and entropy bonus, with gradients (subsection "Optimizing the
                 Policy"; appendix "Exploration", subsection "Loss function";
                 appendix "Neural Network Architecture").
+* ``ppo_logits`` -- the same loss on logits, with row weights and a KL penalty
+                towards a reference policy.
 * ``prelstm`` -- the LSTM's input side: running observation normalisation,
                 the pre-LSTM fully-connected layer and the cross-hero
                 max-pool, forward and backward (appendices "Observation

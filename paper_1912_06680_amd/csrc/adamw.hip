@@ -58,6 +58,7 @@ __host__ __device__ inline const Chunk* chunks_of(const void* plan, uint32_t ten
 struct Consts {
   float lr, b1, b2, one_m_b1, one_m_b2, inv_bc1, inv_bc2, eps, clip_k;
   uint32_t key0, key1, step;
+  float scale;  // of the gradients
 };
 
 // The update of one element; m and v leave in 32 bits.  Every product and sum
@@ -217,7 +218,7 @@ __device__ __forceinline__ int count4(uint64_t n, size_t i) { return i >= n ? 0 
 
 constexpr int kRuns = kChunk / 1024;  // of four elements, for a thread
 
-template <bool kFull, typename G>
+template <bool kFull, bool kClip, typename G>
 __device__ __forceinline__ void step32(const Tensor& t, const Consts& c, size_t i0, float lr, float keep) {
   const G* gp = static_cast<const G*>(t.g);
   float *mp = static_cast<float*>(t.m), *vp = static_cast<float*>(t.v);
@@ -239,7 +240,7 @@ __device__ __forceinline__ void step32(const Tensor& t, const Consts& c, size_t 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float pj = p[k][j], mj = m[k][j], vj = v[k][j];
-      update(c, lr, keep, element(g[k], j), pj, mj, vj);
+      update(c, lr, keep, kClip ? element(g[k], j) * c.scale : element(g[k], j), pj, mj, vj);
       p[k][j] = pj, m[k][j] = mj, v[k][j] = vj;
     }
     store4<kFull>(t.p, i, n[k], p[k]);
@@ -250,7 +251,7 @@ __device__ __forceinline__ void step32(const Tensor& t, const Consts& c, size_t 
 }
 
 // A wave's run of 4 x 64 elements is one group.
-template <bool kFull, typename G>
+template <bool kFull, bool kClip, typename G>
 __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Consts& c, size_t i0, float lr, float keep) {
   const G* gp = static_cast<const G*>(t.g);
   uint8_t *mp = static_cast<uint8_t*>(t.m), *vp = static_cast<uint8_t*>(t.v);
@@ -280,7 +281,7 @@ __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Con
       float pj = p[k][j];
       m[j] = decode_m((mc[k] >> (8 * j)) & 0xff, em);
       v[j] = decode_v((vc[k] >> (8 * j)) & 0xff, ev);
-      update(c, lr, keep, element(g[k], j), pj, m[j], v[j]);
+      update(c, lr, keep, kClip ? element(g[k], j) * c.scale : element(g[k], j), pj, m[j], v[j]);
       p[k][j] = pj;
       if (j >= n[k]) m[j] = v[j] = 0.0f;
       tm = fmaxf(tm, finite(m[j]) ? fabsf(m[j]) : 0.0f);
@@ -311,8 +312,15 @@ __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Con
 // bound: 168M parameters with bf16 gradients, 8-bit moments and bf16 copies, 16
 // bytes each, 541 to 615 us, 5.0 to 4.4 TB/s; 5.3M with 32-bit moments 27 us, 5.9 TB/s
 // (partly from the caches).
+// kClip: the gradients are taken times clip[1]; where that is 0 nothing
+// changes.
+template <bool kClip>
 __global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, uint32_t first,
-                                                    Consts c) {
+                                                    Consts c, const float* __restrict__ clip) {
+  if (kClip) {
+    c.scale = clip[1];
+    if (c.scale == 0.0f) return;
+  }
   const Chunk ch = chunks_of(plan, tensors)[first + blockIdx.x];
   const Tensor t = tensors_of(plan)[ch.tensor];
   const float lr = c.lr * t.lr_scale;
@@ -321,14 +329,16 @@ __global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ pla
   const bool full = (static_cast<size_t>(ch.index) + 1) * kChunk <= t.n;
   if (t.bits == 32) {
     if (t.g_bf16)
-      full ? step32<true, uint16_t>(t, c, i, lr, keep) : step32<false, uint16_t>(t, c, i, lr, keep);
+      full ? step32<true, kClip, uint16_t>(t, c, i, lr, keep) : step32<false, kClip, uint16_t>(t, c, i, lr, keep);
     else
-      full ? step32<true, float>(t, c, i, lr, keep) : step32<false, float>(t, c, i, lr, keep);
+      full ? step32<true, kClip, float>(t, c, i, lr, keep) : step32<false, kClip, float>(t, c, i, lr, keep);
   } else {
     if (t.g_bf16)
-      full ? step8<true, uint16_t>(t, ch.tensor, c, i, lr, keep) : step8<false, uint16_t>(t, ch.tensor, c, i, lr, keep);
+      full ? step8<true, kClip, uint16_t>(t, ch.tensor, c, i, lr, keep)
+           : step8<false, kClip, uint16_t>(t, ch.tensor, c, i, lr, keep);
     else
-      full ? step8<true, float>(t, ch.tensor, c, i, lr, keep) : step8<false, float>(t, ch.tensor, c, i, lr, keep);
+      full ? step8<true, kClip, float>(t, ch.tensor, c, i, lr, keep)
+           : step8<false, kClip, float>(t, ch.tensor, c, i, lr, keep);
   }
 }
 
@@ -383,6 +393,96 @@ __global__ void __launch_bounds__(256) adamw_moments(const void* __restrict__ pl
     moments<true>(t, i, mo + t.at, vo + t.at);
   else
     moments<false>(t, i, mo + t.at, vo + t.at);
+}
+
+// ------------------------------------------------- norm of the gradients
+
+// Sums of squares are taken in 64 bits: no gradient that fp32 holds is lost in
+// them or overflows them.
+template <typename G> struct Run16;  // 16 bytes of gradients
+template <> struct Run16<float> {
+  static constexpr int kLen = 4;
+  f32x4 v;
+  __device__ __forceinline__ void load(const float* p, size_t i) { v = *reinterpret_cast<const f32x4*>(p + i); }
+  __device__ __forceinline__ float operator[](int j) const { return v[j]; }
+};
+template <> struct Run16<uint16_t> {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  static constexpr int kLen = 8;
+  u32x4 v;
+  __device__ __forceinline__ void load(const uint16_t* p, size_t i) { v = *reinterpret_cast<const u32x4*>(p + i); }
+  __device__ __forceinline__ float operator[](int j) const {
+    return __uint_as_float((j & 1) ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
+  }
+};
+
+// A thread's part of the sum of squares of the elements from i to end.
+template <typename G>
+__device__ __forceinline__ double squares(const G* g, size_t i, size_t end) {
+  constexpr int V = Run16<G>::kLen;
+  double s = 0.0;
+  for (i += threadIdx.x * V; i + V <= end; i += 256 * V) {
+    Run16<G> x;
+    x.load(g, i);
+#pragma unroll
+    for (int j = 0; j < V; ++j) s = fma(static_cast<double>(x[j]), static_cast<double>(x[j]), s);
+  }
+  for (; i < end; ++i) {  // the tensor's last elements, in one thread
+    const double x = elem<G>::to_f32(g[i]);
+    s = fma(x, x, s);
+  }
+  return s;
+}
+
+// The sum over the block in a fixed order, in thread 0.
+__device__ __forceinline__ double block_sum(double s) {
+  __shared__ double red[256];
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int w = 128; w > 0; w >>= 1) {
+    if (static_cast<int>(threadIdx.x) < w) red[threadIdx.x] += red[threadIdx.x + w];
+    __syncthreads();
+  }
+  return red[0];
+}
+
+constexpr uint32_t kNormBlocks = 2048;
+
+// A block takes its share of the chunks, which lie one after another in a
+// tensor.
+__global__ void __launch_bounds__(256) grad_squares(const void* __restrict__ plan, uint32_t tensors, uint32_t chunks,
+                                                    double* __restrict__ part) {
+  const uint32_t b = blockIdx.x, nb = gridDim.x;
+  uint32_t at = static_cast<uint32_t>(static_cast<uint64_t>(chunks) * b / nb);
+  const uint32_t to = static_cast<uint32_t>(static_cast<uint64_t>(chunks) * (b + 1) / nb);
+  double s = 0.0;
+  while (at < to) {
+    const Chunk ch = chunks_of(plan, tensors)[at];
+    const Tensor& t = tensors_of(plan)[ch.tensor];
+    const uint64_t have = (t.n + kChunk - 1) / kChunk - ch.index;
+    const uint32_t take = have < to - at ? static_cast<uint32_t>(have) : to - at;
+    const size_t i = static_cast<size_t>(ch.index) * kChunk, end = i + static_cast<size_t>(take) * kChunk;
+    const size_t stop = end < t.n ? end : t.n;
+    s += t.g_bf16 ? squares(static_cast<const uint16_t*>(t.g), i, stop) : squares(static_cast<const float*>(t.g), i, stop);
+    at += take;
+  }
+  s = block_sum(s);
+  if (threadIdx.x == 0) part[b] = s;
+}
+
+// clip: the norm, and the factor that brings the gradients down to max_norm.
+__global__ void __launch_bounds__(256) grad_norm(int n, const double* __restrict__ part, float max_norm,
+                                                 float* __restrict__ clip) {
+  double s = 0.0;
+  for (int k = threadIdx.x; k < n; k += 256) s += part[k];
+  s = block_sum(s);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    clip[0] = static_cast<float>(norm);
+    // (a factor too small for fp32 is not the 0 of a norm that is not finite)
+    const float f = norm > max_norm ? fmaxf(static_cast<float>(max_norm / norm), 0x1p-126f) : 1.0f;
+    clip[1] = norm < INFINITY ? f : 0.0f;
+  }
 }
 
 // A launch holds fewer than 2^32 threads in a dimension (with more the grid
@@ -469,8 +569,8 @@ extern "C" int o5_adamw_plan(int count, const o5_adamw_tensor* tensors, void* pl
   return O5_OK;
 }
 
-extern "C" int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp hp, uint64_t seed, int step, void* stream) {
-  const char* fn = "o5_adamw_step";
+static int adamw_run(const char* fn, const void* plan, const void* plan_dev, o5_adam_hp hp, const float* clip, uint64_t seed,
+                     int step, void* stream) {
   O5_CHECK(step >= 1, O5_E_ARG, "%s: step=%d must be >= 1", fn, step);
   O5_CHECK(hp.beta1 >= 0.0f && hp.beta1 < 1.0f && hp.beta2 >= 0.0f && hp.beta2 < 1.0f, O5_E_ARG,
            "%s: betas must lie in [0, 1)", fn);
@@ -491,9 +591,45 @@ extern "C" int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp 
   c.key0 = static_cast<uint32_t>(seed);
   c.key1 = static_cast<uint32_t>(seed >> 32);
   c.step = static_cast<uint32_t>(step);
+  c.scale = 1.0f;
   launch_chunks(h->chunks, [&](uint32_t first, uint32_t blocks) {
-    hipLaunchKernelGGL(adamw_kernel, dim3(blocks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, first, c);
+    hipLaunchKernelGGL(clip ? adamw_kernel<true> : adamw_kernel<false>, dim3(blocks), dim3(256), 0, as_stream(stream),
+                       plan_dev, h->tensors, first, c, clip);
   });
+  return check_launch(fn);
+}
+
+extern "C" int o5_adamw_step(const void* plan, const void* plan_dev, o5_adam_hp hp, uint64_t seed, int step, void* stream) {
+  return adamw_run("o5_adamw_step", plan, plan_dev, hp, nullptr, seed, step, stream);
+}
+
+extern "C" int o5_adamw_step_clipped(const void* plan, const void* plan_dev, o5_adam_hp hp, const float* clip, uint64_t seed,
+                                     int step, void* stream) {
+  O5_PTR(clip, "clip");
+  return adamw_run("o5_adamw_step_clipped", plan, plan_dev, hp, clip, seed, step, stream);
+}
+
+static uint32_t norm_blocks(const void* plan) { return std::min(static_cast<const Header*>(plan)->chunks, kNormBlocks); }
+
+extern "C" size_t o5_adamw_grad_norm_workspace_bytes(const void* plan) {
+  if (check_plan("o5_adamw_grad_norm_workspace_bytes", plan, plan) != O5_OK) return 0;
+  return norm_blocks(plan) * sizeof(double);
+}
+
+extern "C" int o5_adamw_grad_norm(const void* plan, const void* plan_dev, float max_norm, float* clip, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  const char* fn = "o5_adamw_grad_norm";
+  O5_TRY(check_plan(fn, plan, plan_dev));
+  O5_CHECK(max_norm > 0.0f, O5_E_ARG, "%s: max_norm must be positive", fn);
+  O5_PTR(clip, "clip");
+  O5_CHECK(ws != nullptr && ws_bytes >= o5_adamw_grad_norm_workspace_bytes(plan), O5_E_WORKSPACE,
+           "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
+  O5_PTR(ws, "ws");
+  const Header* h = static_cast<const Header*>(plan);
+  const uint32_t blocks = norm_blocks(plan);
+  double* part = static_cast<double*>(ws);
+  hipLaunchKernelGGL(grad_squares, dim3(blocks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, h->chunks, part);
+  hipLaunchKernelGGL(grad_norm, dim3(1), dim3(256), 0, as_stream(stream), static_cast<int>(blocks), part, max_norm, clip);
   return check_launch(fn);
 }
 

@@ -27,6 +27,7 @@ EXPORTED = (
     "o5_obs_normalize_workspace_bytes", "o5_obs_normalize", "o5_prelstm_fwd",
     "o5_prelstm_bwd_workspace_bytes", "o5_prelstm_bwd",
     "o5_ppo_loss_grad_workspace_bytes", "o5_ppo_loss_grad", "o5_ppo_head_grad_ld", "o5_ppo_loss_grad_factored",
+    "o5_ppo_logits_grad_workspace_bytes", "o5_ppo_logits_grad",
     "o5_adam_step",
     "o5_policy_sample_workspace_bytes", "o5_policy_sample", "o5_policy_sample_static",
     "o5_linattn_fwd_workspace_bytes", "o5_linattn_fwd", "o5_linattn_bwd_workspace_bytes", "o5_linattn_bwd",
@@ -35,6 +36,7 @@ EXPORTED = (
     "o5_gatedrec_bwd", "o5_gatedrec_step",
     "o5_resnorm_fwd", "o5_resnorm_bwd_workspace_bytes", "o5_resnorm_bwd",
     "o5_adamw_plan_bytes", "o5_adamw_plan", "o5_adamw_step", "o5_adamw_moments",
+    "o5_adamw_grad_norm_workspace_bytes", "o5_adamw_grad_norm", "o5_adamw_step_clipped",
     "o5_f32_to_bf16",
     "o5_param_count", "o5_surgery_widen", "o5_surgery_fold_input",
     "o5_ktimer_enable", "o5_ktimer_enable_sites", "o5_ktimer_read", "o5_ktimer_site_name",
@@ -132,6 +134,9 @@ _SIGS = {
     "o5_ppo_head_grad_ld": (_i, [_i, _i, _vp, _vp]),
     "o5_ppo_loss_grad_factored": (_i, [_i, _i, _i, _i, _vp] + [_vp] * 10 + [PpoHp] + [_vp] * 3 + [_i] + [_vp] * 3
                                   + [_sz, _vp]),
+    "o5_ppo_logits_grad_workspace_bytes": (_sz, [_i, _i, _i, _vp]),
+    "o5_ppo_logits_grad": (_i, [_i, _i, _i, _vp] + [_vp, _sz] * 2 + [_vp] * 7 + [PpoHp, _f] + [_vp] * 4
+                           + [_sz, _vp, _sz, _vp]),
     "o5_adam_step": (_i, [_sz, _vp, _vp, _vp, _vp, _vp, AdamHp, _i, _vp]),
     "o5_policy_sample_workspace_bytes": (_sz, [_i, _i, _i, _i, _vp, _vp]),
     "o5_policy_sample": (_i, [_i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp, _vp, _vp, _sz,
@@ -158,6 +163,9 @@ _SIGS = {
     "o5_adamw_plan": (_i, [_i, _vp, _vp, _sz]),
     "o5_adamw_step": (_i, [_vp, _vp, AdamHp, _u64, _i, _vp]),
     "o5_adamw_moments": (_i, [_vp] * 5),
+    "o5_adamw_grad_norm_workspace_bytes": (_sz, [_vp]),
+    "o5_adamw_grad_norm": (_i, [_vp, _vp, _f, _vp, _vp, _sz, _vp]),
+    "o5_adamw_step_clipped": (_i, [_vp, _vp, AdamHp, _vp, _u64, _i, _vp]),
     "o5_f32_to_bf16": (_i, [_sz, _vp, _vp, _vp]),
     "o5_param_count": (_sz, [_i, _i, _i]),
     "o5_surgery_widen": (_i, [_i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _u64, _vp]),
@@ -342,6 +350,20 @@ def o5_ppo_loss_grad_factored(dt, N, H, head_sizes, h, Wp, bp, act, logp_old, ad
         int(ld), _p(dWp), _p(dbp), wp, wn, _stream(stream)))
 
 
+def o5_ppo_logits_grad_workspace_bytes(dt, N, head_sizes):
+    return lib().o5_ppo_logits_grad_workspace_bytes(dt, N, len(head_sizes), _heads(head_sizes))
+
+
+def o5_ppo_logits_grad(dt, N, head_sizes, logits, ldl, ref, ldr, act, logp_old, adv, ret, weight, head_mask, avail,
+                       clip_eps, vf_coef, ent_coef, kl_coef, stats, logp, kl, dlogits, ldd, ws, stream=None):
+    wp, wn = _ws(ws)
+    hp = PpoHp(clip_eps, vf_coef, ent_coef)
+    _check("o5_ppo_logits_grad", lib().o5_ppo_logits_grad(
+        dt, N, len(head_sizes), _heads(head_sizes), _p(logits), ldl, _p(ref), ldr, _p(act), _p(logp_old), _p(adv), _p(ret),
+        _p(weight), _p(head_mask), _p(avail), hp, float(kl_coef), _p(stats), _p(logp), _p(kl), _p(dlogits), ldd, wp, wn,
+        _stream(stream)))
+
+
 def o5_adam_step(n, p, m, v, g, p_bf16, lr, beta1, beta2, eps, clip_k, step, stream=None):
     hp = AdamHp(lr, beta1, beta2, eps, clip_k)
     _check("o5_adam_step", lib().o5_adam_step(n, _p(p), _p(m), _p(v), _p(g), _p(p_bf16), hp,
@@ -483,6 +505,22 @@ def o5_adamw_step(plan, plan_dev, lr, beta1, beta2, eps, clip_k, seed, step, str
 
 def o5_adamw_moments(plan, plan_dev, m, v, stream=None):
     _check("o5_adamw_moments", lib().o5_adamw_moments(_p(plan), _p(plan_dev), _p(m), _p(v), _stream(stream)))
+
+
+def o5_adamw_grad_norm_workspace_bytes(plan):
+    return lib().o5_adamw_grad_norm_workspace_bytes(_p(plan))
+
+
+def o5_adamw_grad_norm(plan, plan_dev, max_norm, clip, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check("o5_adamw_grad_norm", lib().o5_adamw_grad_norm(_p(plan), _p(plan_dev), float(max_norm), _p(clip), wp, wn,
+                                                          _stream(stream)))
+
+
+def o5_adamw_step_clipped(plan, plan_dev, lr, beta1, beta2, eps, clip_k, clip, seed, step, stream=None):
+    hp = AdamHp(lr, beta1, beta2, eps, clip_k)
+    _check("o5_adamw_step_clipped", lib().o5_adamw_step_clipped(_p(plan), _p(plan_dev), hp, _p(clip), int(seed), int(step),
+                                                                _stream(stream)))
 
 
 def o5_f32_to_bf16(n, src, dst, stream=None):
