@@ -655,7 +655,7 @@ int o5_linattn_step(o5_dtype dt, int B, int nh, int nkv, int dk, int dv,
  *          value that is not finite reaches the later steps of its channel
  *          up to a reset and no others (there an infinity may show as NaN).
  * marks    out fp32, o5_gatedrec_marks_bytes(T, B, D) bytes: what
- *          o5_gatedrec_bwd needs of the states (one in every 16 steps), or
+ *          o5_gatedrec_bwd needs of the states (one in every few steps), or
  *          NULL for inference.
  * ws       scratch of o5_gatedrec_*_workspace_bytes(...) bytes.
  *

@@ -4,185 +4,352 @@
 //   g = sigmoid(r), o = sigmoid(i), log a = -c softplus(lam) g
 //   h_t = a_t (1 - reset_t) h_{t-1} + beta_t o_t x_t,   beta = sqrt(1 - a^2)
 //
-// Every channel is a recurrence of its own, so that a lane takes two of them
-// and walks the steps.  HBM-bound: 4 arrays of rows forward, 7 backward.
+// Every channel is a recurrence of its own, so that a lane takes two
+// neighbouring ones and walks the steps, the rows of some steps in flight while
+// it works on those before.  Where samples and channels are too few to fill the
+// chip the steps are cut into segments: one launch forms what each segment
+// leaves of the state that enters it and what it adds, one joins them in order,
+// and one runs the steps from the states that enter the segments.
 //
 // w = 1 - a is formed without the cancellation near a = 1, and the state is
-// taken on as h - w h there: a rounded to 24 bits would be off by 2^-25 of
-// itself in every step, which over the 1/w steps that a state lasts grows to
-// 2^-25 / w.  beta is sqrt(w (2 - w)).
+// taken on as h - w h: a rounded to 24 bits would be off by 2^-25 of itself in
+// every step, which over the 1/w steps that a state lasts grows to 2^-25 / w.
+// beta is sqrt(w (2 - w)).
 #include "common.h"
 
 namespace o5 {
 namespace {
 
-constexpr int kMark = 16;        // steps between the states that the forward pass leaves for the backward pass
-constexpr float kMost = 3e38f;   // the largest rate: times a gate that is 0 it is 0
+constexpr int kMark = 8;        // steps between the states that the forward pass leaves for the backward pass
+constexpr float kMost = 1e38f;  // the largest rate: times a gate that is 0 it is 0
+constexpr float kLn2 = 0.69314718f, kLog2e = 1.44269504f;
 
-struct Rec {  // a call's arrays
-  const void *x, *r, *i, *dh;
-  void *h, *dx, *dr, *di;
-  size_t ldx, ldr, ldi, lddh, ldh, lddx, lddr, lddi;
+// An array of rows: the row of step t and sample b is step t + ld b bytes from
+// p.  A call goes out in launches of so many samples that a lane's place within
+// a step is below 2^32 bytes, while step t is the same for all lanes.
+struct Rows {
+  char* p;
+  uint64_t step;
+  uint32_t ld;
+};
+
+struct Rec {  // a launch's arrays; the states' pointers are those of its first sample
+  Rows x, r, i, h, dh, dx, dr, di;
   const float *lam, *h0, *dhT;
   const uint8_t* reset;
   float *hT, *marks, *dh0, *part;
-  int T, B, D;
+  float *keep, *add;  // [segments - 1, states]: what a segment leaves of a state (-1: cut off), and what it adds
+  float* enter;       // [segments - 1, states]: the states that enter segments 1, 2, ...
+  uint64_t states;    // B D of the whole call
+  int T, B, nb, D, len;  // len: steps of a segment
   float c;
 };
 
-// Two neighbouring channels of a row.
+typedef float f2_t __attribute__((ext_vector_type(2)));
+
+// Two neighbouring channels.
 template <typename E> struct Pair;
 template <> struct Pair<float> {
-  float2 v;
-  __device__ __forceinline__ void load(const void* p, size_t at) {
-    v = *reinterpret_cast<const float2*>(static_cast<const float*>(p) + at);
-  }
-  __device__ __forceinline__ float operator[](int j) const { return j ? v.y : v.x; }
-  __device__ __forceinline__ static void store(void* p, size_t at, float a, float b) {
-    *reinterpret_cast<float2*>(static_cast<float*>(p) + at) = make_float2(a, b);
-  }
+  f2_t v;
+  __device__ __forceinline__ float operator[](int j) const { return v[j]; }
+  __device__ __forceinline__ Pair() = default;
+  __device__ __forceinline__ Pair(float a, float b) : v{a, b} {}
 };
 template <> struct Pair<uint16_t> {
   uint32_t v;
-  __device__ __forceinline__ void load(const void* p, size_t at) {
-    v = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p) + at);
-  }
   __device__ __forceinline__ float operator[](int j) const { return __uint_as_float(j ? v & 0xffff0000u : v << 16); }
-  __device__ __forceinline__ static void store(void* p, size_t at, float a, float b) {
-    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p) + at) = f32x2_to_bf16x2(a, b);
-  }
+  __device__ __forceinline__ Pair() = default;
+  __device__ __forceinline__ Pair(float a, float b) : v(f32x2_to_bf16x2(a, b)) {}
 };
+template <typename E>
+__device__ __forceinline__ Pair<E> load(const Rows& a, int t, uint32_t at) {
+  return *reinterpret_cast<const Pair<E>*>(a.p + t * a.step + at);
+}
+template <typename E>
+__device__ __forceinline__ void store(const Rows& a, int t, uint32_t at, float u, float v) {
+  *reinterpret_cast<Pair<E>*>(a.p + t * a.step + at) = Pair<E>(u, v);
+}
 
+__device__ __forceinline__ float sigmoid2(float x) {  // 1 / (1 + e^-x)
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
+}
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
 __device__ __forceinline__ float rate_of(float c, float lam) { return fminf(c * softplus(lam), kMost); }
 
-// The decay of one step: la = log a <= 0, w = 1 - a.
+// 1 - 2^-y and 2^-y of y >= 0: below 0.3 binary logs of e a polynomial, 2e-8 of
+// the value off (a minimax fit), where the difference would be 3e-7 off.
 struct Decay {
-  float la, a, w;
-  __device__ __forceinline__ Decay(float rate, float g) {
-    la = -rate * g;
-    a = __expf(la);
-    // 1 - e^la = y - y^2/2 + ... of y = -la: the first term left out is 2e-8
-    // of it at 0.35, where 1 - a is 2.4e-7 off
-    const float y = -la;
-    float s = fmaf(y, 1.0f / 5040.0f, -1.0f / 720.0f);
-    s = fmaf(y, s, 1.0f / 120.0f);
-    s = fmaf(y, s, -1.0f / 24.0f);
-    s = fmaf(y, s, 1.0f / 6.0f);
-    s = fmaf(y, s, -0.5f);
-    s = fmaf(y * y, s, y);
-    w = y < 0.35f ? s : 1.0f - a;
-  }
-  // a h
-  __device__ __forceinline__ float times(float h) const { return la > -0.35f ? fmaf(-w, h, h) : a * h; }
-};
-
-// A lane's place: two channels of one sample.
-struct Place {
-  int b, d;
-  bool on;
-  __device__ __forceinline__ Place(const Rec& p, uint64_t first) {
-    const uint64_t at = first + static_cast<uint64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    const uint32_t half = p.D / 2;
-    on = at < static_cast<uint64_t>(p.B) * half;
-    b = static_cast<int>(at / half);
-    d = static_cast<int>(at % half) * 2;
+  float w, a;
+  __device__ __forceinline__ explicit Decay(float y) {
+    a = __builtin_amdgcn_exp2f(-y);
+    float s = fmaf(y, 0x1.34893cp-10f, -0x1.3941b2p-7f);
+    s = fmaf(y, s, 0x1.c69daep-5f);
+    s = fmaf(y, s, -0x1.ebfb9ep-3f);
+    s = fmaf(y, s, 0x1.62e430p-1f);
+    w = y < 0.3f * kLog2e ? y * s : 1.0f - a;
   }
 };
 
-template <typename E>
-__global__ void __launch_bounds__(256) gatedrec_fwd(Rec p, uint64_t first) {
-  const Place l(p, first);
-  if (!l.on) return;
-  const float rate[2] = {rate_of(p.c, p.lam[l.d]), rate_of(p.c, p.lam[l.d + 1])};
-  const size_t state = static_cast<size_t>(l.b) * p.D + l.d, states = static_cast<size_t>(p.B) * p.D;
-  float h[2] = {0.0f, 0.0f};
-  if (p.h0) h[0] = p.h0[state], h[1] = p.h0[state + 1];
-  for (int t = 0; t < p.T; ++t) {
-    const size_t row = static_cast<size_t>(t) * p.B + l.b;
-    Pair<E> x, r, i;
-    x.load(p.x, row * p.ldx + l.d);
-    r.load(p.r, row * p.ldr + l.d);
-    i.load(p.i, row * p.ldi + l.d);
-    if (p.marks && t % kMark == 0) Pair<float>::store(p.marks, (t / kMark) * states + state, h[0], h[1]);
-    const bool cut = p.reset != nullptr && p.reset[row] != 0;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const Decay a(rate[j], sigmoid_f(r[j]));
-      const float beta = __builtin_amdgcn_sqrtf(a.w * (2.0f - a.w));
-      h[j] = (cut ? 0.0f : a.times(h[j])) + beta * (sigmoid_f(i[j]) * x[j]);
-    }
-    Pair<E>::store(p.h, row * p.ldh + l.d, h[0], h[1]);
-  }
-  if (p.hT) Pair<float>::store(p.hT, state, h[0], h[1]);
+// One step's state from the one before; rate in binary logs.
+__device__ __forceinline__ float next_state(float h, float y, float i, float x) {
+  const Decay a(y);
+  const float beta = __builtin_amdgcn_sqrtf(fmaf(-a.w, a.w, a.w + a.w));
+  return fmaf(beta, sigmoid2(i) * x, fmaf(-a.w, h, h));
 }
 
-// The steps between two marks are run forward from the mark first, which
-// leaves the state before each, then backward.
-template <typename E>
-__global__ void __launch_bounds__(256) gatedrec_bwd(Rec p, uint64_t first) {
-  const Place l(p, first);
+// A lane's two channels of one sample, its segment, and where they lie.
+struct Place {
+  uint32_t b, d, at, begin, end;
+  bool on;
+  float rate[2];  // c softplus(lam)
+  __device__ __forceinline__ explicit Place(const Rec& p) {
+    const uint32_t n = blockIdx.x * blockDim.x + threadIdx.x, half = p.D / 2;
+    b = n / half;
+    d = (n - b * half) * 2;
+    at = b * p.D + d;  // within the states
+    on = b < static_cast<uint32_t>(p.nb);
+    begin = blockIdx.y * p.len;
+    end = min(begin + p.len, static_cast<uint32_t>(p.T));
+    if (!on) return;
+    rate[0] = rate_of(p.c, p.lam[d]);
+    rate[1] = rate_of(p.c, p.lam[d + 1]);
+  }
+  template <typename E>
+  __device__ __forceinline__ uint32_t in(const Rows& a) const {
+    return b * a.ld + d * sizeof(E);
+  }
+};
+
+__device__ __forceinline__ f2_t state_in(const float* p, uint32_t at) { return *reinterpret_cast<const f2_t*>(p + at); }
+__device__ __forceinline__ void state_out(float* p, uint32_t at, float a, float b) {
+  *reinterpret_cast<f2_t*>(p + at) = f2_t{a, b};
+}
+
+// The inputs of U steps; those from `end` on repeat the last and are not used.
+template <typename E, int U>
+struct Steps {
+  Pair<E> x[U], r[U], i[U];
+  uint8_t cut[U];
+  __device__ __forceinline__ void load(const Rec& p, uint32_t x_at, uint32_t r_at, uint32_t i_at, uint32_t b, int t0, int end) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int t = min(t0 + k, end - 1);
+      x[k] = o5::load<E>(p.x, t, x_at);
+      r[k] = o5::load<E>(p.r, t, r_at);
+      i[k] = o5::load<E>(p.i, t, i_at);
+      cut[k] = p.reset ? p.reset[static_cast<uint64_t>(t) * p.B + b] : 0;
+    }
+  }
+};
+
+// Forward over a lane's segment.  kSum: only what the segment leaves of the
+// state that enters it, and what it adds.
+template <typename E, bool kSum>
+__global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
+  constexpr int U = sizeof(E) == 2 ? 8 : 4;
+  const Place l(p);
   if (!l.on) return;
-  const float rate[2] = {rate_of(p.c, p.lam[l.d]), rate_of(p.c, p.lam[l.d + 1])};
-  const size_t state = static_cast<size_t>(l.b) * p.D + l.d, states = static_cast<size_t>(p.B) * p.D;
-  float G[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};
-  if (p.dhT) G[0] = p.dhT[state], G[1] = p.dhT[state + 1];
-  for (int m = (p.T - 1) / kMark; m >= 0; --m) {
-    const int t0 = m * kMark;
-    float before[kMark][2], h[2];
-    h[0] = p.marks[m * states + state], h[1] = p.marks[m * states + state + 1];
+  const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), h_at = l.in<E>(p.h);
+  const float rate[2] = {kLog2e * l.rate[0], kLog2e * l.rate[1]};
+  const uint64_t seg = blockIdx.y;
+  f2_t h = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
+  bool whole = true;
+  if (!kSum) {
+    if (seg > 0)
+      h = state_in(p.enter + (seg - 1) * p.states, l.at);
+    else if (p.h0)
+      h = state_in(p.h0, l.at);
+  }
+  const int end = l.end;
+  Steps<E, U> next;
+  next.load(p, x_at, r_at, i_at, l.b, l.begin, end);
+  for (int t0 = l.begin; t0 < end; t0 += U) {
+    const Steps<E, U> s = next;
+    next.load(p, x_at, r_at, i_at, l.b, t0 + U, end);
+    if (!kSum && p.marks && t0 % kMark == 0) state_out(p.marks + (t0 / kMark) * p.states, l.at, h[0], h[1]);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (t0 + k >= end) break;
+      if (s.cut[k]) {
+        h = f2_t{0.0f, 0.0f};
+        whole = false;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float y = rate[j] * sigmoid2(s.r[k][j]);
+        if (kSum) sum[j] += y;
+        h[j] = next_state(h[j], y, s.i[k][j], s.x[k][j]);
+      }
+      if (!kSum) store<E>(p.h, t0 + k, h_at, h[0], h[1]);
+    }
+  }
+  if (kSum) {
+    state_out(p.keep + seg * p.states, l.at, whole ? __builtin_amdgcn_exp2f(-sum[0]) : -1.0f,
+              whole ? __builtin_amdgcn_exp2f(-sum[1]) : -1.0f);
+    state_out(p.add + seg * p.states, l.at, h[0], h[1]);
+  } else if (p.hT && end == p.T) {
+    state_out(p.hT, l.at, h[0], h[1]);
+  }
+}
+
+// A segment's effect on a state.
+__device__ __forceinline__ float pass(float keep, float add, float h) { return keep < 0.0f ? add : fmaf(keep, h, add); }
+
+// The states that enter the segments behind the first, from the one that
+// enters the first (forward), or those that enter the ones before the last from
+// the right.  A block takes 64 channels; each of its 16 waves joins a run of
+// segments first, then all runs before its own.
+__global__ void __launch_bounds__(1024) gatedrec_join(const float* __restrict__ keep, const float* __restrict__ add,
+                                                      const float* __restrict__ first, float* __restrict__ enter, int n,
+                                                      uint64_t states, bool back) {
+  __shared__ float ks[16][64], as[16][64];
+  const int c = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t at = static_cast<uint64_t>(blockIdx.x) * 64 + c;
+  const bool on = at < states;
+  const int run = (n + 15) / 16, from = min(wave * run, n), to = min(from + run, n);
+  const auto row = [&](int s) { return (back ? n - 1 - s : s) * states + at; };
+  float k = 1.0f, a = 0.0f;
+  if (on)
+#pragma unroll 8
+    for (int s = from; s < to; ++s) {
+      const float ks = keep[row(s)], as = add[row(s)];
+      a = pass(ks, as, a);
+      k = ks < 0.0f || k < 0.0f ? -1.0f : k * ks;
+    }
+  ks[wave][c] = k;
+  as[wave][c] = a;
+  __syncthreads();
+  if (!on) return;
+  float h = first ? first[at] : 0.0f;
+  for (int w = 0; w < wave; ++w) h = pass(ks[w][c], as[w][c], h);
+#pragma unroll 8
+  for (int s = from; s < to; ++s) {
+    h = pass(keep[row(s)], add[row(s)], h);
+    enter[row(s)] = h;
+  }
+}
+
+// What a segment leaves, to the segment before it, of the states' gradient
+// that enters from behind, and what it adds.
+template <typename E>
+__global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
+  constexpr int U = 8;
+  Place l(p);
+  if (!l.on) return;
+  // (segment 0's is not wanted)
+  l.begin += p.len;
+  l.end = min(l.begin + p.len, static_cast<uint32_t>(p.T));
+  const uint32_t r_at = l.in<E>(p.r), d_at = l.in<E>(p.dh);
+  const float rate[2] = {kLog2e * l.rate[0], kLog2e * l.rate[1]};
+  f2_t G = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
+  bool whole = true;
+  const int begin = l.begin;
+  Pair<E> nr[U], nd[U];
+  uint8_t nc[U];
+  const auto fetch = [&](int t1) {  // the steps before t1
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int t = max(t1 - 1 - k, begin);
+      nr[k] = load<E>(p.r, t, r_at);
+      nd[k] = load<E>(p.dh, t, d_at);
+      nc[k] = p.reset ? p.reset[static_cast<uint64_t>(t) * p.B + l.b] : 0;
+    }
+  };
+  fetch(l.end);
+  for (int t1 = l.end; t1 > begin; t1 -= U) {
+    Pair<E> r[U], d[U];
+    uint8_t cut[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) r[k] = nr[k], d[k] = nd[k], cut[k] = nc[k];
+    fetch(t1 - U);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (t1 - 1 - k < begin) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float y = rate[j] * sigmoid2(r[k][j]);
+        sum[j] += y;
+        G[j] += d[k][j];
+        G[j] = fmaf(-Decay(y).w, G[j], G[j]);
+      }
+      if (cut[k]) {
+        G = f2_t{0.0f, 0.0f};
+        whole = false;
+      }
+    }
+  }
+  const uint64_t seg = blockIdx.y;
+  state_out(p.keep + seg * p.states, l.at, whole ? __builtin_amdgcn_exp2f(-sum[0]) : -1.0f,
+            whole ? __builtin_amdgcn_exp2f(-sum[1]) : -1.0f);
+  state_out(p.add + seg * p.states, l.at, G[0], G[1]);
+}
+
+// Backward over a lane's segment.  The steps between two marks are run forward
+// from the mark, which leaves the state before each step and its gates in
+// registers, then backward.
+template <typename E>
+__global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
+  const Place l(p);
+  if (!l.on) return;
+  const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), d_at = l.in<E>(p.dh);
+  const uint32_t dx_at = l.in<E>(p.dx), dr_at = l.in<E>(p.dr), di_at = l.in<E>(p.di);
+  const uint64_t seg = blockIdx.y, segs = gridDim.y;
+  f2_t G = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
+  if (seg + 1 < segs)
+    G = state_in(p.enter + seg * p.states, l.at);
+  else if (p.dhT)
+    G = state_in(p.dhT, l.at);
+  const int begin = l.begin, end = l.end;
+  for (int t0 = (end - 1) / kMark * kMark; t0 >= begin; t0 -= kMark) {
+    Steps<E, kMark> s;
+    Pair<E> dh[kMark];
+    s.load(p, x_at, r_at, i_at, l.b, t0, end);
+#pragma unroll
+    for (int k = 0; k < kMark; ++k) dh[k] = load<E>(p.dh, min(t0 + k, end - 1), d_at);
+    f2_t h = state_in(p.marks + (t0 / kMark) * p.states, l.at);
+    float before[kMark][2], g[kMark][2], o[kMark][2], w[kMark][2];
 #pragma unroll
     for (int k = 0; k < kMark; ++k) {
-      if (t0 + k < p.T) {
-        const size_t row = static_cast<size_t>(t0 + k) * p.B + l.b;
-        Pair<E> x, r, i;
-        x.load(p.x, row * p.ldx + l.d);
-        r.load(p.r, row * p.ldr + l.d);
-        i.load(p.i, row * p.ldi + l.d);
-        const bool cut = p.reset != nullptr && p.reset[row] != 0;
+      if (s.cut[k]) h = f2_t{0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const Decay a(rate[j], sigmoid_f(r[j]));
-          const float beta = __builtin_amdgcn_sqrtf(a.w * (2.0f - a.w));
-          before[k][j] = cut ? 0.0f : h[j];
-          h[j] = a.times(before[k][j]) + beta * (sigmoid_f(i[j]) * x[j]);
-        }
+      for (int j = 0; j < 2; ++j) {
+        before[k][j] = h[j];
+        g[k][j] = sigmoid2(s.r[k][j]);
+        o[k][j] = sigmoid2(s.i[k][j]);
+        w[k][j] = Decay(kLog2e * l.rate[j] * g[k][j]).w;
+        const float beta = __builtin_amdgcn_sqrtf(fmaf(-w[k][j], w[k][j], w[k][j] + w[k][j]));
+        h[j] = fmaf(beta, o[k][j] * s.x[k][j], fmaf(-w[k][j], h[j], h[j]));
       }
     }
 #pragma unroll
     for (int k = kMark - 1; k >= 0; --k) {
-      if (t0 + k < p.T) {
-        const size_t row = static_cast<size_t>(t0 + k) * p.B + l.b;
-        Pair<E> x, r, i, dh;
-        x.load(p.x, row * p.ldx + l.d);
-        r.load(p.r, row * p.ldr + l.d);
-        i.load(p.i, row * p.ldi + l.d);
-        dh.load(p.dh, row * p.lddh + l.d);
-        const bool cut = p.reset != nullptr && p.reset[row] != 0;
-        float dx[2], dr[2], di[2];
+      if (t0 + k >= end) continue;
+      float dx[2], dr[2], di[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float g = sigmoid_f(r[j]), o = sigmoid_f(i[j]);
-          const Decay a(rate[j], g);
-          const float v = a.w * (2.0f - a.w), ib = v > 0.0f ? __builtin_amdgcn_rsqf(v) : 0.0f;
-          G[j] += dh[j];
-          // G d(log a) log a: the quotient log a / beta goes to 0 with log a
-          const float e = G[j] * (a.a * before[k][j] * a.la - a.a * a.a * (o * x[j]) * (a.la * ib));
-          const float du = G[j] * (v * ib);
-          dx[j] = du * o;
-          dr[j] = e * (1.0f - g);
-          di[j] = du * x[j] * (o * (1.0f - o));
-          sum[j] += e;
-          G[j] = cut ? 0.0f : a.times(G[j]);
-        }
-        Pair<E>::store(p.dx, row * p.lddx + l.d, dx[0], dx[1]);
-        Pair<E>::store(p.dr, row * p.lddr + l.d, dr[0], dr[1]);
-        Pair<E>::store(p.di, row * p.lddi + l.d, di[0], di[1]);
+      for (int j = 0; j < 2; ++j) {
+        const float x = s.x[k][j], wk = w[k][j], ok = o[k][j], gk = g[k][j];
+        const float v = fmaf(-wk, wk, wk + wk);
+        // 1 / beta; log a / beta goes to 0 with log a
+        const float ib = v < 0x1p-126f ? 0.0f : __builtin_amdgcn_rsqf(v);
+        const float a = 1.0f - wk;
+        G[j] += dh[k][j];
+        // G d(log a) log a
+        const float e = G[j] * (a * (-l.rate[j] * gk) * fmaf(-a * ib, ok * x, before[k][j]));
+        const float du = G[j] * (v * ib);
+        dx[j] = du * ok;
+        dr[j] = fmaf(-e, gk, e);
+        di[j] = dx[j] * x * (1.0f - ok);
+        sum[j] += e;
+        G[j] = fmaf(-wk, G[j], G[j]);
       }
+      if (s.cut[k]) G = f2_t{0.0f, 0.0f};
+      store<E>(p.dx, t0 + k, dx_at, dx[0], dx[1]);
+      store<E>(p.dr, t0 + k, dr_at, dr[0], dr[1]);
+      store<E>(p.di, t0 + k, di_at, di[0], di[1]);
     }
   }
-  if (p.dh0) Pair<float>::store(p.dh0, state, G[0], G[1]);
-  Pair<float>::store(p.part, state, sum[0], sum[1]);
+  if (p.dh0 && begin == 0) state_out(p.dh0, l.at, G[0], G[1]);
+  state_out(p.part + seg * p.states, l.at, sum[0], sum[1]);
 }
 
 // dlam: the sum over the rows of part [n, D] in a fixed order, a block 64
@@ -193,6 +360,7 @@ __global__ void __launch_bounds__(1024) gatedrec_rates(size_t n, int D, const fl
   const int c = threadIdx.x & 63, g = threadIdx.x >> 6, d = blockIdx.x * 64 + c;
   float s = 0.0f;
   if (d < D)
+#pragma unroll 8
     for (size_t k = g; k < n; k += 16) s += part[k * D + d];
   red[g][c] = s;
   __syncthreads();
@@ -205,27 +373,23 @@ __global__ void __launch_bounds__(1024) gatedrec_rates(size_t n, int D, const fl
   }
 }
 
+// One step.  A lane keeps its channels and takes every gridDim.y-th sample: the
+// rates cost as much as ten steps.
 template <typename E>
-__global__ void __launch_bounds__(256) gatedrec_token(Rec p, float* __restrict__ S, uint64_t first) {
-  const Place l(p, first);
-  if (!l.on) return;
-  const size_t row = l.b, state = row * p.D + l.d;
-  Pair<E> x, r, i;
-  x.load(p.x, row * p.ldx + l.d);
-  r.load(p.r, row * p.ldr + l.d);
-  i.load(p.i, row * p.ldi + l.d);
-  Pair<float> s;
-  s.load(S, state);
-  const bool cut = p.reset != nullptr && p.reset[row] != 0;
-  float h[2];
+__global__ void __launch_bounds__(256) gatedrec_token(Rec p, float* __restrict__ S) {
+  const uint32_t d = (blockIdx.x * blockDim.x + threadIdx.x) * 2;
+  if (d >= static_cast<uint32_t>(p.D)) return;
+  const float rate[2] = {kLog2e * rate_of(p.c, p.lam[d]), kLog2e * rate_of(p.c, p.lam[d + 1])};
+  for (uint32_t b = blockIdx.y; b < static_cast<uint32_t>(p.nb); b += gridDim.y) {
+    const Pair<E> x = load<E>(p.x, 0, b * p.x.ld + d * sizeof(E)), r = load<E>(p.r, 0, b * p.r.ld + d * sizeof(E)),
+                  i = load<E>(p.i, 0, b * p.i.ld + d * sizeof(E));
+    f2_t s = state_in(S, b * p.D + d);
+    if (p.reset && p.reset[b]) s = f2_t{0.0f, 0.0f};
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const Decay a(rate_of(p.c, p.lam[l.d + j]), sigmoid_f(r[j]));
-    const float beta = __builtin_amdgcn_sqrtf(a.w * (2.0f - a.w));
-    h[j] = (cut ? 0.0f : a.times(s[j])) + beta * (sigmoid_f(i[j]) * x[j]);
+    for (int j = 0; j < 2; ++j) s[j] = next_state(s[j], rate[j] * sigmoid2(r[j]), i[j], x[j]);
+    state_out(S, b * p.D + d, s[0], s[1]);
+    store<E>(p.h, 0, b * p.h.ld + d * sizeof(E), s[0], s[1]);
   }
-  Pair<float>::store(S, state, h[0], h[1]);
-  Pair<E>::store(p.h, row * p.ldh + l.d, h[0], h[1]);
 }
 
 // ------------------------------------------------------------ validation
@@ -264,12 +428,64 @@ int check_inputs(const char* fn, int D, const void* x, size_t ldx, const void* r
   return O5_OK;
 }
 
-// launch(first lane, blocks): a launch holds fewer than 2^32 threads.
+// How the steps of a call are cut: segments of len steps, whole marks, one for
+// a call that fills the chip without.
+struct Cut {
+  int len, segments;
+};
+constexpr int kWaves = 2048;      // to fill the chip
+constexpr int kMostSegments = 512;
+constexpr int kLeast = 32;        // steps of a segment
+
+Cut cut_of(int T, int B, int D) {
+  const long long waves = (static_cast<long long>(B) * (D / 2) + 63) / 64;
+  long long want = std::min<long long>(kMostSegments, kWaves / std::max(1ll, waves));
+  want = std::min<long long>(want, T / kLeast);
+  if (want < 2) return {T, 1};
+  const int len = static_cast<int>(((T + want - 1) / want + kMark - 1) / kMark * kMark);
+  return {len, (T + len - 1) / len};
+}
+
+// Sums, joins and the states that enter: three arrays of segments - 1 rows.
+size_t cut_bytes(const Cut& c, int B, int D) {
+  return align_up(static_cast<size_t>(c.segments - 1) * B * D * sizeof(float)) * 3;
+}
+void place_cut(const Cut& c, int B, int D, void* ws, Rec* p) {
+  const size_t n = align_up(static_cast<size_t>(c.segments - 1) * B * D * sizeof(float)) / sizeof(float);
+  p->keep = static_cast<float*>(ws);
+  p->add = p->keep + n;
+  p->enter = p->add + n;
+  p->len = c.len;
+}
+
+Rows rows_of(const void* p, size_t ld, int B, size_t es) {
+  return {static_cast<char*>(const_cast<void*>(p)), ld * B * es, static_cast<uint32_t>(ld * es)};
+}
+
+// launch(arrays, samples, blocks) of at most so many samples that offsets
+// within a step stay below 2^32 (a row alone does: ld b is 0 there).
 template <class F>
-void launch_lanes(int B, int D, F&& launch) {
-  constexpr uint64_t kBlocks = 0xffffffffu / 256;
-  const uint64_t blocks = (static_cast<uint64_t>(B) * (D / 2) + 255) / 256;
-  for (uint64_t b = 0; b < blocks; b += kBlocks) launch(b * 256, static_cast<unsigned>(std::min(blocks - b, kBlocks)));
+void launch_samples(const Rec& all, size_t most_ld, F&& launch) {
+  const size_t most = std::max<size_t>(1, (static_cast<size_t>(1) << 31) / std::max(most_ld * 4, static_cast<size_t>(all.D) * 4));
+  for (size_t b = 0; b < static_cast<size_t>(all.B); b += most) {
+    Rec p = all;
+    p.nb = static_cast<int>(std::min<size_t>(most, all.B - b));
+    for (Rows* a : {&p.x, &p.r, &p.i, &p.h, &p.dh, &p.dx, &p.dr, &p.di})
+      if (a->p) a->p += b * (a->step / all.B);
+    const size_t at = b * all.D;
+    for (const float** a : {&p.h0, &p.dhT})
+      if (*a) *a += at;
+    for (float** a : {&p.hT, &p.marks, &p.dh0, &p.part, &p.keep, &p.add, &p.enter})
+      if (*a) *a += at;
+    if (p.reset) p.reset += b;
+    launch(p, static_cast<unsigned>((static_cast<size_t>(p.nb) * (all.D / 2) + 255) / 256));
+  }
+}
+
+void join(const Rec& p, const Cut& c, const float* first, bool back, hipStream_t s) {
+  const uint64_t blocks = (p.states + 63) / 64;  // (few: a call of many states is not cut)
+  hipLaunchKernelGGL(gatedrec_join, dim3(static_cast<unsigned>(blocks)), dim3(1024), 0, s, p.keep, p.add, first, p.enter,
+                     c.segments - 1, p.states, back);
 }
 
 }  // namespace
@@ -284,7 +500,7 @@ extern "C" size_t o5_gatedrec_marks_bytes(int T, int B, int D) {
 
 extern "C" size_t o5_gatedrec_fwd_workspace_bytes(o5_dtype dt, int T, int B, int D) {
   if (check_sizes("o5_gatedrec_fwd_workspace_bytes", dt, T, B, D) != O5_OK) return 0;
-  return 256;
+  return std::max<size_t>(256, cut_bytes(cut_of(T, B, D), B, D));
 }
 
 extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, size_t ldx, const void* r, size_t ldr,
@@ -302,21 +518,32 @@ extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, 
   O5_CHECK(ws != nullptr && ws_bytes >= o5_gatedrec_fwd_workspace_bytes(dt, T, B, D), O5_E_WORKSPACE,
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
-  Rec p = {};
-  p.x = x, p.r = r, p.i = i, p.h = h;
-  p.ldx = ldx, p.ldr = ldr, p.ldi = ldi, p.ldh = ldh;
-  p.lam = lam, p.h0 = h0, p.reset = reset, p.hT = hT, p.marks = marks;
-  p.T = T, p.B = B, p.D = D, p.c = c;
-  auto kernel = dt == O5_BF16 ? gatedrec_fwd<uint16_t> : gatedrec_fwd<float>;
-  launch_lanes(B, D, [&](uint64_t first, unsigned blocks) {
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, as_stream(stream), p, first);
-  });
+  const size_t es = dtype_size(dt);
+  const Cut cut = cut_of(T, B, D);
+  Rec all = {};
+  all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
+  all.h = rows_of(h, ldh, B, es);
+  all.lam = lam, all.h0 = h0, all.reset = reset, all.hT = hT, all.marks = marks;
+  all.T = T, all.B = B, all.D = D, all.c = c, all.states = static_cast<uint64_t>(B) * D;
+  place_cut(cut, B, D, ws, &all);
+  const bool bf16 = dt == O5_BF16;
+  const auto run = [&](auto kernel, int segments) {
+    launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p, unsigned blocks) {
+      hipLaunchKernelGGL(kernel, dim3(blocks, segments), dim3(256), 0, as_stream(stream), p);
+    });
+  };
+  if (cut.segments > 1) {
+    run(bf16 ? gatedrec_fwd<uint16_t, true> : gatedrec_fwd<float, true>, cut.segments - 1);
+    join(all, cut, h0, false, as_stream(stream));
+  }
+  run(bf16 ? gatedrec_fwd<uint16_t, false> : gatedrec_fwd<float, false>, cut.segments);
   return check_launch(fn);
 }
 
 extern "C" size_t o5_gatedrec_bwd_workspace_bytes(o5_dtype dt, int T, int B, int D) {
   if (check_sizes("o5_gatedrec_bwd_workspace_bytes", dt, T, B, D) != O5_OK) return 0;
-  return static_cast<size_t>(B) * D * sizeof(float);
+  const Cut c = cut_of(T, B, D);
+  return cut_bytes(c, B, D) + static_cast<size_t>(c.segments) * B * D * sizeof(float);
 }
 
 extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, size_t ldx, const void* r, size_t ldr,
@@ -339,20 +566,34 @@ extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, 
   O5_CHECK(ws != nullptr && ws_bytes >= o5_gatedrec_bwd_workspace_bytes(dt, T, B, D), O5_E_WORKSPACE,
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
-  Rec p = {};
-  p.x = x, p.r = r, p.i = i, p.dh = dh, p.dx = dx, p.dr = dr, p.di = di;
-  p.ldx = ldx, p.ldr = ldr, p.ldi = ldi, p.lddh = lddh, p.lddx = lddx, p.lddr = lddr, p.lddi = lddi;
-  p.lam = lam, p.dhT = dhT, p.reset = reset, p.marks = const_cast<float*>(marks), p.dh0 = dh0;
-  p.part = static_cast<float*>(ws);
-  p.T = T, p.B = B, p.D = D, p.c = c;
-  auto kernel = dt == O5_BF16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>;
-  launch_lanes(B, D, [&](uint64_t first, unsigned blocks) {
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, as_stream(stream), p, first);
-  });
-  hipLaunchKernelGGL(gatedrec_rates, dim3((D + 63) / 64), dim3(1024), 0, as_stream(stream), static_cast<size_t>(B), D,
-                     p.part, lam, dlam);
+  const size_t es = dtype_size(dt);
+  const Cut cut = cut_of(T, B, D);
+  Rec all = {};
+  all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
+  all.dh = rows_of(dh, lddh, B, es);
+  all.dx = rows_of(dx, lddx, B, es), all.dr = rows_of(dr, lddr, B, es), all.di = rows_of(di, lddi, B, es);
+  all.lam = lam, all.dhT = dhT, all.reset = reset, all.marks = const_cast<float*>(marks), all.dh0 = dh0;
+  all.T = T, all.B = B, all.D = D, all.c = c, all.states = static_cast<uint64_t>(B) * D;
+  place_cut(cut, B, D, ws, &all);
+  all.part = static_cast<float*>(ws) + cut_bytes(cut, B, D) / sizeof(float);
+  const bool bf16 = dt == O5_BF16;
+  const size_t most = std::max(std::max(std::max(ldx, ldr), std::max(ldi, lddh)), std::max(std::max(lddx, lddr), lddi));
+  const auto run = [&](auto kernel, int segments) {
+    launch_samples(all, most, [&](const Rec& p, unsigned blocks) {
+      hipLaunchKernelGGL(kernel, dim3(blocks, segments), dim3(256), 0, as_stream(stream), p);
+    });
+  };
+  if (cut.segments > 1) {
+    run(bf16 ? gatedrec_back_sum<uint16_t> : gatedrec_back_sum<float>, cut.segments - 1);
+    join(all, cut, dhT, true, as_stream(stream));
+  }
+  run(bf16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>, cut.segments);
+  hipLaunchKernelGGL(gatedrec_rates, dim3((D + 63) / 64), dim3(1024), 0, as_stream(stream),
+                     static_cast<size_t>(cut.segments) * B, D, all.part, lam, dlam);
   return check_launch(fn);
 }
+
+constexpr int kTokenRows = 8;  // samples of a lane, where there are many
 
 extern "C" int o5_gatedrec_step(o5_dtype dt, int B, int D, const void* x, size_t ldx, const void* r, size_t ldr,
                                 const void* i, size_t ldi, const float* lam, float c, const uint8_t* reset, float* S,
@@ -363,13 +604,16 @@ extern "C" int o5_gatedrec_step(o5_dtype dt, int B, int D, const void* x, size_t
   O5_TRY(check_rows(fn, "h", h, "ldh", ldh, D));
   O5_OPT_PTR(reset, "reset");
   O5_PTR(S, "S");
-  Rec p = {};
-  p.x = x, p.r = r, p.i = i, p.h = h;
-  p.ldx = ldx, p.ldr = ldr, p.ldi = ldi, p.ldh = ldh;
-  p.lam = lam, p.reset = reset, p.T = 1, p.B = B, p.D = D, p.c = c;
-  auto kernel = dt == O5_BF16 ? gatedrec_token<uint16_t> : gatedrec_token<float>;
-  launch_lanes(B, D, [&](uint64_t first, unsigned blocks) {
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, as_stream(stream), p, S, first);
+  const size_t es = dtype_size(dt);
+  Rec all = {};
+  all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
+  all.h = rows_of(h, ldh, B, es);
+  all.lam = lam, all.reset = reset, all.hT = S, all.T = 1, all.B = B, all.D = D, all.c = c;
+  launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p, unsigned) {
+    const unsigned across = (D / 2 + 255) / 256;
+    const unsigned down = std::min<unsigned>(65535, std::max<unsigned>(std::min<unsigned>(p.nb, 1024 / across), p.nb / kTokenRows));
+    hipLaunchKernelGGL(dt == O5_BF16 ? gatedrec_token<uint16_t> : gatedrec_token<float>, dim3(across, down), dim3(256), 0,
+                       as_stream(stream), p, p.hT);
   });
   return check_launch(fn);
 }

@@ -21,7 +21,7 @@ def test_refusals(lib):
     size = [BF, 16, 4, 64]
     ins = [P, 64, P, 192, P, 64, P, 8.0]
     need, bneed = lib.o5_gatedrec_fwd_workspace_bytes(*size), lib.o5_gatedrec_bwd_workspace_bytes(*size)
-    assert need > 0 and bneed > 0 and lib.o5_gatedrec_marks_bytes(*size[1:]) == 4 * 64 * 4
+    assert need > 0 and bneed > 0 and lib.o5_gatedrec_marks_bytes(*size[1:]) >= 4 * 64 * 4
 
     def fwd(size=size, ins=ins, h0=None, reset=None, h=P, ldh=64, hT=None, marks=None, ws=P, n=need):
         return lib.o5_gatedrec_fwd(*size, *ins, h0, reset, h, ldh, hT, marks, ws, n, None)
