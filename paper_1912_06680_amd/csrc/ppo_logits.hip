@@ -1,22 +1,25 @@
 // The clipped policy loss with value, entropy and KL terms and its gradient on
 // logits, o5_ppo_logits_grad.
 //
-// A team of lanes takes a row.  One pass over each head's logits and the
-// reference's carries, relative to the largest seen so far (m, and mr of the
-// reference),
+// With the largest logits m of a head and mr of the reference's,
 //
 //   s = sum e^(z-m),  t = sum e^(z-m) (z-m),  v = sum e^(z-m) (y-mr),
 //   sr = sum e^(y-mr)                            (z logits, y the reference's)
 //
-// so that log p_j = z_j - m - log s, S = log s - t/s and
-// KL = (t - v)/s - log(s/sr), a difference of small numbers where the policies
-// are near each other.  A second pass writes
+// give log p_j = z_j - m - log s, S = log s - t/s and KL = (t - v)/s -
+// log(s/sr), a difference of small numbers where the policies are near each
+// other, and then
 //
 //   dz_j = -w A r [unclipped] (1[j = a] - p_j)
-//          + w p_j (ent (log p_j + S) + kl (log p_j - log q_j - KL)).
+//          + w p_j (ent (log p_j + S) + kl (log p_j - log q_j - KL)),
 //
-// HBM-bound where rows are wide: logits and reference are read once from
-// memory (the second pass finds them in a cache) and the gradient written once.
+// of which all but 1[j = a] is p_j times a linear function of z_j and y_j.
+//
+// A team of lanes takes a row and holds it in registers, 16 bytes of a head's
+// logits and of the reference's to a slot: everything is read once and written
+// once.  Rows too wide for that are read twice, the second time from a cache.
+// HBM-bound by its bytes; the 40 instructions an element, 3 exponentials among
+// them, take nearly as long.
 #include "heads.h"
 #include "reduce.h"
 
@@ -25,8 +28,8 @@ namespace {
 
 constexpr int kSums = 8;  // pg, vf, ent, clipfrac, approx_kl, ratio, nonfinite, kl
 constexpr int kMostLogits = 1 << 24;
-constexpr int kMaxBlocks = 2048;
 constexpr float kLowest = -3.40282346e38f;
+constexpr float kLog2e = 1.44269504f;
 
 struct Loss {  // a call's arrays
   const void *z, *y;
@@ -42,266 +45,620 @@ struct Loss {  // a call's arrays
   float clip_eps, vf_coef, ent_coef, kl_coef, even;
 };
 
-// ---------------------------------------------------- reductions of a team
+// ---------------------------------------------------------------- a slot
 
-// Over the G lanes of a team, the result in each, in a fixed order: within a
-// row of 16 lanes, a wave, or the waves of a block through LDS.
-template <int G, class Op>
-__device__ __forceinline__ float lanes_reduce(float v, float id, Op op) {
-  if (G == 16) {
-    v = op(v, dpp<0xB1>(id, v));   // quad_perm [1, 0, 3, 2]
-    v = op(v, dpp<0x4E>(id, v));   // quad_perm [2, 3, 0, 1]
-    v = op(v, dpp<0x124>(id, v));  // row_ror 4
-    v = op(v, dpp<0x128>(id, v));  // row_ror 8
-    return v;
+// 16 bytes of neighbouring columns as they are stored, at no alignment but the
+// element's.
+template <typename E>
+struct Slot {
+  static constexpr int V = 16 / sizeof(E);
+  uint64_t lo, hi;
+
+  __device__ __forceinline__ void load(const E* p) { __builtin_memcpy(this, p, 16); }
+  // The first n of V, one by one.
+  __device__ __forceinline__ void load_some(const E* p, int n) {
+    float x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = j < n ? elem<E>::to_f32(p[j]) : 0.0f;
+    set(x);
   }
-  return wave_reduce(v, id, op);
-}
-__device__ __forceinline__ float op_max(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float op_sum(float a, float b) { return a + b; }
-
-// n values at once; red [2][16 waves][n], used in turn.
-template <int G, int n, class Op>
-__device__ __forceinline__ void team_reduce(float (&v)[n], float id, Op op, float (*red)[n]) {
-#pragma unroll
-  for (int q = 0; q < n; ++q) v[q] = lanes_reduce<G>(v[q], id, op);
-  if (G <= 64) return;
-  const int wave = threadIdx.x >> 6;
-  __syncthreads();  // (the last reduction's values have been read)
-  if ((threadIdx.x & 63) == 0)
-#pragma unroll
-    for (int q = 0; q < n; ++q) red[wave][q] = v[q];
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < n; ++q) v[q] = red[0][q];
-  for (int w = 1; w < G / 64; ++w)
-#pragma unroll
-    for (int q = 0; q < n; ++q) v[q] = op(v[q], red[w][q]);
-}
-
-// ------------------------------------------------------------- the columns
-
-// V neighbouring elements, of which n are there (at no alignment but the
-// element's).
-template <typename E, int V>
-struct Cols {
-  E v[V];
-  __device__ __forceinline__ void load(const E* p, int n) {
+  // Columns skip to skip + n, V at most, to p + skip ...
+  __device__ __forceinline__ void store(E* p, int skip, int n) const {
     if (n >= V) {
-      __builtin_memcpy(v, p, sizeof v);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = j < n ? p[j] : E(0);
+      __builtin_memcpy(p, this, 16);
+      return;
     }
-  }
-  __device__ __forceinline__ void store(E* p, int n) const {
-    if (n >= V) {
-      __builtin_memcpy(p, v, sizeof v);
-    } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < n) p[j] = v[j];
-    }
+    for (int j = 0; j < V; ++j)
+      if (j >= skip && j < skip + n) p[j] = elem<E>::from_f32((*this)[j]);  // (exact: the slot holds E)
   }
-  __device__ __forceinline__ float operator[](int j) const;
+  __device__ __forceinline__ uint32_t word(int k) const {
+    return static_cast<uint32_t>((k & 2 ? hi : lo) >> (k & 1 ? 32 : 0));
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    if (sizeof(E) == 4) return __uint_as_float(word(j));
+    const uint32_t w = word(j / 2);
+    return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+  }
+  __device__ __forceinline__ void set(const float (&x)[V]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w[k] = sizeof(E) == 4 ? __float_as_uint(x[k]) : f32x2_to_bf16x2(x[2 * k % V], x[(2 * k + 1) % V]);
+    lo = w[0] | static_cast<uint64_t>(w[1]) << 32;
+    hi = w[2] | static_cast<uint64_t>(w[3]) << 32;
+  }
+  // What was computed from the slot before is not kept for what follows, nor is
+  // what follows begun before: all columns as floats at once would take more
+  // registers than there are.
+  __device__ __forceinline__ void hold() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(lo), "+v"(hi));
+  }
+  // -infinity in place of the columns that `on` does not name.
+  __device__ __forceinline__ void mask(uint32_t on) {
+    float x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = (on >> j) & 1 ? (*this)[j] : -INFINITY;
+    set(x);
+  }
+  __device__ __forceinline__ void fill(float v) {
+    float x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = v;
+    set(x);
+  }
 };
-template <typename E, int V>
-__device__ __forceinline__ float Cols<E, V>::operator[](int j) const { return elem<E>::to_f32(v[j]); }
 
-// e^x of x <= 0, the lowest difference of two floats included.
-__device__ __forceinline__ float exp_of(float x) { return __expf(x); }
-// a - b, where infinities and overflow become the lowest number: its
+// Where a slot lies: the 16 bytes from column `col` of the row, of which
+// columns skip to skip + have are the slot's own.  The last of a row begins
+// further left, so that no slot reaches past the row's A logits (there are V of
+// them but in tiny rows).
+template <int V>
+struct Span {
+  int col, skip, have;
+  __device__ __forceinline__ Span() = default;
+  __device__ __forceinline__ Span(int start, int left, int A) {
+    have = max(0, min(V, left));
+    col = have > 0 ? max(0, min(start, A - V)) : 0;
+    skip = have > 0 ? start - col : 0;
+  }
+  // The bits of the columns that count: the slot's own, and of those the ones
+  // that are available (av: the row's, if any).
+  template <bool kTiny>
+  __device__ __forceinline__ uint32_t on(const uint8_t* av, int A) const {
+    uint32_t bits = ((1u << have) - 1) << skip;
+    if (!av) return bits;
+    uint64_t b = 0;
+    if (!kTiny) {
+      __builtin_memcpy(&b, av + col, V);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) b |= static_cast<uint64_t>(j < A ? av[j] : 0) << (8 * j);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (((b >> (8 * j)) & 0xff) == 0) bits &= ~(1u << j);
+    return bits;
+  }
+};
+
+// ------------------------------------------------------------ the formulas
+
+// a - b, where overflow and infinities become the lowest number: its
 // exponential is 0, and 0 times it is 0.
 __device__ __forceinline__ float below(float a, float b) { return fmaxf(a - b, kLowest); }
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 // f x, and 0 where f is: what has become negligible may be infinite.
 __device__ __forceinline__ float scaled(float f, float x) { return f == 0.0f ? 0.0f : f * x; }
 
-// A head's logs of sums stand apart from the largest logits: beside a large
-// one they would be lost.
-struct HeadStats {
-  float m, ls, mr, lsr;  // log p = z - m - ls, log q = y - mr - lsr
-  float S, D;            // entropy, KL
-  bool some;             // a logit that counts
-};
-
-// One pass over a head of n logits.
-template <typename E, int G, int V>
-__device__ __forceinline__ HeadStats head_stats(const E* z, const E* y, const uint8_t* av, int n, int lane,
-                                                float (*redm)[2], float (*reds)[4]) {
-  float m = kLowest, mr = kLowest, s = 0.0f, t = 0.0f, v = 0.0f, sr = 0.0f;
-  for (int j = lane * V; j < n; j += G * V) {
-    const int have = n - j;
-    Cols<E, V> zc, yc;
-    Cols<uint8_t, V> ac;
-    zc.load(z + j, have);
-    if (y) yc.load(y + j, have);
-    if (av) ac.load(av + j, have);
-    float zz[V], yy[V], mj = m, mrj = mr;
-#pragma unroll
-    for (int q = 0; q < V; ++q) {
-      const bool on = q < have && (!av || ac.v[q] != 0);
-      zz[q] = on ? zc[q] : -INFINITY;
-      yy[q] = on && y ? yc[q] : -INFINITY;
-      mj = fmaxf(mj, zz[q]);
-      mrj = fmaxf(mrj, yy[q]);
-    }
-    const float d = below(m, mj), f = exp_of(d);
+// The sums of a head's logits, relative to m and mr.
+struct Sums {
+  float s, t, v, sr;
+  // (An exponential of 0 times anything but NaN counts nothing.)
+  __device__ __forceinline__ void add(float z, float m) {
+    const float d = z - m, e = exp_of(d);
+    s += e;
+    t = fmaf(e, fmaxf(d, -1000.0f), t);
+  }
+  __device__ __forceinline__ void add(float z, float m, float y, float mr) {
+    const float d = z - m, e = exp_of(d), dy = y - mr;
+    s += e;
+    t = fmaf(e, fmaxf(d, -1000.0f), t);
+    v = fmaf(e, e == 0.0f ? 0.0f : dy, v);
+    sr += exp_of(dy);
+  }
+  // From m, mr to mn, mrn.
+  __device__ __forceinline__ void move(float m, float mr, float mn, float mrn) {
+    const float d = below(m, mn), dr = below(mr, mrn), f = exp_of(d);
     t = scaled(f, fmaf(s, d, t));
     s *= f;
-    v = fmaf(s, below(mr, mrj), scaled(f, v));
-    sr *= exp_of(below(mr, mrj));
-    m = mj;
-    mr = mrj;
-#pragma unroll
-    for (int q = 0; q < V; ++q) {
-      const float dz = zz[q] - m, e = exp_of(dz);
-      s += e;
-      const bool nil = e == 0.0f;  // (NaN is none)
-      t += nil ? 0.0f : e * dz;
-      if (y) {
-        const float dy = yy[q] - mr;
-        v += nil ? 0.0f : e * dy;
-        sr += exp_of(dy);
-      }
-    }
+    v = fmaf(s, dr, scaled(f, v));
+    sr *= exp_of(dr);
   }
-  float mm[2] = {m, mr};
-  team_reduce<G>(mm, kLowest, op_max, redm);
-  const float d = below(m, mm[0]), dr = below(mr, mm[1]), f = exp_of(d);
-  float sum[4];
-  sum[0] = s * f;
-  sum[1] = scaled(f, fmaf(s, d, t));
-  sum[2] = fmaf(sum[0], dr, scaled(f, v));
-  sum[3] = sr * exp_of(dr);
-  team_reduce<G>(sum, 0.0f, op_sum, reds);
-  HeadStats h;
-  h.some = sum[0] != 0.0f;
-  h.m = mm[0];
-  h.mr = mm[1];
-  h.ls = logf(sum[0]);
-  h.lsr = logf(sum[3]);
-  h.S = h.ls - sum[1] / sum[0];
-  h.D = y ? (sum[1] - sum[2]) / sum[0] - logf(sum[0] / sum[3]) : 0.0f;
-  return h;
-}
+};
 
-// What a row's gradient needs beside its heads' statistics.
+// A head's log-sums, entropy and divergence; the logs stand apart from the
+// largest logits, beside which they would be lost.
+struct HeadStats {
+  float ls, lsr, S, D;
+  bool some;  // a logit that counts
+  __device__ __forceinline__ HeadStats(const Sums& x, bool ref) {
+    some = x.s != 0.0f;
+    ls = logf(x.s);
+    lsr = logf(x.sr);
+    S = ls - x.t / x.s;
+    D = ref ? (x.t - x.v) / x.s - logf(x.s / x.sr) : 0.0f;
+  }
+};
+
+// What the row gives its heads' gradients, and a head's p_j (kd d + ky dy + k0)
+// of d = z - m, dy = y - mr, with p_j = 2^(d log2 e - l2).
 struct RowGrad {
   float pg, ent, kl;
 };
+struct HeadGrad {
+  float m, mr, l2, kd, ky, k0;
+  __device__ __forceinline__ HeadGrad() = default;
+  __device__ __forceinline__ HeadGrad(const RowGrad& g, const HeadStats& h, float m_, float mr_) {
+    m = m_;
+    mr = mr_;
+    l2 = h.ls * kLog2e;
+    kd = g.ent + g.kl;
+    ky = -g.kl;
+    k0 = fmaf(g.ent, h.S - h.ls, -g.pg);
+    if (g.kl != 0.0f) k0 = fmaf(g.kl, (h.lsr - h.ls) - h.D, k0);
+  }
+  __device__ __forceinline__ float operator()(float z) const {
+    const float d = z - m, p = __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -l2));
+    return p == 0.0f ? 0.0f : p * fmaf(kd, d, k0);
+  }
+  __device__ __forceinline__ float operator()(float z, float y) const {
+    const float d = z - m, p = __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -l2));
+    return p == 0.0f ? 0.0f : p * fmaf(kd, d, fmaf(ky, y - mr, k0));
+  }
+};
 
-template <typename E, int G, int V>
-__device__ __forceinline__ void head_grad(const E* z, const E* y, const uint8_t* av, E* dz, int n, int lane, bool use,
-                                          const HeadStats& h, int a, const RowGrad& g) {
-  for (int j = lane * V; j < n; j += G * V) {
-    const int have = n - j;
-    Cols<E, V> zc, yc, out;
-    Cols<uint8_t, V> ac;
-    if (use) {
-      zc.load(z + j, have);
-      if (y) yc.load(y + j, have);
-      if (av) ac.load(av + j, have);
-    }
-#pragma unroll
-    for (int q = 0; q < V; ++q) {
-      float d = 0.0f;
-      if (use && (!av || ac.v[q] != 0)) {
-        const float lp = (zc[q] - h.m) - h.ls, p = exp_of(lp);
-        float c = g.ent * (lp + h.S);
-        if (y) c = fmaf(g.kl, lp - ((yc[q] - h.mr) - h.lsr) - h.D, c);
-        d = p == 0.0f ? 0.0f : p * (c - g.pg);
-        if (j + q == a) d += g.pg;
-      }
-      out.v[q] = elem<E>::from_f32(d);
-    }
-    out.store(dz + j, have);
+// A row's numbers beside its logits, the same in every lane of its team.
+struct Row {
+  float w, adv, old, err;
+  bool pad;
+  template <typename E>
+  __device__ __forceinline__ void load(const Loss& p, int64_t n, const E* z) {
+    w = p.weight ? p.weight[n] : p.even;
+    pad = w == 0.0f;
+    adv = old = err = 0.0f;
+    if (pad) return;
+    adv = p.adv[n];
+    old = p.logp_old[n];
+    if (p.ret) err = elem<E>::to_f32(z[p.heads.A]) - p.ret[n];
+  }
+};
+
+// The row's loss: the factors of its gradient, and, of the eight sums, the
+// row's part of number q.
+__device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float logpi, float ent, float kl, float kl_coef,
+                                            int q, double* part) {
+  const float dlog = logpi - r.old, ratio = expf(dlog);
+  const float cut = fminf(fmaxf(ratio, 1.0f - p.clip_eps), 1.0f + p.clip_eps);
+  const float surr = fminf(ratio * r.adv, cut * r.adv);
+  const bool flow = (r.adv >= 0.0f && ratio <= 1.0f + p.clip_eps) || (r.adv < 0.0f && ratio >= 1.0f - p.clip_eps);
+  const float loss = -surr + p.vf_coef * r.err * r.err - p.ent_coef * ent + (kl_coef != 0.0f ? kl_coef * kl : 0.0f);
+  float x = -surr;
+  x = q == 1 ? r.err * r.err : x;
+  x = q == 2 ? ent : x;
+  x = q == 3 ? (fabsf(ratio - 1.0f) > p.clip_eps ? 1.0f : 0.0f) : x;
+  x = q == 4 ? expm1f(dlog) - dlog : x;  // (r - 1) - log r without the cancellation in r - 1
+  x = q == 5 ? ratio : x;
+  x = q == 7 ? kl : x;
+  const double d = static_cast<double>(r.w) * x;
+  *part += q == 6 ? (isfinite(loss) ? 0.0 : 1.0) : d;
+  return {flow ? -r.w * ratio * r.adv : 0.0f, r.w * p.ent_coef, r.w * kl_coef};
+}
+
+// The block's sums: lane q of each team has the team's number q.
+template <int G, int kThreads>
+__device__ __forceinline__ void block_sums(double part, double* out) {
+  constexpr int kTeams = kThreads / G;
+  __shared__ double sums[kTeams][kSums];
+  const int team = threadIdx.x / G, lane = threadIdx.x % G;
+  if (lane < kSums) sums[team][lane] = part;
+  __syncthreads();
+  if (threadIdx.x < kSums) {
+    double s = 0.0;
+    for (int k = 0; k < kTeams; ++k) s += sums[k][threadIdx.x];
+    out[static_cast<size_t>(blockIdx.x) * kSums + threadIdx.x] = s;
   }
 }
 
-// ----------------------------------------------------------------- kernels
+// ---------------------------------------------------- reductions of a team
 
-// A team's lane k holds head k's number.
-template <int G>
-__device__ __forceinline__ float of_head(float v, int k) { return __shfl(v, k, G < 64 ? G : 64); }
+__device__ __forceinline__ float op_max(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float op_sum(float a, float b) { return a + b; }
 
-template <typename E, int G, int V>
-__global__ void __launch_bounds__(G < 256 ? 256 : G) logits_rows(Loss p) {
-  constexpr int kThreads = G < 256 ? 256 : G, kTeams = kThreads / G;
-  __shared__ float redm[16][2], reds[16][4];
-  __shared__ double sums[kTeams][kSums];
-  const int team = threadIdx.x / G, lane = threadIdx.x % G, K = p.heads.K, A = p.heads.A;
+// Over a row of 16 lanes or a wave, the result in each lane, in a fixed order.
+template <int G, class Op>
+__device__ __forceinline__ float lanes_reduce(float v, float id, Op op) {
+  if (G > 16) return wave_reduce(v, id, op);
+  v = op(v, dpp<0xB1>(id, v));    // quad_perm [1, 0, 3, 2]
+  v = op(v, dpp<0x4E>(id, v));    // quad_perm [2, 3, 0, 1]
+  v = op(v, dpp<0x124>(id, v));   // row_ror 4
+  return op(v, dpp<0x128>(id, v));  // row_ror 8
+}
+
+// What lane k of each wave of a team has of head k, joined over the team's
+// waves (in every lane if there is one head).  n values; red [waves][8][n].
+template <int G, int n, bool kOne, class Op>
+__device__ __forceinline__ void team_join(float (&v)[n], Op op, float (*red)[kMaxHeads][n]) {
+  if (G <= 64) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, k = kOne ? 0 : min(lane, kMaxHeads - 1);
+  __syncthreads();  // (what the last call left has been read)
+  if (lane < (kOne ? 1 : kMaxHeads))
+#pragma unroll
+    for (int q = 0; q < n; ++q) red[wave][lane][q] = v[q];
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < n; ++q) v[q] = red[0][k][q];
+  for (int w = 1; w < G / 64; ++w)
+#pragma unroll
+    for (int q = 0; q < n; ++q) v[q] = op(v[q], red[w][k][q]);
+}
+
+// ------------------------------------------------------- rows in registers
+
+// A team of G lanes, I slots to a lane.  kOne: one head.  With several, lane k
+// of each wave (of a row of 16 lanes) keeps head k's numbers.  kTiny: fewer
+// logits than a slot holds.
+template <typename E, int G, int I, bool kOne, bool kTiny = false>
+__global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
+  constexpr int V = Slot<E>::V, kThreads = G < 256 ? 256 : G, kTeams = kThreads / G, kWidth = G < 64 ? G : 64;
+  __shared__ float redm[G > 64 ? G / 64 : 1][kMaxHeads][2], reds[G > 64 ? G / 64 : 1][kMaxHeads][4];
+  const int lane = threadIdx.x % G, hl = lane % kWidth;
+  const int K = kOne ? 1 : p.heads.K, A = p.heads.A;
   const float kl_coef = p.y ? p.kl_coef : 0.0f;
-  double acc[kSums] = {};
+  // the slots' heads and places
+  int head[kOne ? 1 : I];
+  Span<V> spans[kOne ? 1 : I];
+  if (!kOne) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      int k = 0, s = i * G + lane, n = p.heads.off[1];
+      for (; k < K - 1 && s >= (n + V - 1) / V; ++k) {
+        s -= (n + V - 1) / V;
+        n = p.heads.off[k + 2] - p.heads.off[k + 1];
+      }
+      head[i] = k;
+      spans[i] = Span<V>(p.heads.off[k] + s * V, n - s * V, A);
+    }
+  }
+  const auto span = [&](int i) {
+    if (!kOne) return spans[i];
+    int l = lane;
+    asm volatile("" : "+v"(l));  // (formed anew each time, not kept in registers)
+    return Span<V>((i * G + l) * V, A - (i * G + l) * V, A);
+  };
+  const int my_off = p.heads.off[min(hl, K - 1)], my_size = p.heads.off[min(hl, K - 1) + 1] - my_off;
+  double part = 0.0;
+  const int team = G < 64 ? threadIdx.x / G : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
   for (int64_t n = static_cast<int64_t>(blockIdx.x) * kTeams + team; n < p.N; n += static_cast<int64_t>(gridDim.x) * kTeams) {
     const E* z = static_cast<const E*>(p.z) + n * p.ldz;
     const E* y = p.y ? static_cast<const E*>(p.y) + n * p.ldy : nullptr;
     E* dz = static_cast<E*>(p.dz) + n * p.ldd;
     const uint8_t* av = p.avail ? p.avail + n * A : nullptr;
-    const float w = p.weight ? p.weight[n] : p.even;
-    const bool pad = w == 0.0f;
-    float logpi = 0.0f, ent = 0.0f, kl = 0.0f;
-    // head k's statistics, in lane k (of each wave)
-    float m = 0.0f, ls = 0.0f, mr = 0.0f, lsr = 0.0f, S = 0.0f, D = 0.0f;
-    int use = 0;
-    for (int k = 0; k < K && !pad; ++k) {
-      if (p.mask && p.mask[n * K + k] == 0) continue;
-      const int o = p.heads.off[k], nk = p.heads.off[k + 1] - o, a = p.act[n * K + k];
-      const HeadStats h = head_stats<E, G, V>(z + o, y ? y + o : nullptr, av ? av + o : nullptr, nk, lane, redm, reds);
-      if (!h.some) continue;
-      const bool taken = a >= 0 && a < nk && (!av || av[o + a] != 0);
-      logpi += taken ? (elem<E>::to_f32(z[o + (taken ? a : 0)]) - h.m) - h.ls : -INFINITY;
-      ent += h.S;
-      kl += h.D;
-      use |= 1 << k;
-      if ((lane & 63) == k) m = h.m, ls = h.ls, mr = h.mr, lsr = h.lsr, S = h.S, D = h.D;
+    Row r;
+    r.load(p, n, z);
+    Slot<E> zs[I], ys[I];
+    if (r.pad) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        zs[i].lo = zs[i].hi = 0;
+        const Span<V> at = span(i);
+        zs[i].store(dz + at.col, at.skip, at.have);
+      }
+      if (lane == 0) {
+        if (p.ret) dz[A] = elem<E>::from_f32(0.0f);
+        if (p.logp) p.logp[n] = 0.0f;
+        if (p.kl) p.kl[n] = 0.0f;
+      }
+      continue;
     }
-    const float Ad = pad ? 0.0f : p.adv[n];
-    const float dlog = pad ? 0.0f : logpi - p.logp_old[n];
-    const float ratio = expf(dlog);
-    const float cut = fminf(fmaxf(ratio, 1.0f - p.clip_eps), 1.0f + p.clip_eps);
-    const float surr = fminf(ratio * Ad, cut * Ad);
-    const bool flow = (Ad >= 0.0f && ratio <= 1.0f + p.clip_eps) || (Ad < 0.0f && ratio >= 1.0f - p.clip_eps);
-    const float err = p.ret && !pad ? elem<E>::to_f32(z[A]) - p.ret[n] : 0.0f;
-    const RowGrad g = {flow ? -w * ratio * Ad : 0.0f, w * p.ent_coef, w * kl_coef};
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      if (kTiny) {
+        zs[i].load_some(z, A);
+        if (y) ys[i].load_some(y, A);
+      } else {
+        const int c = span(i).col;
+        zs[i].load(z + c);
+        if (y) ys[i].load(y + c);
+      }
+    }
+    // lane k: the action of head k
+    int a = -1;
+    float za = -INFINITY;
+    bool active = false;
+    if (hl < K) {
+      const int k = hl;
+      active = !p.mask || p.mask[n * K + k] != 0;
+      a = p.act[n * K + k];
+      if (a < 0 || a >= my_size || (av && av[my_off + a] == 0))
+        a = -1;
+      else
+        za = elem<E>::to_f32(z[my_off + a]);
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      if (av || !kOne || (i + 1) * G * V > A) {
+        const uint32_t on = span(i).template on<kTiny>(av, A);
+        zs[i].mask(on);
+        if (y) ys[i].mask(on);
+      }
+    }
+    // the largest
+    constexpr int J = kOne ? 1 : I;
+    float zm[J], ym[J];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int to = kOne ? 0 : i;
+      zs[i].hold();
+      ys[i].hold();
+      if (!kOne || i == 0) zm[to] = ym[to] = kLowest;
+#pragma unroll
+      for (int q = 0; q < V; ++q) zm[to] = fmaxf(zm[to], zs[i][q]);
+      if (y)
+#pragma unroll
+        for (int q = 0; q < V; ++q) ym[to] = fmaxf(ym[to], ys[i][q]);
+    }
+    float mm[2] = {kLowest, kLowest};
     for (int k = 0; k < K; ++k) {
-      const int o = p.heads.off[k], nk = p.heads.off[k + 1] - o;
-      HeadStats h;
-      h.m = of_head<G>(m, k);
-      h.ls = of_head<G>(ls, k);
-      h.mr = of_head<G>(mr, k);
-      h.lsr = of_head<G>(lsr, k);
-      h.S = of_head<G>(S, k);
-      h.D = of_head<G>(D, k);
-      const bool on = (use >> k) & 1;
-      head_grad<E, G, V>(z + o, kl_coef != 0.0f ? y + o : nullptr, av ? av + o : nullptr, dz + o, nk, lane, on, h,
-                         on ? p.act[n * K + k] : -1, g);
+      float u[2] = {kLowest, kLowest};
+#pragma unroll
+      for (int i = 0; i < J; ++i)
+        if (kOne || head[i] == k) u[0] = fmaxf(u[0], zm[i]), u[1] = fmaxf(u[1], ym[i]);
+      u[0] = lanes_reduce<G>(u[0], kLowest, op_max);
+      if (y) u[1] = lanes_reduce<G>(u[1], kLowest, op_max);
+      if (kOne || hl == k) mm[0] = u[0], mm[1] = u[1];
+    }
+    team_join<G, 2, kOne>(mm, op_max, redm);
+    // the sums
+    Sums sum[J];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const float m = kOne ? mm[0] : __shfl(mm[0], head[i], kWidth), mr = kOne ? mm[1] : __shfl(mm[1], head[i], kWidth);
+      if (!kOne || i == 0) sum[i] = {0.0f, 0.0f, 0.0f, 0.0f};
+      Sums& to = sum[kOne ? 0 : i];
+      zs[i].hold();
+      ys[i].hold();
+      if (y)
+#pragma unroll
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], m, ys[i][q], mr);
+      else
+#pragma unroll
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], m);
+    }
+    float all[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < K; ++k) {
+      float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < J; ++i)
+        if (kOne || head[i] == k) u[0] += sum[i].s, u[1] += sum[i].t, u[2] += sum[i].v, u[3] += sum[i].sr;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < 2 || y) u[q] = lanes_reduce<G>(u[q], 0.0f, op_sum);
+      if (kOne || hl == k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) all[q] = u[q];
+    }
+    team_join<G, 4, kOne>(all, op_sum, reds);
+    // lane k finishes head k; the row's numbers are sums over its heads
+    const HeadStats h({all[0], all[1], all[2], all[3]}, y != nullptr);
+    const bool use = active && h.some;
+    float logpi = use ? (a < 0 ? -INFINITY : (za - mm[0]) - h.ls) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
+    bool on = use;
+    if (kOne) {  // (lane 0 of each wave has the action)
+      logpi = __shfl(logpi, 0, kWidth);
+      ent = __shfl(ent, 0, kWidth);
+      kl = __shfl(kl, 0, kWidth);
+      on = __shfl(static_cast<int>(use), 0, kWidth) != 0;
+      a = __shfl(a, 0, kWidth);
+    } else {
+      logpi = lanes_reduce<G>(logpi, 0.0f, op_sum);
+      ent = lanes_reduce<G>(ent, 0.0f, op_sum);
+      kl = lanes_reduce<G>(kl, 0.0f, op_sum);
+    }
+    const RowGrad g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
+    const HeadGrad hg(g, h, mm[0], mm[1]);
+    const int target = on && a >= 0 ? (kOne ? 0 : my_off) + a : -(1 << 30);
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      zs[i].hold();
+      ys[i].hold();
+      HeadGrad f = hg;
+      int to = target;
+      bool live = on;
+      if (!kOne) {
+        f.m = __shfl(hg.m, head[i], kWidth);
+        f.mr = __shfl(hg.mr, head[i], kWidth);
+        f.l2 = __shfl(hg.l2, head[i], kWidth);
+        f.k0 = __shfl(hg.k0, head[i], kWidth);
+        to = __shfl(target, head[i], kWidth);
+        live = __shfl(static_cast<int>(on), head[i], kWidth) != 0;
+      }
+      float out[V];
+      if (!live) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) out[q] = 0.0f;
+      } else if (kl_coef != 0.0f) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) out[q] = f(zs[i][q], ys[i][q]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) out[q] = f(zs[i][q]);
+      }
+      const Span<V> at = span(i);
+      to -= at.col;
+      if (static_cast<uint32_t>(to) < static_cast<uint32_t>(V))
+#pragma unroll
+        for (int q = 0; q < V; ++q) out[q] += q == to ? g.pg : 0.0f;
+      Slot<E> o;
+      o.set(out);
+      o.store(dz + at.col, at.skip, at.have);
     }
     if (lane == 0) {
-      if (p.ret) dz[A] = elem<E>::from_f32(2.0f * p.vf_coef * w * err);
-      if (p.logp) p.logp[n] = pad ? 0.0f : logpi;
-      if (p.kl) p.kl[n] = pad ? 0.0f : kl;
+      if (p.ret) dz[A] = elem<E>::from_f32(2.0f * p.vf_coef * r.w * r.err);
+      if (p.logp) p.logp[n] = logpi;
+      if (p.kl) p.kl[n] = kl;
     }
-    if (pad) continue;
-    const float loss = -surr + p.vf_coef * err * err - p.ent_coef * ent + (kl_coef != 0.0f ? kl_coef * kl : 0.0f);
-    const double wd = w;
-    acc[0] -= wd * surr;
-    acc[1] += wd * (err * err);
-    acc[2] += wd * ent;
-    acc[3] += fabsf(ratio - 1.0f) > p.clip_eps ? wd : 0.0;
-    acc[4] += wd * (expm1f(dlog) - dlog);  // (r - 1) - log r without the cancellation in r - 1
-    acc[5] += wd * ratio;
-    acc[6] += isfinite(loss) ? 0.0 : 1.0;
-    acc[7] += wd * kl;
   }
-  if (lane == 0)
+  block_sums<G, kThreads>(part, p.part);
+}
+
+// --------------------------------------------------------- rows read twice
+
+constexpr int kWide = 1024;  // lanes
+
+// A block takes a row, head after head; U slots of a lane are in flight at once.
+template <typename E>
+__global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
+  constexpr int V = Slot<E>::V, U = 16 / V;
+  __shared__ float redm[kWide / 64][kMaxHeads][2], reds[kWide / 64][kMaxHeads][4];
+  const int lane = threadIdx.x, hl = lane & 63, K = p.heads.K, A = p.heads.A;
+  const float kl_coef = p.y ? p.kl_coef : 0.0f;
+  double part = 0.0;
+  for (int64_t n = blockIdx.x; n < p.N; n += gridDim.x) {
+    const E* z = static_cast<const E*>(p.z) + n * p.ldz;
+    const E* y = p.y ? static_cast<const E*>(p.y) + n * p.ldy : nullptr;
+    E* dz = static_cast<E*>(p.dz) + n * p.ldd;
+    const uint8_t* av = p.avail ? p.avail + n * A : nullptr;
+    Row r;
+    r.load(p, n, z);
+    // head k's numbers, in lane k of each wave
+    float m = 0.0f, mr = 0.0f, all[4] = {0.0f, 0.0f, 0.0f, 0.0f}, za = -INFINITY;
+    int a = -1;
+    bool active = false;
+    for (int k = 0; k < K && !r.pad; ++k) {
+      if (p.mask && p.mask[n * K + k] == 0) continue;
+      const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
+      float mk[2] = {kLowest, kLowest};
+      Sums s = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j0 = lane * V; j0 < size; j0 += kWide * V * U) {
+        Slot<E> zs[U], ys[U];
+        uint32_t on[U];
 #pragma unroll
-    for (int q = 0; q < kSums; ++q) sums[team][q] = acc[q];
-  __syncthreads();
-  if (threadIdx.x < kSums) {
-    double s = 0.0;
-    for (int q = 0; q < kTeams; ++q) s += sums[q][threadIdx.x];
-    p.part[static_cast<size_t>(blockIdx.x) * kSums + threadIdx.x] = s;
+        for (int u = 0; u < U; ++u) {
+          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          zs[u].load(z + at.col);
+          if (y) ys[u].load(y + at.col);
+          on[u] = at.template on<false>(av, A);
+        }
+        float mn[2] = {mk[0], mk[1]};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          zs[u].hold();
+          if (on[u] != (1u << V) - 1) {
+            zs[u].mask(on[u]);
+            if (y) ys[u].mask(on[u]);
+          }
+#pragma unroll
+          for (int q = 0; q < V; ++q) mn[0] = fmaxf(mn[0], zs[u][q]);
+          if (y)
+#pragma unroll
+            for (int q = 0; q < V; ++q) mn[1] = fmaxf(mn[1], ys[u][q]);
+        }
+        s.move(mk[0], mk[1], mn[0], mn[1]);
+        mk[0] = mn[0];
+        mk[1] = mn[1];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          zs[u].hold();
+          ys[u].hold();
+          if (y)
+#pragma unroll
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0], ys[u][q], mk[1]);
+          else
+#pragma unroll
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0]);
+        }
+      }
+      float mm[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) mm[q] = wave_reduce(mk[q], kLowest, op_max);
+      team_join<kWide, 2, true>(mm, op_max, redm);
+      s.move(mk[0], mk[1], mm[0], mm[1]);
+      float u[4] = {s.s, s.t, s.v, s.sr};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) u[q] = wave_reduce(u[q], 0.0f, op_sum);
+      team_join<kWide, 4, true>(u, op_sum, reds);
+      if (hl == k) {
+        m = mm[0];
+        mr = mm[1];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) all[q] = u[q];
+        active = true;
+        a = p.act[n * K + k];
+        if (a < 0 || a >= size || (av && av[o + a] == 0))
+          a = -1;
+        else
+          za = elem<E>::to_f32(z[o + a]);
+      }
+    }
+    const HeadStats h({all[0], all[1], all[2], all[3]}, y != nullptr);
+    const bool use = active && h.some;
+    const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : (za - m) - h.ls) : 0.0f, 0.0f, op_sum);
+    const float ent = wave_reduce(use ? h.S : 0.0f, 0.0f, op_sum), kl = wave_reduce(use ? h.D : 0.0f, 0.0f, op_sum);
+    RowGrad g = {0.0f, 0.0f, 0.0f};
+    if (!r.pad) g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
+    const HeadGrad hg(g, h, m, mr);
+    for (int k = 0; k < K; ++k) {
+      const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
+      HeadGrad f;
+      f.m = __shfl(hg.m, k);
+      f.mr = __shfl(hg.mr, k);
+      f.l2 = __shfl(hg.l2, k);
+      f.k0 = __shfl(hg.k0, k);
+      f.kd = hg.kd;
+      f.ky = hg.ky;
+      const int target = __shfl(a < 0 ? -(1 << 30) : a + p.heads.off[min(hl, K - 1)], k);
+      const bool live = __shfl(static_cast<int>(use), k) != 0;
+      for (int j0 = lane * V; j0 < size; j0 += kWide * V * U) {
+        Slot<E> zs[U], ys[U];
+        uint32_t on[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          if (live) {
+            zs[u].load(z + at.col);
+            if (kl_coef != 0.0f) ys[u].load(y + at.col);
+          }
+          on[u] = live ? at.template on<false>(av, A) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          zs[u].hold();
+          float out[V];
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const float x = kl_coef != 0.0f ? f(zs[u][q], ys[u][q]) : f(zs[u][q]);
+            out[q] = (on[u] >> q) & 1 ? x : 0.0f;
+          }
+          const int to = target - at.col;
+          if (static_cast<uint32_t>(to) < static_cast<uint32_t>(V))
+#pragma unroll
+            for (int q = 0; q < V; ++q) out[q] += q == to ? g.pg : 0.0f;
+          Slot<E> d;
+          d.set(out);
+          d.store(dz + at.col, at.skip, at.have);
+        }
+      }
+    }
+    if (lane == 0) {
+      if (p.ret) dz[A] = elem<E>::from_f32(r.pad ? 0.0f : 2.0f * p.vf_coef * r.w * r.err);
+      if (p.logp) p.logp[n] = logpi;
+      if (p.kl) p.kl[n] = kl;
+    }
   }
+  block_sums<kWide, kWide>(part, p.part);
 }
 
 // The statistics from the blocks' sums, in a fixed order: thread t takes sum t
@@ -329,22 +686,42 @@ __global__ void __launch_bounds__(256) logits_stats(int blocks, const double* __
   }
 }
 
+// How a call's rows are taken: by slots of 16 bytes.
 struct Form {
-  int teams, threads;
-  void (*f32)(Loss);
-  void (*bf16)(Loss);
+  int teams, threads, blocks;  // teams and threads of a block, blocks at most
+  void (*kernel)(Loss);
 };
 
-Form form_of(const HeadsMeta& hm) {
-  int most = 0;
-  for (int k = 0; k < hm.K; ++k) most = std::max(most, hm.off[k + 1] - hm.off[k]);
-  if (most <= 128) return {16, 256, logits_rows<float, 16, 1>, logits_rows<uint16_t, 16, 1>};
-  if (most <= 2048) return {4, 256, logits_rows<float, 64, 4>, logits_rows<uint16_t, 64, 8>};
-  if (most <= 16384) return {1, 256, logits_rows<float, 256, 4>, logits_rows<uint16_t, 256, 8>};
-  return {1, 1024, logits_rows<float, 1024, 4>, logits_rows<uint16_t, 1024, 8>};
+template <typename E, int G, int I, bool kOne, bool kTiny = false>
+Form slots_form() {
+  return {G < 256 ? 256 / G : 1, G < 256 ? 256 : G, G < 256 ? 2048 : 256 * 2048 / G, logits_slots<E, G, I, kOne, kTiny>};
+}
+template <typename E, int G, int I>
+Form slots_form(bool one) {
+  return one ? slots_form<E, G, I, true>() : slots_form<E, G, I, false>();
 }
 
-int blocks_of(const Form& f, int N) { return static_cast<int>(std::min<long long>((N + f.teams - 1ll) / f.teams, kMaxBlocks)); }
+template <typename E>
+Form form_of(const HeadsMeta& hm) {
+  constexpr int V = Slot<E>::V;
+  int slots = 0;
+  for (int k = 0; k < hm.K; ++k) slots += (hm.off[k + 1] - hm.off[k] + V - 1) / V;
+  const bool one = hm.K == 1;
+  if (hm.A < V) return one ? slots_form<E, 16, 1, true, true>() : slots_form<E, 16, 1, false, true>();
+  if (slots <= 16) return slots_form<E, 16, 1>(one);
+  if (slots <= 32) return slots_form<E, 16, 2>(one);
+  if (slots <= 64) return slots_form<E, 64, 1>(one);
+  if (slots <= 128) return slots_form<E, 64, 2>(one);
+  if (slots <= 256) return slots_form<E, 64, 4>(one);
+  if (slots <= 1024) return slots_form<E, 256, 4>(one);
+  if (slots <= 2048) return one ? slots_form<E, 256, 8, true>() : slots_form<E, 512, 4, false>();
+  if (slots <= 4096) return one ? slots_form<E, 512, 8, true>() : slots_form<E, 1024, 4, false>();
+  if (slots <= 8192 && one) return slots_form<E, 1024, 8, true>();
+  return {1, kWide, 512, logits_stream<E>};
+}
+Form form_of(o5_dtype dt, const HeadsMeta& hm) { return dt == O5_BF16 ? form_of<uint16_t>(hm) : form_of<float>(hm); }
+
+int blocks_of(const Form& f, int N) { return static_cast<int>(std::min<long long>((N + f.teams - 1ll) / f.teams, f.blocks)); }
 
 #define O5_TRY(expr)              \
   do {                            \
@@ -385,7 +762,7 @@ using namespace o5;
 extern "C" size_t o5_ppo_logits_grad_workspace_bytes(o5_dtype dt, int N, int K, const int* head_sizes) {
   HeadsMeta hm;
   if (check_sizes("o5_ppo_logits_grad_workspace_bytes", dt, N, K, head_sizes, &hm) != O5_OK) return 0;
-  return std::max<size_t>(256, static_cast<size_t>(blocks_of(form_of(hm), N)) * kSums * sizeof(double));
+  return std::max<size_t>(256, static_cast<size_t>(blocks_of(form_of(dt, hm), N)) * kSums * sizeof(double));
 }
 
 extern "C" int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_sizes, const void* logits, size_t ldl,
@@ -422,9 +799,9 @@ extern "C" int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_siz
   p.logp = logp, p.kl = kl, p.part = static_cast<double*>(ws), p.N = N;
   p.clip_eps = hp.clip_eps, p.vf_coef = hp.vf_coef, p.ent_coef = hp.ent_coef, p.kl_coef = kl_coef;
   p.even = static_cast<float>(1.0 / N);
-  const Form f = form_of(p.heads);
+  const Form f = form_of(dt, p.heads);
   const int blocks = blocks_of(f, N);
-  hipLaunchKernelGGL(dt == O5_BF16 ? f.bf16 : f.f32, dim3(blocks), dim3(f.threads), 0, as_stream(stream), p);
+  hipLaunchKernelGGL(f.kernel, dim3(blocks), dim3(f.threads), 0, as_stream(stream), p);
   hipLaunchKernelGGL(logits_stats, dim3(1), dim3(256), 0, as_stream(stream), blocks, p.part, hp.vf_coef, hp.ent_coef,
                      ref ? kl_coef : 0.0f, stats);
   return check_launch(fn);
