@@ -4,12 +4,15 @@
 //   g = sigmoid(r), o = sigmoid(i), log a = -c softplus(lam) g
 //   h_t = a_t (1 - reset_t) h_{t-1} + beta_t o_t x_t,   beta = sqrt(1 - a^2)
 //
-// Every channel is a recurrence of its own, so that a lane takes two
-// neighbouring ones and walks the steps, the rows of some steps in flight while
-// it works on those before.  Where samples and channels are too few to fill the
-// chip the steps are cut into segments: one launch forms what each segment
-// leaves of the state that enters it and what it adds, one joins them in order,
-// and one runs the steps from the states that enter the segments.
+// Every channel is a recurrence of its own.  Where samples and channels fill the
+// chip, a lane takes two neighbouring channels and walks the steps, the rows of
+// some steps in flight while it works on those before.  Where they are fewer,
+// short sequences go to blocks of 16 waves with 8 steps each of the same 64
+// channels: each forms what its steps leave of the state that enters them and what
+// they add, the block joins these in LDS, and each wave finishes its steps from the
+// state that enters them, with the gates still in registers.  Long sequences of
+// few channels are cut into segments: one launch forms what each segment leaves and
+// adds, one joins them, and one runs the segments.
 //
 // w = 1 - a is formed without the cancellation near a = 1, and the state is
 // taken on as h - w h: a rounded to 24 bits would be off by 2^-25 of itself in
@@ -22,7 +25,7 @@ namespace {
 
 constexpr int kMark = 8;        // steps between the states that the forward pass leaves for the backward pass
 constexpr float kMost = 1e38f;  // the largest rate: times a gate that is 0 it is 0
-constexpr float kLn2 = 0.69314718f, kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f;
 
 // An array of rows: the row of step t and sample b is step t + ld b bytes from
 // p.  A call goes out in launches of so many samples that a lane's place within
@@ -90,29 +93,52 @@ struct Decay {
   }
 };
 
-// One step's state from the one before; rate in binary logs.
-__device__ __forceinline__ float next_state(float h, float y, float i, float x) {
-  const Decay a(y);
-  const float beta = __builtin_amdgcn_sqrtf(fmaf(-a.w, a.w, a.w + a.w));
-  return fmaf(beta, sigmoid2(i) * x, fmaf(-a.w, h, h));
+// What a step takes in, and its state from the one before: rounded the same in
+// every kernel (no product is joined with the sum), so that single tokens give
+// the bits of a sequence.
+__device__ __forceinline__ float taken_in(float w, float o, float x) {
+#pragma clang fp contract(off)
+  return __builtin_amdgcn_sqrtf(__builtin_fmaf(-w, w, w + w)) * (o * x);
+}
+__device__ __forceinline__ float next_state(float h, float w, float v) {
+#pragma clang fp contract(off)
+  return __builtin_fmaf(-w, h, h) + v;
+}
+__device__ __forceinline__ float next_state(float h, float y, float i, float x) {  // y: the decay in binary logs
+  const float w = Decay(y).w;
+  return next_state(h, w, taken_in(w, sigmoid2(i), x));
 }
 
-// A lane's two channels of one sample, its segment, and where they lie.
+// One step's gradients, from G, that of its state.
+struct Grad {
+  float dx, dr, di, e;  // e = G d(log a) log a
+  __device__ __forceinline__ Grad(float G, float rate, float x, float g, float o, float w, float before) {
+    const float v = fmaf(-w, w, w + w), a = 1.0f - w;
+    // 1 / beta; log a / beta goes to 0 with log a
+    const float ib = v < 0x1p-126f ? 0.0f : __builtin_amdgcn_rsqf(v);
+    e = G * (a * (-rate * g) * fmaf(-a * ib, o * x, before));
+    dx = G * (v * ib) * o;
+    dr = fmaf(-e, g, e);
+    di = dx * x * (1.0f - o);
+  }
+};
+
+// A lane's C neighbouring channels of one sample, n-th of its launch, and where
+// they lie.
+template <int C>
 struct Place {
-  uint32_t b, d, at, begin, end;
+  uint32_t b, d, at;
   bool on;
-  float rate[2];  // c softplus(lam)
-  __device__ __forceinline__ explicit Place(const Rec& p) {
-    const uint32_t n = blockIdx.x * blockDim.x + threadIdx.x, half = p.D / 2;
-    b = n / half;
-    d = (n - b * half) * 2;
+  float rate[C];  // c softplus(lam)
+  __device__ __forceinline__ Place(const Rec& p, uint32_t n) {
+    const uint32_t most = static_cast<uint32_t>(p.nb) * (p.D / C), per = p.D / C;
+    on = n < most;
+    n = min(n, most - 1);
+    b = n / per;
+    d = (n - b * per) * C;
     at = b * p.D + d;  // within the states
-    on = b < static_cast<uint32_t>(p.nb);
-    begin = blockIdx.y * p.len;
-    end = min(begin + p.len, static_cast<uint32_t>(p.T));
-    if (!on) return;
-    rate[0] = rate_of(p.c, p.lam[d]);
-    rate[1] = rate_of(p.c, p.lam[d + 1]);
+#pragma unroll
+    for (int j = 0; j < C; ++j) rate[j] = rate_of(p.c, p.lam[d + j]);
   }
   template <typename E>
   __device__ __forceinline__ uint32_t in(const Rows& a) const {
@@ -142,16 +168,17 @@ struct Steps {
   }
 };
 
-// Forward over a lane's segment.  kSum: only what the segment leaves of the
+// Forward, two channels to a lane, over segment blockIdx.y.  kSum: only what the segment leaves of the
 // state that enters it, and what it adds.
 template <typename E, bool kSum>
 __global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
-  constexpr int U = sizeof(E) == 2 ? 8 : 4;
-  const Place l(p);
+  constexpr int U = 4;
+  const Place<2> l(p, blockIdx.x * blockDim.x + threadIdx.x);
   if (!l.on) return;
   const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), h_at = l.in<E>(p.h);
   const float rate[2] = {kLog2e * l.rate[0], kLog2e * l.rate[1]};
   const uint64_t seg = blockIdx.y;
+  const int begin = seg * p.len, end = min(begin + p.len, p.T);
   f2_t h = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
   bool whole = true;
   if (!kSum) {
@@ -160,10 +187,9 @@ __global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
     else if (p.h0)
       h = state_in(p.h0, l.at);
   }
-  const int end = l.end;
   Steps<E, U> next;
-  next.load(p, x_at, r_at, i_at, l.b, l.begin, end);
-  for (int t0 = l.begin; t0 < end; t0 += U) {
+  next.load(p, x_at, r_at, i_at, l.b, begin, end);
+  for (int t0 = begin; t0 < end; t0 += U) {
     const Steps<E, U> s = next;
     next.load(p, x_at, r_at, i_at, l.b, t0 + U, end);
     if (!kSum && p.marks && t0 % kMark == 0) state_out(p.marks + (t0 / kMark) * p.states, l.at, h[0], h[1]);
@@ -229,21 +255,199 @@ __global__ void __launch_bounds__(1024) gatedrec_join(const float* __restrict__ 
   }
 }
 
-// What a segment leaves, to the segment before it, of the states' gradient
-// that enters from behind, and what it adds.
+// ------------------------------------------------ blocks of 64 channels
+
+constexpr int kWavesOf = 16;  // of a block at most, each kMark steps at a time
+
+template <typename E>
+__device__ __forceinline__ float one(const Rows& a, int t, uint32_t at) {
+  return elem<E>::to_f32(*reinterpret_cast<const E*>(a.p + t * a.step + at));
+}
+template <typename E>
+__device__ __forceinline__ void put(const Rows& a, int t, uint32_t at, float v) {
+  *reinterpret_cast<E*>(a.p + t * a.step + at) = elem<E>::from_f32(v);
+}
+
+// What the block's waves leave of a state and add, in the order in which a
+// state passes them; two buffers, so that one barrier keeps a wave that is a
+// round ahead from what the others still read.
+struct Board {
+  float keep[2][kWavesOf][64], add[2][kWavesOf][64];
+};
+
+// The state s passes the block's waves 0, 1, ... (or, back, ..., 1, 0); what
+// enters wave `wave` is left in `in`.
+__device__ __forceinline__ float pass_block(const Board& m, int buf, int waves, int wave, int lane, bool back, float s,
+                                            float* in) {
+#pragma unroll 4
+  for (int q = 0; q < waves; ++q) {
+    const int w = back ? waves - 1 - q : q;
+    *in = w == wave ? s : *in;
+    s = pass(m.keep[buf][w][lane], m.add[buf][w][lane], s);
+  }
+  return s;
+}
+
+// Forward.
+template <typename E>
+__global__ void __launch_bounds__(64 * kWavesOf) gatedrec_fwd_block(Rec p) {
+  constexpr int U = kMark;
+  __shared__ Board board;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const Place<1> l(p, blockIdx.x * 64 + lane);
+  const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), h_at = l.in<E>(p.h);
+  const float rate = kLog2e * l.rate[0];
+  const int end = p.T, round = waves * U;
+  float h = p.h0 ? p.h0[l.at] : 0.0f;
+  float x[U], r[U], i[U];
+  uint32_t cut = 0;
+  const auto fetch = [&](int t0) {
+    cut = 0;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int t = min(t0 + k, end - 1);
+      x[k] = one<E>(p.x, t, x_at);
+      r[k] = one<E>(p.r, t, r_at);
+      i[k] = one<E>(p.i, t, i_at);
+    }
+    if (p.reset)
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int t = min(t0 + k, end - 1);
+        cut |= t0 + k < end && p.reset[static_cast<uint64_t>(t) * p.B + l.b] != 0 ? 1u << k : 0u;
+      }
+  };
+  fetch(wave * U);
+  int buf = 0;
+  for (int c0 = 0; c0 < end; c0 += round, buf ^= 1) {
+    const int t0 = c0 + wave * U;
+    float w[U], v[U], e = 0.0f, y = 0.0f;
+    const uint32_t off = cut;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const bool there = t0 + k < end;
+      const float yk = there ? rate * sigmoid2(r[k]) : 0.0f;
+      w[k] = Decay(yk).w;
+      v[k] = there ? taken_in(w[k], sigmoid2(i[k]), x[k]) : 0.0f;
+      if ((off >> k) & 1) e = 0.0f;
+      e = next_state(e, w[k], v[k]);
+      y += yk;
+    }
+    if (c0 + round < end) fetch(t0 + round);
+    board.keep[buf][wave][lane] = off ? -1.0f : __builtin_amdgcn_exp2f(-y);
+    board.add[buf][wave][lane] = e;
+    __syncthreads();
+    float in = 0.0f;
+    h = pass_block(board, buf, waves, wave, lane, false, h, &in);
+    if (t0 >= end) continue;
+    if (p.marks && l.on) p.marks[(t0 / kMark) * p.states + l.at] = in;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (t0 + k >= end) break;
+      if ((off >> k) & 1) in = 0.0f;
+      in = next_state(in, w[k], v[k]);
+      if (l.on) put<E>(p.h, t0 + k, h_at, in);
+    }
+    if (p.hT && t0 + U >= p.T && l.on) p.hT[l.at] = in;
+  }
+}
+
+// Backward.
+template <typename E>
+__global__ void __launch_bounds__(64 * kWavesOf) gatedrec_bwd_block(Rec p) {
+  constexpr int U = kMark;
+  __shared__ Board board;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const Place<1> l(p, blockIdx.x * 64 + lane);
+  const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), d_at = l.in<E>(p.dh);
+  const uint32_t dx_at = l.in<E>(p.dx), dr_at = l.in<E>(p.dr), di_at = l.in<E>(p.di);
+  const int end = p.T, round = waves * U;
+  float G = p.dhT ? p.dhT[l.at] : 0.0f, sum = 0.0f;
+  int buf = 0;
+  for (int c0 = (end - 1) / round * round; c0 >= 0; c0 -= round, buf ^= 1) {
+    const int t0 = c0 + wave * U;
+    float x[U], g[U], o[U], dh[U], w[U], before[U];
+    uint32_t cut = 0;
+    float h = p.marks[(min(t0, end - 1) / kMark) * p.states + l.at];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int t = min(t0 + k, end - 1);
+      g[k] = one<E>(p.r, t, r_at);
+      x[k] = one<E>(p.x, t, x_at);
+      o[k] = one<E>(p.i, t, i_at);
+      dh[k] = one<E>(p.dh, t, d_at);
+    }
+    if (p.reset)
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int t = min(t0 + k, end - 1);
+        cut |= t0 + k < end && p.reset[static_cast<uint64_t>(t) * p.B + l.b] != 0 ? 1u << k : 0u;
+      }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if ((cut >> k) & 1) h = 0.0f;
+      before[k] = h;
+      g[k] = sigmoid2(g[k]);
+      o[k] = sigmoid2(o[k]);
+      w[k] = Decay(kLog2e * l.rate[0] * g[k]).w;
+      h = next_state(h, w[k], taken_in(w[k], o[k], x[k]));
+    }
+    float e = 0.0f, y = 0.0f;
+    bool open = true;
+#pragma unroll
+    for (int k = U - 1; k >= 0; --k) {
+      if (t0 + k >= end) continue;
+      e += dh[k];
+      e = fmaf(-w[k], e, e);
+      y += g[k];
+      if ((cut >> k) & 1) {
+        e = 0.0f;
+        open = false;
+      }
+    }
+    board.keep[buf][wave][lane] = open ? __builtin_amdgcn_exp2f(-kLog2e * l.rate[0] * y) : -1.0f;
+    board.add[buf][wave][lane] = e;
+    __syncthreads();
+    float in = 0.0f;
+    G = pass_block(board, buf, waves, wave, lane, true, G, &in);
+    if (t0 >= end) continue;
+#pragma unroll
+    for (int k = U - 1; k >= 0; --k) {
+      if (t0 + k >= end) continue;
+      const Grad d(in += dh[k], l.rate[0], x[k], g[k], o[k], w[k], before[k]);
+      sum += d.e;
+      in = (cut >> k) & 1 ? 0.0f : fmaf(-w[k], in, in);
+      if (l.on) {
+        put<E>(p.dx, t0 + k, dx_at, d.dx);
+        put<E>(p.dr, t0 + k, dr_at, d.dr);
+        put<E>(p.di, t0 + k, di_at, d.di);
+      }
+    }
+    if (p.dh0 && t0 == 0 && l.on) p.dh0[l.at] = in;
+  }
+  __syncthreads();
+  board.add[0][wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && l.on) {
+    for (int w = 1; w < waves; ++w) sum += board.add[0][w][lane];
+    p.part[l.at] = sum;
+  }
+}
+
+// --------------------------------------------------------------------------
+
+// What segment blockIdx.y + 1 leaves, to the segment before it, of the states'
+// gradient that enters it from behind, and what it adds.
 template <typename E>
 __global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
   constexpr int U = 8;
-  Place l(p);
+  const Place<2> l(p, blockIdx.x * blockDim.x + threadIdx.x);
   if (!l.on) return;
-  // (segment 0's is not wanted)
-  l.begin += p.len;
-  l.end = min(l.begin + p.len, static_cast<uint32_t>(p.T));
+  const int begin = (blockIdx.y + 1) * p.len, end = min(begin + p.len, p.T);
   const uint32_t r_at = l.in<E>(p.r), d_at = l.in<E>(p.dh);
   const float rate[2] = {kLog2e * l.rate[0], kLog2e * l.rate[1]};
   f2_t G = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
   bool whole = true;
-  const int begin = l.begin;
   Pair<E> nr[U], nd[U];
   uint8_t nc[U];
   const auto fetch = [&](int t1) {  // the steps before t1
@@ -255,8 +459,8 @@ __global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
       nc[k] = p.reset ? p.reset[static_cast<uint64_t>(t) * p.B + l.b] : 0;
     }
   };
-  fetch(l.end);
-  for (int t1 = l.end; t1 > begin; t1 -= U) {
+  fetch(end);
+  for (int t1 = end; t1 > begin; t1 -= U) {
     Pair<E> r[U], d[U];
     uint8_t cut[U];
 #pragma unroll
@@ -284,29 +488,39 @@ __global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
   state_out(p.add + seg * p.states, l.at, G[0], G[1]);
 }
 
-// Backward over a lane's segment.  The steps between two marks are run forward
+// Backward, two channels to a lane, over segment blockIdx.y.  The steps between two marks are run forward
 // from the mark, which leaves the state before each step and its gates in
-// registers, then backward.
+// registers, then backward, while those before them are in flight.
 template <typename E>
 __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
-  const Place l(p);
+  const Place<2> l(p, blockIdx.x * blockDim.x + threadIdx.x);
   if (!l.on) return;
   const uint32_t x_at = l.in<E>(p.x), r_at = l.in<E>(p.r), i_at = l.in<E>(p.i), d_at = l.in<E>(p.dh);
   const uint32_t dx_at = l.in<E>(p.dx), dr_at = l.in<E>(p.dr), di_at = l.in<E>(p.di);
   const uint64_t seg = blockIdx.y, segs = gridDim.y;
+  const int begin = seg * p.len, end = min(begin + p.len, p.T);
   f2_t G = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
   if (seg + 1 < segs)
     G = state_in(p.enter + seg * p.states, l.at);
   else if (p.dhT)
     G = state_in(p.dhT, l.at);
-  const int begin = l.begin, end = l.end;
-  for (int t0 = (end - 1) / kMark * kMark; t0 >= begin; t0 -= kMark) {
-    Steps<E, kMark> s;
-    Pair<E> dh[kMark];
-    s.load(p, x_at, r_at, i_at, l.b, t0, end);
+  Steps<E, kMark> next;
+  Pair<E> next_dh[kMark];
+  f2_t next_h;
+  const auto fetch = [&](int t0) {
+    next.load(p, x_at, r_at, i_at, l.b, t0, end);
 #pragma unroll
-    for (int k = 0; k < kMark; ++k) dh[k] = load<E>(p.dh, min(t0 + k, end - 1), d_at);
-    f2_t h = state_in(p.marks + (t0 / kMark) * p.states, l.at);
+    for (int k = 0; k < kMark; ++k) next_dh[k] = load<E>(p.dh, min(t0 + k, end - 1), d_at);
+    next_h = state_in(p.marks + (t0 / kMark) * p.states, l.at);
+  };
+  fetch((end - 1) / kMark * kMark);
+  for (int t0 = (end - 1) / kMark * kMark; t0 >= begin; t0 -= kMark) {
+    const Steps<E, kMark> s = next;
+    Pair<E> dh[kMark];
+#pragma unroll
+    for (int k = 0; k < kMark; ++k) dh[k] = next_dh[k];
+    f2_t h = next_h;
+    fetch(max(t0 - kMark, begin));
     float before[kMark][2], g[kMark][2], o[kMark][2], w[kMark][2];
 #pragma unroll
     for (int k = 0; k < kMark; ++k) {
@@ -317,8 +531,7 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
         g[k][j] = sigmoid2(s.r[k][j]);
         o[k][j] = sigmoid2(s.i[k][j]);
         w[k][j] = Decay(kLog2e * l.rate[j] * g[k][j]).w;
-        const float beta = __builtin_amdgcn_sqrtf(fmaf(-w[k][j], w[k][j], w[k][j] + w[k][j]));
-        h[j] = fmaf(beta, o[k][j] * s.x[k][j], fmaf(-w[k][j], h[j], h[j]));
+        h[j] = next_state(h[j], w[k][j], taken_in(w[k][j], o[k][j], s.x[k][j]));
       }
     }
 #pragma unroll
@@ -327,20 +540,13 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
       float dx[2], dr[2], di[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float x = s.x[k][j], wk = w[k][j], ok = o[k][j], gk = g[k][j];
-        const float v = fmaf(-wk, wk, wk + wk);
-        // 1 / beta; log a / beta goes to 0 with log a
-        const float ib = v < 0x1p-126f ? 0.0f : __builtin_amdgcn_rsqf(v);
-        const float a = 1.0f - wk;
         G[j] += dh[k][j];
-        // G d(log a) log a
-        const float e = G[j] * (a * (-l.rate[j] * gk) * fmaf(-a * ib, ok * x, before[k][j]));
-        const float du = G[j] * (v * ib);
-        dx[j] = du * ok;
-        dr[j] = fmaf(-e, gk, e);
-        di[j] = dx[j] * x * (1.0f - ok);
-        sum[j] += e;
-        G[j] = fmaf(-wk, G[j], G[j]);
+        const Grad d(G[j], l.rate[j], s.x[k][j], g[k][j], o[k][j], w[k][j], before[k][j]);
+        dx[j] = d.dx;
+        dr[j] = d.dr;
+        di[j] = d.di;
+        sum[j] += d.e;
+        G[j] = fmaf(-w[k][j], G[j], G[j]);
       }
       if (s.cut[k]) G = f2_t{0.0f, 0.0f};
       store<E>(p.dx, t0 + k, dx_at, dx[0], dx[1]);
@@ -428,22 +634,23 @@ int check_inputs(const char* fn, int D, const void* x, size_t ldx, const void* r
   return O5_OK;
 }
 
-// How the steps of a call are cut: segments of len steps, whole marks, one for
-// a call that fills the chip without.
+// How a call is run: in blocks of so many waves, or (0) in lanes, which take
+// segments of len steps (a multiple of a mark's).
 struct Cut {
-  int len, segments;
+  int waves, len, segments;
 };
-constexpr int kWaves = 2048;      // to fill the chip
+constexpr long long kLanes = 1024 * 64;  // that fill the chip
+constexpr int kShort = 2 * kWavesOf * kMark;
 constexpr int kMostSegments = 512;
-constexpr int kLeast = 32;        // steps of a segment
 
 Cut cut_of(int T, int B, int D) {
-  const long long waves = (static_cast<long long>(B) * (D / 2) + 63) / 64;
-  long long want = std::min<long long>(kMostSegments, kWaves / std::max(1ll, waves));
-  want = std::min<long long>(want, T / kLeast);
-  if (want < 2) return {T, 1};
+  const long long lanes = static_cast<long long>(B) * (D / 2);
+  if (lanes >= kLanes) return {0, T, 1};
+  if (T <= kShort) return {std::min(kWavesOf, (T + kMark - 1) / kMark), T, 1};
+  const long long want = std::min<long long>(std::min<long long>(kMostSegments, 2 * kLanes / std::max(64ll, lanes)), T / kMark);
+  if (want < 2) return {0, T, 1};
   const int len = static_cast<int>(((T + want - 1) / want + kMark - 1) / kMark * kMark);
-  return {len, (T + len - 1) / len};
+  return {0, len, (T + len - 1) / len};
 }
 
 // Sums, joins and the states that enter: three arrays of segments - 1 rows.
@@ -462,8 +669,7 @@ Rows rows_of(const void* p, size_t ld, int B, size_t es) {
   return {static_cast<char*>(const_cast<void*>(p)), ld * B * es, static_cast<uint32_t>(ld * es)};
 }
 
-// launch(arrays, samples, blocks) of at most so many samples that offsets
-// within a step stay below 2^32 (a row alone does: ld b is 0 there).
+// launch(arrays) of at most so many samples that offsets within a step stay below 2^32 (a row alone does: ld b is 0 there).
 template <class F>
 void launch_samples(const Rec& all, size_t most_ld, F&& launch) {
   const size_t most = std::max<size_t>(1, (static_cast<size_t>(1) << 31) / std::max(most_ld * 4, static_cast<size_t>(all.D) * 4));
@@ -478,8 +684,22 @@ void launch_samples(const Rec& all, size_t most_ld, F&& launch) {
     for (float** a : {&p.hT, &p.marks, &p.dh0, &p.part, &p.keep, &p.add, &p.enter})
       if (*a) *a += at;
     if (p.reset) p.reset += b;
-    launch(p, static_cast<unsigned>((static_cast<size_t>(p.nb) * (all.D / 2) + 255) / 256));
+    launch(p);
   }
+}
+
+void run_lanes(const Rec& all, size_t most_ld, int segments, void (*kernel)(Rec), hipStream_t s) {
+  launch_samples(all, most_ld, [&](const Rec& p) {
+    const unsigned blocks = static_cast<unsigned>((static_cast<size_t>(p.nb) * (p.D / 2) + 255) / 256);
+    hipLaunchKernelGGL(kernel, dim3(blocks, segments), dim3(256), 0, s, p);
+  });
+}
+
+void run_blocks(const Rec& all, size_t most_ld, int waves, void (*kernel)(Rec), hipStream_t s) {
+  launch_samples(all, most_ld, [&](const Rec& p) {
+    const unsigned blocks = static_cast<unsigned>((static_cast<size_t>(p.nb) * p.D + 63) / 64);
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), 0, s, p);
+  });
 }
 
 void join(const Rec& p, const Cut& c, const float* first, bool back, hipStream_t s) {
@@ -527,16 +747,16 @@ extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, 
   all.T = T, all.B = B, all.D = D, all.c = c, all.states = static_cast<uint64_t>(B) * D;
   place_cut(cut, B, D, ws, &all);
   const bool bf16 = dt == O5_BF16;
-  const auto run = [&](auto kernel, int segments) {
-    launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p, unsigned blocks) {
-      hipLaunchKernelGGL(kernel, dim3(blocks, segments), dim3(256), 0, as_stream(stream), p);
-    });
-  };
+  const size_t most = std::max(std::max(ldx, ldr), std::max(ldi, ldh));
+  if (cut.waves > 0) {
+    run_blocks(all, most, cut.waves, bf16 ? gatedrec_fwd_block<uint16_t> : gatedrec_fwd_block<float>, as_stream(stream));
+    return check_launch(fn);
+  }
   if (cut.segments > 1) {
-    run(bf16 ? gatedrec_fwd<uint16_t, true> : gatedrec_fwd<float, true>, cut.segments - 1);
+    run_lanes(all, most, cut.segments - 1, bf16 ? gatedrec_fwd<uint16_t, true> : gatedrec_fwd<float, true>, as_stream(stream));
     join(all, cut, h0, false, as_stream(stream));
   }
-  run(bf16 ? gatedrec_fwd<uint16_t, false> : gatedrec_fwd<float, false>, cut.segments);
+  run_lanes(all, most, cut.segments, bf16 ? gatedrec_fwd<uint16_t, false> : gatedrec_fwd<float, false>, as_stream(stream));
   return check_launch(fn);
 }
 
@@ -578,16 +798,15 @@ extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, 
   all.part = static_cast<float*>(ws) + cut_bytes(cut, B, D) / sizeof(float);
   const bool bf16 = dt == O5_BF16;
   const size_t most = std::max(std::max(std::max(ldx, ldr), std::max(ldi, lddh)), std::max(std::max(lddx, lddr), lddi));
-  const auto run = [&](auto kernel, int segments) {
-    launch_samples(all, most, [&](const Rec& p, unsigned blocks) {
-      hipLaunchKernelGGL(kernel, dim3(blocks, segments), dim3(256), 0, as_stream(stream), p);
-    });
-  };
-  if (cut.segments > 1) {
-    run(bf16 ? gatedrec_back_sum<uint16_t> : gatedrec_back_sum<float>, cut.segments - 1);
-    join(all, cut, dhT, true, as_stream(stream));
+  if (cut.waves > 0) {
+    run_blocks(all, most, cut.waves, bf16 ? gatedrec_bwd_block<uint16_t> : gatedrec_bwd_block<float>, as_stream(stream));
+  } else {
+    if (cut.segments > 1) {
+      run_lanes(all, most, cut.segments - 1, bf16 ? gatedrec_back_sum<uint16_t> : gatedrec_back_sum<float>, as_stream(stream));
+      join(all, cut, dhT, true, as_stream(stream));
+    }
+    run_lanes(all, most, cut.segments, bf16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>, as_stream(stream));
   }
-  run(bf16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>, cut.segments);
   hipLaunchKernelGGL(gatedrec_rates, dim3((D + 63) / 64), dim3(1024), 0, as_stream(stream),
                      static_cast<size_t>(cut.segments) * B, D, all.part, lam, dlam);
   return check_launch(fn);
@@ -609,7 +828,7 @@ extern "C" int o5_gatedrec_step(o5_dtype dt, int B, int D, const void* x, size_t
   all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
   all.h = rows_of(h, ldh, B, es);
   all.lam = lam, all.reset = reset, all.hT = S, all.T = 1, all.B = B, all.D = D, all.c = c;
-  launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p, unsigned) {
+  launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p) {
     const unsigned across = (D / 2 + 255) / 256;
     const unsigned down = std::min<unsigned>(65535, std::max<unsigned>(std::min<unsigned>(p.nb, 1024 / across), p.nb / kTokenRows));
     hipLaunchKernelGGL(dt == O5_BF16 ? gatedrec_token<uint16_t> : gatedrec_token<float>, dim3(across, down), dim3(256), 0,

@@ -31,18 +31,21 @@ constexpr int kMostLogits = 1 << 24;
 constexpr float kLowest = -3.40282346e38f;
 constexpr float kLog2e = 1.44269504f;
 
-struct Loss {  // a call's arrays
+// A call's arrays.  What a call has not is read all the same, from an array that
+// it has, and not used (has_*): a branch around a load would wait for it.
+struct Loss {
   const void *z, *y;
   void* dz;
-  size_t ldz, ldy, ldd;
+  size_t ldz, ldy, ldd, lda;
   const int32_t* act;
   const float *logp_old, *adv, *ret, *weight;
   const uint8_t *mask, *avail;
-  float *logp, *kl;
+  float *logp, *kl, *stats;
   double* part;  // [blocks][kSums]
   int N;
+  int has_ref, has_ret, has_weight, has_mask, has_avail;
   HeadsMeta heads;
-  float clip_eps, vf_coef, ent_coef, kl_coef, even;
+  float clip_eps, vf_coef, ent_coef, kl_coef, even;  // kl_coef: 0 without a reference
 };
 
 // ---------------------------------------------------------------- a slot
@@ -52,9 +55,9 @@ struct Loss {  // a call's arrays
 template <typename E>
 struct Slot {
   static constexpr int V = 16 / sizeof(E);
-  uint64_t lo, hi;
+  uint32_t w[4];
 
-  __device__ __forceinline__ void load(const E* p) { __builtin_memcpy(this, p, 16); }
+  __device__ __forceinline__ void load(const E* p) { __builtin_memcpy(w, p, 16); }
   // The first n of V, one by one.
   __device__ __forceinline__ void load_some(const E* p, int n) {
     float x[V];
@@ -65,48 +68,50 @@ struct Slot {
   // Columns skip to skip + n, V at most, to p + skip ...
   __device__ __forceinline__ void store(E* p, int skip, int n) const {
     if (n >= V) {
-      __builtin_memcpy(p, this, 16);
+      __builtin_memcpy(p, w, 16);
       return;
     }
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j >= skip && j < skip + n) p[j] = elem<E>::from_f32((*this)[j]);  // (exact: the slot holds E)
-  }
-  __device__ __forceinline__ uint32_t word(int k) const {
-    return static_cast<uint32_t>((k & 2 ? hi : lo) >> (k & 1 ? 32 : 0));
+    if (n <= 0) return;
+    constexpr int kBits = 8 * sizeof(E);
+    uint64_t lo = w[0] | static_cast<uint64_t>(w[1]) << 32, hi = w[2] | static_cast<uint64_t>(w[3]) << 32;
+    if (skip > 0) {
+      p += skip;
+      lo = skip < V / 2 ? (lo >> (kBits * skip)) | (hi << (64 - kBits * skip)) : hi >> (kBits * (skip - V / 2));
+      hi >>= kBits * min(skip, V / 2 - 1);  // (what is left of more is not stored)
+    }
+    if (n & (V / 2)) {
+      __builtin_memcpy(p, &lo, 8);
+      p += V / 2;
+      lo = hi;
+    }
+    if (V == 8 && (n & 2)) {
+      __builtin_memcpy(p, &lo, 4);
+      p += 2;
+      lo >>= 32;
+    }
+    if (n & 1) __builtin_memcpy(p, &lo, sizeof(E));
   }
   __device__ __forceinline__ float operator[](int j) const {
-    if (sizeof(E) == 4) return __uint_as_float(word(j));
-    const uint32_t w = word(j / 2);
-    return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+    if (sizeof(E) == 4) return __uint_as_float(w[j % 4]);
+    return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
   }
   __device__ __forceinline__ void set(const float (&x)[V]) {
-    uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       w[k] = sizeof(E) == 4 ? __float_as_uint(x[k]) : f32x2_to_bf16x2(x[2 * k % V], x[(2 * k + 1) % V]);
-    lo = w[0] | static_cast<uint64_t>(w[1]) << 32;
-    hi = w[2] | static_cast<uint64_t>(w[3]) << 32;
   }
   // What was computed from the slot before is not kept for what follows, nor is
   // what follows begun before: all columns as floats at once would take more
   // registers than there are.
   __device__ __forceinline__ void hold() {
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" : "+v"(lo), "+v"(hi));
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
   }
-  // -infinity in place of the columns that `on` does not name.
-  __device__ __forceinline__ void mask(uint32_t on) {
-    float x[V];
+  // -infinity in place of the columns whose bits in m are 0.
+  __device__ __forceinline__ void mask(const uint32_t (&m)[4]) {
+    const uint32_t low = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = (on >> j) & 1 ? (*this)[j] : -INFINITY;
-    set(x);
-  }
-  __device__ __forceinline__ void fill(float v) {
-    float x[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = v;
-    set(x);
+    for (int k = 0; k < 4; ++k) w[k] = (w[k] & m[k]) | (low & ~m[k]);
   }
 };
 
@@ -114,8 +119,9 @@ struct Slot {
 // columns skip to skip + have are the slot's own.  The last of a row begins
 // further left, so that no slot reaches past the row's A logits (there are V of
 // them but in tiny rows).
-template <int V>
+template <typename E>
 struct Span {
+  static constexpr int V = Slot<E>::V;
   int col, skip, have;
   __device__ __forceinline__ Span() = default;
   __device__ __forceinline__ Span(int start, int left, int A) {
@@ -123,23 +129,45 @@ struct Span {
     col = have > 0 ? max(0, min(start, A - V)) : 0;
     skip = have > 0 ? start - col : 0;
   }
-  // The bits of the columns that count: the slot's own, and of those the ones
-  // that are available (av: the row's, if any).
+  // The availability of the slot's columns as it is stored, a byte each.
   template <bool kTiny>
-  __device__ __forceinline__ uint32_t on(const uint8_t* av, int A) const {
-    uint32_t bits = ((1u << have) - 1) << skip;
-    if (!av) return bits;
-    uint64_t b = 0;
+  __device__ __forceinline__ void load(const uint8_t* av, int A, uint32_t (&b)[2]) const {
+    b[1] = 0;
     if (!kTiny) {
-      __builtin_memcpy(&b, av + col, V);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) b |= static_cast<uint64_t>(j < A ? av[j] : 0) << (8 * j);
+      __builtin_memcpy(b, av + col, V);
+      return;
     }
+    uint64_t x = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (((b >> (8 * j)) & 0xff) == 0) bits &= ~(1u << j);
-    return bits;
+    for (int j = 0; j < V; ++j) x |= static_cast<uint64_t>(j < A ? av[j] : 0) << (8 * j);
+    b[0] = static_cast<uint32_t>(x);
+    b[1] = static_cast<uint32_t>(x >> 32);
+  }
+  // All bits of the slot's own columns.
+  __device__ __forceinline__ void own(uint32_t (&m)[4]) const {
+    const int bits = ((1 << have) - 1) << skip;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (sizeof(E) == 4) {
+        m[k] = -((bits >> k) & 1);
+      } else {
+        const uint32_t lo = -((bits >> (2 * k)) & 1), hi = -((bits >> (2 * k + 1)) & 1);
+        m[k] = (lo & 0xffffu) | (hi & 0xffff0000u);
+      }
+    }
+  }
+  // ... and of the columns that are available.
+  __device__ __forceinline__ static void available(const uint32_t (&b)[2], uint32_t (&m)[4]) {
+    uint32_t t[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) t[k] = ((b[k] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | b[k];  // bit 7 of a byte that is not 0
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (sizeof(E) == 4)
+        m[k] &= -static_cast<int>((t[0] >> (8 * k + 7)) & 1);
+      else  // (selectors 8 to 11 are the signs of bytes 1 and 3 of the second and the first operand)
+        m[k] &= __builtin_amdgcn_perm(t[k / 2], t[k / 2] << 8, k & 1 ? 0x0b0b0909u : 0x0a0a0808u);
+    }
   }
 };
 
@@ -149,6 +177,7 @@ struct Span {
 // exponential is 0, and 0 times it is 0.
 __device__ __forceinline__ float below(float a, float b) { return fmaxf(a - b, kLowest); }
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * 0.69314718f; }
 // f x, and 0 where f is: what has become negligible may be infinite.
 __device__ __forceinline__ float scaled(float f, float x) { return f == 0.0f ? 0.0f : f * x; }
 
@@ -185,10 +214,11 @@ struct HeadStats {
   bool some;  // a logit that counts
   __device__ __forceinline__ HeadStats(const Sums& x, bool ref) {
     some = x.s != 0.0f;
-    ls = logf(x.s);
-    lsr = logf(x.sr);
-    S = ls - x.t / x.s;
-    D = ref ? (x.t - x.v) / x.s - logf(x.s / x.sr) : 0.0f;
+    const float inv = __builtin_amdgcn_rcpf(x.s);
+    ls = log_of(x.s);
+    lsr = log_of(x.sr);
+    S = ls - x.t * inv;
+    D = ref ? fmaf(x.t - x.v, inv, log_of(x.sr * inv)) : 0.0f;
   }
 };
 
@@ -224,22 +254,48 @@ struct Row {
   float w, adv, old, err;
   bool pad;
   template <typename E>
-  __device__ __forceinline__ void load(const Loss& p, int64_t n, const E* z) {
-    w = p.weight ? p.weight[n] : p.even;
+  __device__ __forceinline__ void load(const Loss& p, int64_t n, const E* z, float weight) {
+    w = weight;
     pad = w == 0.0f;
-    adv = old = err = 0.0f;
-    if (pad) return;
     adv = p.adv[n];
     old = p.logp_old[n];
-    if (p.ret) err = elem<E>::to_f32(z[p.heads.A]) - p.ret[n];
+    const float value = elem<E>::to_f32(z[p.has_ret ? p.heads.A : 0]), ret = p.ret[n];
+    err = p.has_ret ? value - ret : 0.0f;
   }
 };
+
+// What has to be known of a row before its logits are loaded, and is loaded a
+// row ahead: its weight and, in lane k, the action and the mask of head k.
+struct Ahead {
+  float w;
+  int a;
+  uint8_t active;
+  __device__ __forceinline__ void load(const Loss& p, int64_t n, int k) {
+    n = n < p.N ? n : p.N - 1;
+    w = p.weight[n];
+    a = p.act[n * p.heads.K + k];
+    active = p.mask[n * p.heads.K + k];
+    w = p.has_weight ? w : p.even;
+    active = p.has_mask ? active : 1;
+  }
+};
+
+// (r - 1) - log r of d = log r, without the cancellation near r = 1: the first
+// term left out of d^2/2 + d^3/6 + ... is 1e-7 of them at 0.25.
+__device__ __forceinline__ float beyond(float d, float r) {
+  float s = fmaf(d, 1.0f / 5040.0f, 1.0f / 720.0f);
+  s = fmaf(d, s, 1.0f / 120.0f);
+  s = fmaf(d, s, 1.0f / 24.0f);
+  s = fmaf(d, s, 1.0f / 6.0f);
+  s = fmaf(d, s, 0.5f);
+  return fabsf(d) < 0.25f ? d * d * s : (r - 1.0f) - d;
+}
 
 // The row's loss: the factors of its gradient, and, of the eight sums, the
 // row's part of number q.
 __device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float logpi, float ent, float kl, float kl_coef,
                                             int q, double* part) {
-  const float dlog = logpi - r.old, ratio = expf(dlog);
+  const float dlog = logpi - r.old, ratio = exp_of(dlog);
   const float cut = fminf(fmaxf(ratio, 1.0f - p.clip_eps), 1.0f + p.clip_eps);
   const float surr = fminf(ratio * r.adv, cut * r.adv);
   const bool flow = (r.adv >= 0.0f && ratio <= 1.0f + p.clip_eps) || (r.adv < 0.0f && ratio >= 1.0f - p.clip_eps);
@@ -248,7 +304,7 @@ __device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float l
   x = q == 1 ? r.err * r.err : x;
   x = q == 2 ? ent : x;
   x = q == 3 ? (fabsf(ratio - 1.0f) > p.clip_eps ? 1.0f : 0.0f) : x;
-  x = q == 4 ? expm1f(dlog) - dlog : x;  // (r - 1) - log r without the cancellation in r - 1
+  x = q == 4 ? beyond(dlog, ratio) : x;
   x = q == 5 ? ratio : x;
   x = q == 7 ? kl : x;
   const double d = static_cast<double>(r.w) * x;
@@ -256,19 +312,32 @@ __device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float l
   return {flow ? -r.w * ratio * r.adv : 0.0f, r.w * p.ent_coef, r.w * kl_coef};
 }
 
-// The block's sums: lane q of each team has the team's number q.
+// The statistics from the eight sums.
+__device__ __forceinline__ void write_stats(const double* x, float vf_coef, float ent_coef, float kl_coef, float* stats) {
+  const double kl = kl_coef != 0.0f ? kl_coef * x[7] : 0.0;
+  stats[0] = static_cast<float>(x[0] + vf_coef * x[1] - ent_coef * x[2] + kl);
+  for (int k = 0; k < kSums; ++k) stats[k + 1] = static_cast<float>(x[k]);
+}
+
+// The block's sums, of which lane q of each team has the team's number q; a
+// call's only block writes the statistics itself.
 template <int G, int kThreads>
-__device__ __forceinline__ void block_sums(double part, double* out) {
+__device__ __forceinline__ void block_sums(const Loss& p, double part) {
   constexpr int kTeams = kThreads / G;
   __shared__ double sums[kTeams][kSums];
   const int team = threadIdx.x / G, lane = threadIdx.x % G;
   if (lane < kSums) sums[team][lane] = part;
   __syncthreads();
+  double s = 0.0;
   if (threadIdx.x < kSums) {
-    double s = 0.0;
     for (int k = 0; k < kTeams; ++k) s += sums[k][threadIdx.x];
-    out[static_cast<size_t>(blockIdx.x) * kSums + threadIdx.x] = s;
+    if (gridDim.x > 1) p.part[static_cast<size_t>(blockIdx.x) * kSums + threadIdx.x] = s;
   }
+  if (gridDim.x > 1) return;
+  __syncthreads();
+  if (threadIdx.x < kSums) sums[0][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) write_stats(sums[0], p.vf_coef, p.ent_coef, p.kl_coef, p.stats);
 }
 
 // ---------------------------------------------------- reductions of a team
@@ -309,16 +378,17 @@ __device__ __forceinline__ void team_join(float (&v)[n], Op op, float (*red)[kMa
 // A team of G lanes, I slots to a lane.  kOne: one head.  With several, lane k
 // of each wave (of a row of 16 lanes) keeps head k's numbers.  kTiny: fewer
 // logits than a slot holds.
-template <typename E, int G, int I, bool kOne, bool kTiny = false>
-__global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
-  constexpr int V = Slot<E>::V, kThreads = G < 256 ? 256 : G, kTeams = kThreads / G, kWidth = G < 64 ? G : 64;
+template <typename E, int G, int I, bool kOne, bool kTiny, bool kAvail, int kThreads>
+__global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 3 : 4) logits_slots(Loss p) {
+  constexpr int V = Slot<E>::V, kTeams = kThreads / G, kWidth = G < 64 ? G : 64;
   __shared__ float redm[G > 64 ? G / 64 : 1][kMaxHeads][2], reds[G > 64 ? G / 64 : 1][kMaxHeads][4];
   const int lane = threadIdx.x % G, hl = lane % kWidth;
   const int K = kOne ? 1 : p.heads.K, A = p.heads.A;
-  const float kl_coef = p.y ? p.kl_coef : 0.0f;
+  const bool ref = p.has_ref != 0, some = kAvail && p.has_avail != 0;
+  const float kl_coef = p.kl_coef;
   // the slots' heads and places
   int head[kOne ? 1 : I];
-  Span<V> spans[kOne ? 1 : I];
+  Span<E> spans[kOne ? 1 : I];
   if (!kOne) {
 #pragma unroll
     for (int i = 0; i < I; ++i) {
@@ -328,70 +398,77 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
         n = p.heads.off[k + 2] - p.heads.off[k + 1];
       }
       head[i] = k;
-      spans[i] = Span<V>(p.heads.off[k] + s * V, n - s * V, A);
+      spans[i] = Span<E>(p.heads.off[k] + s * V, n - s * V, A);
     }
   }
   const auto span = [&](int i) {
     if (!kOne) return spans[i];
     int l = lane;
     asm volatile("" : "+v"(l));  // (formed anew each time, not kept in registers)
-    return Span<V>((i * G + l) * V, A - (i * G + l) * V, A);
+    return Span<E>((i * G + l) * V, A - (i * G + l) * V, A);
   };
   const int my_off = p.heads.off[min(hl, K - 1)], my_size = p.heads.off[min(hl, K - 1) + 1] - my_off;
   double part = 0.0;
+  // whether any of the wave's lanes has a slot i
+  const int wave_lane = __builtin_amdgcn_readfirstlane(lane & ~63);
+  const auto any = [&](int i) {
+    if (I == 1) return true;
+    return kOne ? (i * G + wave_lane) * V < A : __builtin_amdgcn_ballot_w64(spans[kOne ? 0 : i].have > 0) != 0;
+  };
   const int team = G < 64 ? threadIdx.x / G : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
-  for (int64_t n = static_cast<int64_t>(blockIdx.x) * kTeams + team; n < p.N; n += static_cast<int64_t>(gridDim.x) * kTeams) {
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams + team, step = static_cast<int64_t>(gridDim.x) * kTeams;
+  Ahead next = {0.0f, -1, 0};
+  next.load(p, first, min(hl, K - 1));
+  for (int64_t n = first; n < p.N; n += step) {
     const E* z = static_cast<const E*>(p.z) + n * p.ldz;
-    const E* y = p.y ? static_cast<const E*>(p.y) + n * p.ldy : nullptr;
+    const E* y = static_cast<const E*>(p.y) + n * p.ldy;
     E* dz = static_cast<E*>(p.dz) + n * p.ldd;
-    const uint8_t* av = p.avail ? p.avail + n * A : nullptr;
-    Row r;
-    r.load(p, n, z);
+    const uint8_t* av = p.avail + n * p.lda;
+    const Ahead now = next;
+    next.load(p, n + step, min(hl, K - 1));
     Slot<E> zs[I], ys[I];
-    if (r.pad) {
+    if (now.w == 0.0f) {
 #pragma unroll
       for (int i = 0; i < I; ++i) {
-        zs[i].lo = zs[i].hi = 0;
-        const Span<V> at = span(i);
+        zs[i] = {};
+        const Span<E> at = span(i);
         zs[i].store(dz + at.col, at.skip, at.have);
       }
       if (lane == 0) {
-        if (p.ret) dz[A] = elem<E>::from_f32(0.0f);
+        if (p.has_ret) dz[A] = elem<E>::from_f32(0.0f);
         if (p.logp) p.logp[n] = 0.0f;
         if (p.kl) p.kl[n] = 0.0f;
       }
       continue;
     }
+    uint32_t avs[I][2];
 #pragma unroll
     for (int i = 0; i < I; ++i) {
+      const Span<E> at = span(i);
       if (kTiny) {
         zs[i].load_some(z, A);
-        if (y) ys[i].load_some(y, A);
+        ys[i].load_some(y, A);
       } else {
-        const int c = span(i).col;
-        zs[i].load(z + c);
-        if (y) ys[i].load(y + c);
+        zs[i].load(z + at.col);
+        ys[i].load(y + at.col);
       }
+      if (kAvail) at.template load<kTiny>(av, A, avs[i]);
     }
     // lane k: the action of head k
-    int a = -1;
-    float za = -INFINITY;
-    bool active = false;
-    if (hl < K) {
-      const int k = hl;
-      active = !p.mask || p.mask[n * K + k] != 0;
-      a = p.act[n * K + k];
-      if (a < 0 || a >= my_size || (av && av[my_off + a] == 0))
-        a = -1;
-      else
-        za = elem<E>::to_f32(z[my_off + a]);
-    }
+    const bool active = hl < K && now.active != 0;
+    int a = hl < K && now.a >= 0 && now.a < my_size ? now.a : -1;
+    const float za = elem<E>::to_f32(z[my_off + max(a, 0)]);
+    if (some && av[my_off + max(a, 0)] == 0) a = -1;
+    Row r;
+    r.load(p, n, z, now.w);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      if (av || !kOne || (i + 1) * G * V > A) {
-        const uint32_t on = span(i).template on<kTiny>(av, A);
-        zs[i].mask(on);
-        if (y) ys[i].mask(on);
+      if (any(i) && (some || !kOne || (i + 1) * G * V > A)) {
+        uint32_t m[4];
+        span(i).own(m);
+        if (some) Span<E>::available(avs[i], m);
+        zs[i].mask(m);
+        ys[i].mask(m);
       }
     }
     // the largest
@@ -400,12 +477,13 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const int to = kOne ? 0 : i;
+      if (!kOne || i == 0) zm[to] = ym[to] = kLowest;
+      if (!any(i)) continue;
       zs[i].hold();
       ys[i].hold();
-      if (!kOne || i == 0) zm[to] = ym[to] = kLowest;
 #pragma unroll
       for (int q = 0; q < V; ++q) zm[to] = fmaxf(zm[to], zs[i][q]);
-      if (y)
+      if (ref)
 #pragma unroll
         for (int q = 0; q < V; ++q) ym[to] = fmaxf(ym[to], ys[i][q]);
     }
@@ -416,7 +494,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
       for (int i = 0; i < J; ++i)
         if (kOne || head[i] == k) u[0] = fmaxf(u[0], zm[i]), u[1] = fmaxf(u[1], ym[i]);
       u[0] = lanes_reduce<G>(u[0], kLowest, op_max);
-      if (y) u[1] = lanes_reduce<G>(u[1], kLowest, op_max);
+      if (ref) u[1] = lanes_reduce<G>(u[1], kLowest, op_max);
       if (kOne || hl == k) mm[0] = u[0], mm[1] = u[1];
     }
     team_join<G, 2, kOne>(mm, op_max, redm);
@@ -426,10 +504,11 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
     for (int i = 0; i < I; ++i) {
       const float m = kOne ? mm[0] : __shfl(mm[0], head[i], kWidth), mr = kOne ? mm[1] : __shfl(mm[1], head[i], kWidth);
       if (!kOne || i == 0) sum[i] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (!any(i)) continue;
       Sums& to = sum[kOne ? 0 : i];
       zs[i].hold();
       ys[i].hold();
-      if (y)
+      if (ref)
 #pragma unroll
         for (int q = 0; q < V; ++q) to.add(zs[i][q], m, ys[i][q], mr);
       else
@@ -444,14 +523,14 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
         if (kOne || head[i] == k) u[0] += sum[i].s, u[1] += sum[i].t, u[2] += sum[i].v, u[3] += sum[i].sr;
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (q < 2 || y) u[q] = lanes_reduce<G>(u[q], 0.0f, op_sum);
+        if (q < 2 || ref) u[q] = lanes_reduce<G>(u[q], 0.0f, op_sum);
       if (kOne || hl == k)
 #pragma unroll
         for (int q = 0; q < 4; ++q) all[q] = u[q];
     }
     team_join<G, 4, kOne>(all, op_sum, reds);
     // lane k finishes head k; the row's numbers are sums over its heads
-    const HeadStats h({all[0], all[1], all[2], all[3]}, y != nullptr);
+    const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some;
     float logpi = use ? (a < 0 ? -INFINITY : (za - mm[0]) - h.ls) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
     bool on = use;
@@ -471,6 +550,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
     const int target = on && a >= 0 ? (kOne ? 0 : my_off) + a : -(1 << 30);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
+      if (!any(i)) continue;
       zs[i].hold();
       ys[i].hold();
       HeadGrad f = hg;
@@ -495,7 +575,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
 #pragma unroll
         for (int q = 0; q < V; ++q) out[q] = f(zs[i][q]);
       }
-      const Span<V> at = span(i);
+      const Span<E> at = span(i);
       to -= at.col;
       if (static_cast<uint32_t>(to) < static_cast<uint32_t>(V))
 #pragma unroll
@@ -505,12 +585,12 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, 4) logits_slots(Loss p) {
       o.store(dz + at.col, at.skip, at.have);
     }
     if (lane == 0) {
-      if (p.ret) dz[A] = elem<E>::from_f32(2.0f * p.vf_coef * r.w * r.err);
+      if (p.has_ret) dz[A] = elem<E>::from_f32(2.0f * p.vf_coef * r.w * r.err);
       if (p.logp) p.logp[n] = logpi;
       if (p.kl) p.kl[n] = kl;
     }
   }
-  block_sums<G, kThreads>(part, p.part);
+  block_sums<G, kThreads>(p, part);
 }
 
 // --------------------------------------------------------- rows read twice
@@ -523,45 +603,50 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
   constexpr int V = Slot<E>::V, U = 16 / V;
   __shared__ float redm[kWide / 64][kMaxHeads][2], reds[kWide / 64][kMaxHeads][4];
   const int lane = threadIdx.x, hl = lane & 63, K = p.heads.K, A = p.heads.A;
-  const float kl_coef = p.y ? p.kl_coef : 0.0f;
+  const bool ref = p.has_ref != 0, some = p.has_avail != 0;
+  const float kl_coef = p.kl_coef;
   double part = 0.0;
   for (int64_t n = blockIdx.x; n < p.N; n += gridDim.x) {
     const E* z = static_cast<const E*>(p.z) + n * p.ldz;
-    const E* y = p.y ? static_cast<const E*>(p.y) + n * p.ldy : nullptr;
+    const E* y = static_cast<const E*>(p.y) + n * p.ldy;
     E* dz = static_cast<E*>(p.dz) + n * p.ldd;
-    const uint8_t* av = p.avail ? p.avail + n * A : nullptr;
+    const uint8_t* av = p.avail + n * p.lda;
     Row r;
-    r.load(p, n, z);
+    r.load(p, n, z, p.has_weight ? p.weight[n] : p.even);
     // head k's numbers, in lane k of each wave
     float m = 0.0f, mr = 0.0f, all[4] = {0.0f, 0.0f, 0.0f, 0.0f}, za = -INFINITY;
     int a = -1;
     bool active = false;
     for (int k = 0; k < K && !r.pad; ++k) {
-      if (p.mask && p.mask[n * K + k] == 0) continue;
+      if (p.has_mask && p.mask[n * K + k] == 0) continue;
       const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
       float mk[2] = {kLowest, kLowest};
       Sums s = {0.0f, 0.0f, 0.0f, 0.0f};
       for (int j0 = lane * V; j0 < size; j0 += kWide * V * U) {
         Slot<E> zs[U], ys[U];
-        uint32_t on[U];
+        uint32_t avs[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          const Span<E> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
           zs[u].load(z + at.col);
-          if (y) ys[u].load(y + at.col);
-          on[u] = at.template on<false>(av, A);
+          ys[u].load(y + at.col);
+          at.template load<false>(av, A, avs[u]);
         }
         float mn[2] = {mk[0], mk[1]};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           zs[u].hold();
-          if (on[u] != (1u << V) - 1) {
-            zs[u].mask(on[u]);
-            if (y) ys[u].mask(on[u]);
+          const Span<E> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          if (some || at.have < V) {
+            uint32_t m[4];
+            at.own(m);
+            if (some) Span<E>::available(avs[u], m);
+            zs[u].mask(m);
+            ys[u].mask(m);
           }
 #pragma unroll
           for (int q = 0; q < V; ++q) mn[0] = fmaxf(mn[0], zs[u][q]);
-          if (y)
+          if (ref)
 #pragma unroll
             for (int q = 0; q < V; ++q) mn[1] = fmaxf(mn[1], ys[u][q]);
         }
@@ -572,7 +657,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
         for (int u = 0; u < U; ++u) {
           zs[u].hold();
           ys[u].hold();
-          if (y)
+          if (ref)
 #pragma unroll
             for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0], ys[u][q], mk[1]);
           else
@@ -596,13 +681,13 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
         for (int q = 0; q < 4; ++q) all[q] = u[q];
         active = true;
         a = p.act[n * K + k];
-        if (a < 0 || a >= size || (av && av[o + a] == 0))
+        if (a < 0 || a >= size || (some && av[o + a] == 0))
           a = -1;
         else
           za = elem<E>::to_f32(z[o + a]);
       }
     }
-    const HeadStats h({all[0], all[1], all[2], all[3]}, y != nullptr);
+    const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some;
     const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : (za - m) - h.ls) : 0.0f, 0.0f, op_sum);
     const float ent = wave_reduce(use ? h.S : 0.0f, 0.0f, op_sum), kl = wave_reduce(use ? h.D : 0.0f, 0.0f, op_sum);
@@ -622,25 +707,28 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
       const bool live = __shfl(static_cast<int>(use), k) != 0;
       for (int j0 = lane * V; j0 < size; j0 += kWide * V * U) {
         Slot<E> zs[U], ys[U];
-        uint32_t on[U];
+        uint32_t avs[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
-          if (live) {
-            zs[u].load(z + at.col);
-            if (kl_coef != 0.0f) ys[u].load(y + at.col);
-          }
-          on[u] = live ? at.template on<false>(av, A) : 0;
+          const Span<E> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          zs[u].load(z + at.col);
+          ys[u].load(y + at.col);
+          at.template load<false>(av, A, avs[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const Span<V> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
-          zs[u].hold();
-          float out[V];
+          const Span<E> at(o + j0 + u * kWide * V, size - j0 - u * kWide * V, A);
+          float out[V] = {};
+          if (live) {
+            zs[u].hold();
+            if (some) {
+              uint32_t m[4] = {~0u, ~0u, ~0u, ~0u};
+              Span<E>::available(avs[u], m);
+              zs[u].mask(m);
+              ys[u].mask(m);
+            }
 #pragma unroll
-          for (int q = 0; q < V; ++q) {
-            const float x = kl_coef != 0.0f ? f(zs[u][q], ys[u][q]) : f(zs[u][q]);
-            out[q] = (on[u] >> q) & 1 ? x : 0.0f;
+            for (int q = 0; q < V; ++q) out[q] = kl_coef != 0.0f ? f(zs[u][q], ys[u][q]) : f(zs[u][q]);
           }
           const int to = target - at.col;
           if (static_cast<uint32_t>(to) < static_cast<uint32_t>(V))
@@ -653,12 +741,12 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
       }
     }
     if (lane == 0) {
-      if (p.ret) dz[A] = elem<E>::from_f32(r.pad ? 0.0f : 2.0f * p.vf_coef * r.w * r.err);
+      if (p.has_ret) dz[A] = elem<E>::from_f32(r.pad ? 0.0f : 2.0f * p.vf_coef * r.w * r.err);
       if (p.logp) p.logp[n] = logpi;
       if (p.kl) p.kl[n] = kl;
     }
   }
-  block_sums<kWide, kWide>(part, p.part);
+  block_sums<kWide, kWide>(p, part);
 }
 
 // The statistics from the blocks' sums, in a fixed order: thread t takes sum t
@@ -677,49 +765,55 @@ __global__ void __launch_bounds__(256) logits_stats(int blocks, const double* __
     red[0][q] = s;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const double* x = red[0];
-    const double kl = kl_coef != 0.0f ? kl_coef * x[7] : 0.0;
-    stats[0] = static_cast<float>(x[0] + vf_coef * x[1] - ent_coef * x[2] + kl);
-    for (int k = 0; k < 7; ++k) stats[k + 1] = static_cast<float>(x[k]);
-    stats[8] = static_cast<float>(x[7]);
-  }
+  if (threadIdx.x == 0) write_stats(red[0], vf_coef, ent_coef, kl_coef, stats);
 }
 
-// How a call's rows are taken: by slots of 16 bytes.
+// How a call's rows are taken, by the slots of 16 bytes that a row has.
 struct Form {
   int teams, threads, blocks;  // teams and threads of a block, blocks at most
   void (*kernel)(Loss);
 };
 
-template <typename E, int G, int I, bool kOne, bool kTiny = false>
-Form slots_form() {
-  return {G < 256 ? 256 / G : 1, G < 256 ? 256 : G, G < 256 ? 2048 : 256 * 2048 / G, logits_slots<E, G, I, kOne, kTiny>};
+template <typename E, int G, int I, bool kOne, bool kTiny = false, bool kAvail = true>
+Form slots_form(int N) {
+  constexpr int kThreads = G < 256 ? 256 : G;
+  // a few rows: one block takes them all and writes the statistics too
+  if constexpr (G < 256)
+    if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, 1024>};
+  return {kThreads / G, kThreads, 2048 * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kThreads>};
 }
 template <typename E, int G, int I>
-Form slots_form(bool one) {
-  return one ? slots_form<E, G, I, true>() : slots_form<E, G, I, false>();
+Form slots_form(int N, bool one) {
+  return one ? slots_form<E, G, I, true>(N) : slots_form<E, G, I, false>(N);
+}
+
+template <typename E, int G>
+Form wide_form(int N, bool avail) {
+  return avail ? slots_form<E, G, 8, true, false, true>(N) : slots_form<E, G, 8, true, false, false>(N);
 }
 
 template <typename E>
-Form form_of(const HeadsMeta& hm) {
+Form form_of(int N, const HeadsMeta& hm, bool avail) {
   constexpr int V = Slot<E>::V;
   int slots = 0;
   for (int k = 0; k < hm.K; ++k) slots += (hm.off[k + 1] - hm.off[k] + V - 1) / V;
   const bool one = hm.K == 1;
-  if (hm.A < V) return one ? slots_form<E, 16, 1, true, true>() : slots_form<E, 16, 1, false, true>();
-  if (slots <= 16) return slots_form<E, 16, 1>(one);
-  if (slots <= 32) return slots_form<E, 16, 2>(one);
-  if (slots <= 64) return slots_form<E, 64, 1>(one);
-  if (slots <= 128) return slots_form<E, 64, 2>(one);
-  if (slots <= 256) return slots_form<E, 64, 4>(one);
-  if (slots <= 1024) return slots_form<E, 256, 4>(one);
-  if (slots <= 2048) return one ? slots_form<E, 256, 8, true>() : slots_form<E, 512, 4, false>();
-  if (slots <= 4096) return one ? slots_form<E, 512, 8, true>() : slots_form<E, 1024, 4, false>();
-  if (slots <= 8192 && one) return slots_form<E, 1024, 8, true>();
+  if (hm.A < V) return one ? slots_form<E, 16, 1, true, true>(N) : slots_form<E, 16, 1, false, true>(N);
+  if (slots <= 16) return slots_form<E, 16, 1>(N, one);
+  if (slots <= 32) return slots_form<E, 16, 2>(N, one);
+  if (slots <= 64) return slots_form<E, 64, 1>(N, one);
+  if (slots <= 128) return slots_form<E, 64, 2>(N, one);
+  if (slots <= 256) return slots_form<E, 64, 4>(N, one);
+  if (slots <= 512) return slots_form<E, 256, 2>(N, one);
+  if (slots <= 1024) return slots_form<E, 256, 4>(N, one);
+  if (slots <= 2048) return one ? wide_form<E, 256>(N, avail) : slots_form<E, 512, 4, false>(N);
+  if (slots <= 4096 && one) return wide_form<E, 512>(N, avail);
+  if (slots <= 8192 && one) return wide_form<E, 1024>(N, avail);
   return {1, kWide, 512, logits_stream<E>};
 }
-Form form_of(o5_dtype dt, const HeadsMeta& hm) { return dt == O5_BF16 ? form_of<uint16_t>(hm) : form_of<float>(hm); }
+Form form_of(o5_dtype dt, int N, const HeadsMeta& hm, bool avail) {
+  return dt == O5_BF16 ? form_of<uint16_t>(N, hm, avail) : form_of<float>(N, hm, avail);
+}
 
 int blocks_of(const Form& f, int N) { return static_cast<int>(std::min<long long>((N + f.teams - 1ll) / f.teams, f.blocks)); }
 
@@ -762,7 +856,7 @@ using namespace o5;
 extern "C" size_t o5_ppo_logits_grad_workspace_bytes(o5_dtype dt, int N, int K, const int* head_sizes) {
   HeadsMeta hm;
   if (check_sizes("o5_ppo_logits_grad_workspace_bytes", dt, N, K, head_sizes, &hm) != O5_OK) return 0;
-  return std::max<size_t>(256, static_cast<size_t>(blocks_of(form_of(dt, hm), N)) * kSums * sizeof(double));
+  return std::max<size_t>(256, static_cast<size_t>(blocks_of(form_of(dt, N, hm, true), N)) * kSums * sizeof(double));
 }
 
 extern "C" int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_sizes, const void* logits, size_t ldl,
@@ -793,16 +887,21 @@ extern "C" int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_siz
   O5_CHECK(ws != nullptr && ws_bytes >= o5_ppo_logits_grad_workspace_bytes(dt, N, K, head_sizes), O5_E_WORKSPACE,
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
-  p.z = logits, p.y = ref, p.dz = dlogits;
-  p.ldz = ldl, p.ldy = ldr, p.ldd = ldd;
-  p.act = act, p.logp_old = logp_old, p.adv = adv, p.ret = ret, p.weight = weight, p.mask = head_mask, p.avail = avail;
-  p.logp = logp, p.kl = kl, p.part = static_cast<double*>(ws), p.N = N;
-  p.clip_eps = hp.clip_eps, p.vf_coef = hp.vf_coef, p.ent_coef = hp.ent_coef, p.kl_coef = kl_coef;
+  const uint8_t* bytes = static_cast<const uint8_t*>(logits);  // (a row of logits has more of them than logits)
+  p.z = logits, p.y = ref ? ref : logits, p.dz = dlogits;
+  p.ldz = ldl, p.ldy = ref ? ldr : ldl, p.ldd = ldd, p.lda = avail ? A : ldl * dtype_size(dt);
+  p.act = act, p.logp_old = logp_old, p.adv = adv, p.ret = ret ? ret : logp_old, p.weight = weight ? weight : logp_old;
+  p.mask = head_mask ? head_mask : reinterpret_cast<const uint8_t*>(act), p.avail = avail ? avail : bytes;
+  p.has_ref = ref != nullptr, p.has_ret = ret != nullptr, p.has_weight = weight != nullptr;
+  p.has_mask = head_mask != nullptr, p.has_avail = avail != nullptr;
+  p.logp = logp, p.kl = kl, p.stats = stats, p.part = static_cast<double*>(ws), p.N = N;
+  p.clip_eps = hp.clip_eps, p.vf_coef = hp.vf_coef, p.ent_coef = hp.ent_coef, p.kl_coef = ref ? kl_coef : 0.0f;
   p.even = static_cast<float>(1.0 / N);
-  const Form f = form_of(dt, p.heads);
+  const Form f = form_of(dt, N, p.heads, avail != nullptr);
   const int blocks = blocks_of(f, N);
   hipLaunchKernelGGL(f.kernel, dim3(blocks), dim3(f.threads), 0, as_stream(stream), p);
-  hipLaunchKernelGGL(logits_stats, dim3(1), dim3(256), 0, as_stream(stream), blocks, p.part, hp.vf_coef, hp.ent_coef,
-                     ref ? kl_coef : 0.0f, stats);
+  if (blocks > 1)
+    hipLaunchKernelGGL(logits_stats, dim3(1), dim3(256), 0, as_stream(stream), blocks, p.part, hp.vf_coef, hp.ent_coef,
+                       p.kl_coef, stats);
   return check_launch(fn);
 }
