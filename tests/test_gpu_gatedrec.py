@@ -118,6 +118,13 @@ SHAPES = [
     (16, 700, 64, 0.1, False),
     (48, 130, 512, 0.02, False),
 ]
+#        (channels that fill the chip: a lane walks two of them over all steps)
+WIDE = [
+    (1, 300, 520, 0.3, True),
+    (9, 4100, 40, 0.1, False),
+    (21, 260, 520, 0.05, True),
+    (16, 2048, 64, 0.1, False),
+]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
@@ -136,6 +143,19 @@ def test_forward_and_backward(bf16, shape):
         assert torch.isnan(c.wide[..., :8]).all()
     # inference without marks or last states: the same outputs
     assert torch.equal(c.fwd(state=False, marks=False)[0], h)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shape", WIDE, ids=lambda s: "x".join(map(str, s[:3])))
+def test_channels_that_fill_the_chip(bf16, shape):
+    need_gpu()
+    banner(f"gatedrec many channels bf16={bf16} {shape}")
+    c = Case(bf16, *shape)
+    h, hT = c.fwd()
+    c.check_fwd(h, hT)
+    got = c.bwd()
+    c.check_bwd(got)
+    assert all(torch.equal(a, b) for a, b in zip((h, hT, *got), (*c.fwd(), *c.bwd()))), "not the same bits twice"
 
 
 @pytest.mark.parametrize("bf16", [False, True])

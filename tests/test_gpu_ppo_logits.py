@@ -119,6 +119,11 @@ CASES = [
     (4, (11, 16385), True, True, True, False, True),
     (3, (50257,), True, True, True, False, False),
     (2, (131071, 2), False, True, False, False, False),
+    (19, (1, 2), True, True, True, True, True),
+    (90, (2, 1), False, False, False, False, False),
+    (70, (700,), True, True, True, False, True),
+    (5, (9000, 5), True, True, True, True, False),
+    (3, (20000,), False, False, True, False, False),
 ]
 
 
@@ -134,6 +139,16 @@ def test_loss_and_gradient(bf16, case):
     assert all(torch.equal(a, b) for a, b in zip(out, again)), "not the same bits twice"
     stats, dz, _, _ = c.run(rows=False)
     assert torch.equal(stats, out[0]) and torch.equal(dz, out[1])
+
+
+@pytest.mark.parametrize("N,heads", [(33000, (3, 5)), (9000, (300,)), (2100, (2500,)), (530, (70000, 2))])
+def test_more_rows_than_the_chip_takes_at_once(N, heads):
+    need_gpu()
+    banner(f"ppo_logits {N} rows of {heads}")
+    c = Case(True, N, heads, value=False, weight=True, seed=3)
+    out = c.run()
+    c.check(out)
+    assert all(torch.equal(a, b) for a, b in zip(out, c.run())), "not the same bits twice"
 
 
 @pytest.mark.parametrize("bf16", [False, True])
