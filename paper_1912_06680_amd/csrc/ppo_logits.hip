@@ -24,12 +24,17 @@
 #include "reduce.h"
 
 namespace o5 {
+
+// x y, and 0 where one of them is, whatever the other (v_mul_legacy_f32): what has
+// probability 0 counts nothing, infinities included.
+__device__ __attribute__((const)) float times(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
 namespace {
 
 constexpr int kSums = 8;  // pg, vf, ent, clipfrac, approx_kl, ratio, nonfinite, kl
 constexpr int kMostLogits = 1 << 24;
 constexpr float kLowest = -3.40282346e38f;
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 // A call's arrays.  What a call has not is read all the same, from an array that
 // it has, and not used (has_*): a branch around a load would wait for it.
@@ -126,8 +131,8 @@ struct Span {
   __device__ __forceinline__ Span() = default;
   __device__ __forceinline__ Span(int start, int left, int A) {
     have = max(0, min(V, left));
-    col = have > 0 ? max(0, min(start, A - V)) : 0;
-    skip = have > 0 ? start - col : 0;
+    col = max(0, min(start, A - V));  // (a slot of no columns lies somewhere in the row)
+    skip = (start - col) & (V - 1);
   }
   // The availability of the slot's columns as it is stored, a byte each.
   template <bool kTiny>
@@ -173,79 +178,88 @@ struct Span {
 
 // ------------------------------------------------------------ the formulas
 
-// a - b, where overflow and infinities become the lowest number: its
-// exponential is 0, and 0 times it is 0.
-__device__ __forceinline__ float below(float a, float b) { return fmaxf(a - b, kLowest); }
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * 0.69314718f; }
-// f x, and 0 where f is: what has become negligible may be infinite.
-__device__ __forceinline__ float scaled(float f, float x) { return f == 0.0f ? 0.0f : f * x; }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
-// The sums of a head's logits, relative to m and mr.
+// Logits relative to the largest, m, in binary logs: z -> fma(z, scale, shift).
+// The shift's rounding is the same for all and goes out of every difference.
+// Beyond 2^120, where binary logs overflow, different floats are 2^96 apart and
+// any scale tells them apart.
+struct Rel {
+  float scale, shift;
+  __device__ __forceinline__ Rel() = default;
+  __device__ __forceinline__ explicit Rel(float m) {
+    scale = fabsf(m) < 0x1p120f ? kLog2e : 0x1p-80f;
+    shift = -m * scale;
+  }
+  __device__ __forceinline__ float operator()(float z) const { return fmaf(z, scale, shift); }
+};
+// What goes from sums relative to `from` to sums relative to the larger `to`.
+__device__ __forceinline__ float between(float from, float to) { return fmaxf((from - to) * kLog2e, kLowest); }
+
+// The sums of a head's logits, relative to m and mr, in binary logs.
 struct Sums {
   float s, t, v, sr;
-  // (An exponential of 0 times anything but NaN counts nothing.)
-  __device__ __forceinline__ void add(float z, float m) {
-    const float d = z - m, e = exp_of(d);
+  __device__ __forceinline__ void add(float z, const Rel& m) {
+    const float d = m(z), e = exp2_of(d);
     s += e;
-    t = fmaf(e, fmaxf(d, -1000.0f), t);
+    t += times(e, d);
   }
-  __device__ __forceinline__ void add(float z, float m, float y, float mr) {
-    const float d = z - m, e = exp_of(d), dy = y - mr;
+  __device__ __forceinline__ void add(float z, const Rel& m, float y, const Rel& mr) {
+    const float d = m(z), e = exp2_of(d), dy = mr(y);
     s += e;
-    t = fmaf(e, fmaxf(d, -1000.0f), t);
-    v = fmaf(e, e == 0.0f ? 0.0f : dy, v);
-    sr += exp_of(dy);
+    t += times(e, d);
+    v += times(e, dy);
+    sr += exp2_of(dy);
   }
   // From m, mr to mn, mrn.
   __device__ __forceinline__ void move(float m, float mr, float mn, float mrn) {
-    const float d = below(m, mn), dr = below(mr, mrn), f = exp_of(d);
-    t = scaled(f, fmaf(s, d, t));
+    const float d = between(m, mn), dr = between(mr, mrn), f = exp2_of(d);
+    t = times(f, t + times(s, d));
     s *= f;
-    v = fmaf(s, dr, scaled(f, v));
-    sr *= exp_of(dr);
+    v = times(f, v) + times(s, dr);
+    sr *= exp2_of(dr);
   }
 };
 
-// A head's log-sums, entropy and divergence; the logs stand apart from the
-// largest logits, beside which they would be lost.
+// A head's log-sums (binary), entropy and divergence; the logs stand apart from
+// the largest logits, beside which they would be lost.
 struct HeadStats {
   float ls, lsr, S, D;
   bool some;  // a logit that counts
   __device__ __forceinline__ HeadStats(const Sums& x, bool ref) {
     some = x.s != 0.0f;
     const float inv = __builtin_amdgcn_rcpf(x.s);
-    ls = log_of(x.s);
-    lsr = log_of(x.sr);
-    S = ls - x.t * inv;
-    D = ref ? fmaf(x.t - x.v, inv, log_of(x.sr * inv)) : 0.0f;
+    ls = __builtin_amdgcn_logf(x.s);
+    lsr = __builtin_amdgcn_logf(x.sr);
+    S = kLn2 * (ls - x.t * inv);
+    D = ref ? fmaf(kLn2 * (x.t - x.v), inv, log_of(x.sr * inv)) : 0.0f;
   }
 };
 
 // What the row gives its heads' gradients, and a head's p_j (kd d + ky dy + k0)
-// of d = z - m, dy = y - mr, with p_j = 2^(d log2 e - l2).
+// of a logit d and the reference's dy in binary logs, with p_j = 2^(d - ls).
 struct RowGrad {
   float pg, ent, kl;
 };
 struct HeadGrad {
-  float m, mr, l2, kd, ky, k0;
+  Rel m, mr;
+  float ls, kd, ky, k0;
   __device__ __forceinline__ HeadGrad() = default;
-  __device__ __forceinline__ HeadGrad(const RowGrad& g, const HeadStats& h, float m_, float mr_) {
-    m = m_;
-    mr = mr_;
-    l2 = h.ls * kLog2e;
-    kd = g.ent + g.kl;
-    ky = -g.kl;
-    k0 = fmaf(g.ent, h.S - h.ls, -g.pg);
-    if (g.kl != 0.0f) k0 = fmaf(g.kl, (h.lsr - h.ls) - h.D, k0);
+  __device__ __forceinline__ HeadGrad(const RowGrad& g, const HeadStats& h, float m_, float mr_) : m(m_), mr(mr_) {
+    ls = h.ls;
+    kd = kLn2 * (g.ent + g.kl);
+    ky = -kLn2 * g.kl;
+    k0 = fmaf(g.ent, fmaf(-kLn2, h.ls, h.S), -g.pg);
+    if (g.kl != 0.0f) k0 = fmaf(g.kl, kLn2 * (h.lsr - h.ls) - h.D, k0);
   }
   __device__ __forceinline__ float operator()(float z) const {
-    const float d = z - m, p = __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -l2));
-    return p == 0.0f ? 0.0f : p * fmaf(kd, d, k0);
+    const float d = m(z);
+    return times(exp2_of(d - ls), fmaf(kd, d, k0));
   }
   __device__ __forceinline__ float operator()(float z, float y) const {
-    const float d = z - m, p = __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -l2));
-    return p == 0.0f ? 0.0f : p * fmaf(kd, d, fmaf(ky, y - mr, k0));
+    const float d = m(z);
+    return times(exp2_of(d - ls), fmaf(kd, d, fmaf(ky, mr(y), k0)));
   }
 };
 
@@ -295,7 +309,7 @@ __device__ __forceinline__ float beyond(float d, float r) {
 // row's part of number q.
 __device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float logpi, float ent, float kl, float kl_coef,
                                             int q, double* part) {
-  const float dlog = logpi - r.old, ratio = exp_of(dlog);
+  const float dlog = logpi - r.old, ratio = exp2_of(dlog * kLog2e);
   const float cut = fminf(fmaxf(ratio, 1.0f - p.clip_eps), 1.0f + p.clip_eps);
   const float surr = fminf(ratio * r.adv, cut * r.adv);
   const bool flow = (r.adv >= 0.0f && ratio <= 1.0f + p.clip_eps) || (r.adv < 0.0f && ratio >= 1.0f - p.clip_eps);
@@ -377,8 +391,9 @@ __device__ __forceinline__ void team_join(float (&v)[n], Op op, float (*red)[kMa
 
 // A team of G lanes, I slots to a lane.  kOne: one head.  With several, lane k
 // of each wave (of a row of 16 lanes) keeps head k's numbers.  kTiny: fewer
-// logits than a slot holds.
-template <typename E, int G, int I, bool kOne, bool kTiny, bool kAvail, int kThreads>
+// logits than a slot holds.  kMore: the row (of one head) has more slots than the
+// team holds; those behind are read twice, the second time from a cache.
+template <typename E, int G, int I, bool kOne, bool kTiny, bool kAvail, bool kMore, int kThreads>
 __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 3 : 4) logits_slots(Loss p) {
   constexpr int V = Slot<E>::V, kTeams = kThreads / G, kWidth = G < 64 ? G : 64;
   __shared__ float redm[G > 64 ? G / 64 : 1][kMaxHeads][2], reds[G > 64 ? G / 64 : 1][kMaxHeads][4];
@@ -434,6 +449,11 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         const Span<E> at = span(i);
         zs[i].store(dz + at.col, at.skip, at.have);
       }
+      if (kMore)
+        for (int j = (I * G + lane) * V; j < A; j += G * V) {
+          const Span<E> at(j, A - j, A);
+          zs[0].store(dz + at.col, at.skip, at.have);
+        }
       if (lane == 0) {
         if (p.has_ret) dz[A] = elem<E>::from_f32(0.0f);
         if (p.logp) p.logp[n] = 0.0f;
@@ -471,13 +491,50 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         ys[i].mask(m);
       }
     }
+    // the slots behind those held, as they come
+    float more_m[2] = {kLowest, kLowest};
+    Sums more = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (kMore)
+      for (int j = (I * G + lane) * V; j < A; j += G * V) {
+        const Span<E> at(j, A - j, A);
+        Slot<E> zx, yx;
+        uint32_t ax[2];
+        zx.load(z + at.col);
+        yx.load(y + at.col);
+        if (kAvail) at.template load<false>(av, A, ax);
+        if (some || at.have < V) {
+          uint32_t m[4];
+          at.own(m);
+          if (some) Span<E>::available(ax, m);
+          zx.mask(m);
+          yx.mask(m);
+        }
+        float mn[2] = {more_m[0], more_m[1]};
+#pragma unroll
+        for (int q = 0; q < V; ++q) mn[0] = fmaxf(mn[0], zx[q]);
+        if (ref)
+#pragma unroll
+          for (int q = 0; q < V; ++q) mn[1] = fmaxf(mn[1], yx[q]);
+        more.move(more_m[0], more_m[1], mn[0], mn[1]);
+        more_m[0] = mn[0];
+        more_m[1] = mn[1];
+        zx.hold();
+        yx.hold();
+        const Rel to_m(mn[0]), to_mr(mn[1]);
+        if (ref)
+#pragma unroll
+          for (int q = 0; q < V; ++q) more.add(zx[q], to_m, yx[q], to_mr);
+        else
+#pragma unroll
+          for (int q = 0; q < V; ++q) more.add(zx[q], to_m);
+      }
     // the largest
     constexpr int J = kOne ? 1 : I;
     float zm[J], ym[J];
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const int to = kOne ? 0 : i;
-      if (!kOne || i == 0) zm[to] = ym[to] = kLowest;
+      if (!kOne || i == 0) zm[to] = more_m[0], ym[to] = more_m[1];
       if (!any(i)) continue;
       zs[i].hold();
       ys[i].hold();
@@ -503,17 +560,21 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const float m = kOne ? mm[0] : __shfl(mm[0], head[i], kWidth), mr = kOne ? mm[1] : __shfl(mm[1], head[i], kWidth);
-      if (!kOne || i == 0) sum[i] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const Rel to_m(m), to_mr(mr);
+      if (!kOne || i == 0) {
+        sum[i] = more;
+        if (kMore) sum[i].move(more_m[0], more_m[1], m, mr);
+      }
       if (!any(i)) continue;
       Sums& to = sum[kOne ? 0 : i];
       zs[i].hold();
       ys[i].hold();
       if (ref)
 #pragma unroll
-        for (int q = 0; q < V; ++q) to.add(zs[i][q], m, ys[i][q], mr);
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], to_m, ys[i][q], to_mr);
       else
 #pragma unroll
-        for (int q = 0; q < V; ++q) to.add(zs[i][q], m);
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], to_m);
     }
     float all[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k = 0; k < K; ++k) {
@@ -532,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     // lane k finishes head k; the row's numbers are sums over its heads
     const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some;
-    float logpi = use ? (a < 0 ? -INFINITY : (za - mm[0]) - h.ls) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
+    float logpi = use ? (a < 0 ? -INFINITY : kLn2 * (Rel(mm[0])(za) - h.ls)) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
     bool on = use;
     if (kOne) {  // (lane 0 of each wave has the action)
       logpi = __shfl(logpi, 0, kWidth);
@@ -557,9 +618,9 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       int to = target;
       bool live = on;
       if (!kOne) {
-        f.m = __shfl(hg.m, head[i], kWidth);
-        f.mr = __shfl(hg.mr, head[i], kWidth);
-        f.l2 = __shfl(hg.l2, head[i], kWidth);
+        f.m = Rel(__shfl(mm[0], head[i], kWidth));
+        f.mr = Rel(__shfl(mm[1], head[i], kWidth));
+        f.ls = __shfl(hg.ls, head[i], kWidth);
         f.k0 = __shfl(hg.k0, head[i], kWidth);
         to = __shfl(target, head[i], kWidth);
         live = __shfl(static_cast<int>(on), head[i], kWidth) != 0;
@@ -584,6 +645,32 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       o.set(out);
       o.store(dz + at.col, at.skip, at.have);
     }
+    if (kMore)
+      for (int j = (I * G + lane) * V; j < A; j += G * V) {
+        const Span<E> at(j, A - j, A);
+        float out[V] = {};
+        if (on) {
+          Slot<E> zx, yx;
+          zx.load(z + at.col);
+          yx.load(y + at.col);
+          if (some) {
+            uint32_t ax[2], m[4] = {~0u, ~0u, ~0u, ~0u};
+            at.template load<false>(av, A, ax);
+            Span<E>::available(ax, m);
+            zx.mask(m);
+            yx.mask(m);
+          }
+#pragma unroll
+          for (int q = 0; q < V; ++q) out[q] = kl_coef != 0.0f ? hg(zx[q], yx[q]) : hg(zx[q]);
+        }
+        const int to = target - at.col;
+        if (static_cast<uint32_t>(to) < static_cast<uint32_t>(V))
+#pragma unroll
+          for (int q = 0; q < V; ++q) out[q] += q == to ? g.pg : 0.0f;
+        Slot<E> o;
+        o.set(out);
+        o.store(dz + at.col, at.skip, at.have);
+      }
     if (lane == 0) {
       if (p.has_ret) dz[A] = elem<E>::from_f32(2.0f * p.vf_coef * r.w * r.err);
       if (p.logp) p.logp[n] = logpi;
@@ -653,16 +740,17 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
         s.move(mk[0], mk[1], mn[0], mn[1]);
         mk[0] = mn[0];
         mk[1] = mn[1];
+        const Rel to_m(mk[0]), to_mr(mk[1]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           zs[u].hold();
           ys[u].hold();
           if (ref)
 #pragma unroll
-            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0], ys[u][q], mk[1]);
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], to_m, ys[u][q], to_mr);
           else
 #pragma unroll
-            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0]);
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], to_m);
         }
       }
       float mm[2];
@@ -689,7 +777,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
     }
     const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some;
-    const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : (za - m) - h.ls) : 0.0f, 0.0f, op_sum);
+    const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : kLn2 * (Rel(m)(za) - h.ls)) : 0.0f, 0.0f, op_sum);
     const float ent = wave_reduce(use ? h.S : 0.0f, 0.0f, op_sum), kl = wave_reduce(use ? h.D : 0.0f, 0.0f, op_sum);
     RowGrad g = {0.0f, 0.0f, 0.0f};
     if (!r.pad) g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
@@ -697,9 +785,9 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
     for (int k = 0; k < K; ++k) {
       const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
       HeadGrad f;
-      f.m = __shfl(hg.m, k);
-      f.mr = __shfl(hg.mr, k);
-      f.l2 = __shfl(hg.l2, k);
+      f.m = Rel(__shfl(m, k));
+      f.mr = Rel(__shfl(mr, k));
+      f.ls = __shfl(hg.ls, k);
       f.k0 = __shfl(hg.k0, k);
       f.kd = hg.kd;
       f.ky = hg.ky;
@@ -774,22 +862,22 @@ struct Form {
   void (*kernel)(Loss);
 };
 
-template <typename E, int G, int I, bool kOne, bool kTiny = false, bool kAvail = true>
+template <typename E, int G, int I, bool kOne, bool kTiny = false, bool kAvail = true, bool kMore = false>
 Form slots_form(int N) {
   constexpr int kThreads = G < 256 ? 256 : G;
   // a few rows: one block takes them all and writes the statistics too
   if constexpr (G < 256)
-    if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, 1024>};
-  return {kThreads / G, kThreads, 2048 * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kThreads>};
+    if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, 1024>};
+  return {kThreads / G, kThreads, (G == 16 ? 1024 : 2048) * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, kThreads>};
 }
 template <typename E, int G, int I>
 Form slots_form(int N, bool one) {
   return one ? slots_form<E, G, I, true>(N) : slots_form<E, G, I, false>(N);
 }
 
-template <typename E, int G>
+template <typename E, int G, bool kMore = false>
 Form wide_form(int N, bool avail) {
-  return avail ? slots_form<E, G, 8, true, false, true>(N) : slots_form<E, G, 8, true, false, false>(N);
+  return avail ? slots_form<E, G, 8, true, false, true, kMore>(N) : slots_form<E, G, 8, true, false, false, kMore>(N);
 }
 
 template <typename E>
@@ -809,6 +897,7 @@ Form form_of(int N, const HeadsMeta& hm, bool avail) {
   if (slots <= 2048) return one ? wide_form<E, 256>(N, avail) : slots_form<E, 512, 4, false>(N);
   if (slots <= 4096 && one) return wide_form<E, 512>(N, avail);
   if (slots <= 8192 && one) return wide_form<E, 1024>(N, avail);
+  if (one) return wide_form<E, 1024, true>(N, avail);
   return {1, kWide, 512, logits_stream<E>};
 }
 Form form_of(o5_dtype dt, int N, const HeadsMeta& hm, bool avail) {
