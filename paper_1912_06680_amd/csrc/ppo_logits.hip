@@ -416,6 +416,17 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       spans[i] = Span<E>(p.heads.off[k] + s * V, n - s * V, A);
     }
   }
+  // the heads that the wave has slots of
+  uint32_t here = 1;
+  if (!kOne) {
+    here = 0;
+    for (int k = 0; k < K; ++k) {
+      bool mine = false;
+#pragma unroll
+      for (int i = 0; i < (kOne ? 1 : I); ++i) mine |= head[i] == k && spans[i].have > 0;
+      here |= __builtin_amdgcn_ballot_w64(mine) != 0 ? 1u << k : 0u;
+    }
+  }
   const auto span = [&](int i) {
     if (!kOne) return spans[i];
     int l = lane;
@@ -546,6 +557,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     }
     float mm[2] = {kLowest, kLowest};
     for (int k = 0; k < K; ++k) {
+      if (!((here >> k) & 1)) continue;
       float u[2] = {kLowest, kLowest};
 #pragma unroll
       for (int i = 0; i < J; ++i)
@@ -578,6 +590,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     }
     float all[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k = 0; k < K; ++k) {
+      if (!((here >> k) & 1)) continue;
       float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int i = 0; i < J; ++i)
