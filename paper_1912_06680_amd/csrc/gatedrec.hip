@@ -77,7 +77,10 @@ __device__ __forceinline__ float sigmoid2(float x) {  // 1 / (1 + e^-x)
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
 }
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
-__device__ __forceinline__ float rate_of(float c, float lam) { return fminf(c * softplus(lam), kMost); }
+__device__ __forceinline__ float rate_of(float c, float lam) {
+  const float rate = c * softplus(lam);
+  return rate > kMost ? kMost : rate;  // (a NaN stays one)
+}
 
 // 1 - 2^-y and 2^-y of y >= 0: below 0.3 binary logs of e a polynomial, 2e-8 of
 // the value off (a minimax fit), where the difference would be 3e-7 off.
@@ -558,35 +561,58 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
   state_out(p.part + seg * p.states, l.at, sum[0], sum[1]);
 }
 
-// dlam: the sum over the rows of part [n, D] in a fixed order, a block 64
-// columns in 16 groups of rows, times d(log rate) / d(lam).
-__global__ void __launch_bounds__(1024) gatedrec_rates(size_t n, int D, const float* __restrict__ part,
-                                                       const float* __restrict__ lam, float* __restrict__ dlam) {
+// The sum over a lane's rows of p [n, D], every 16th from its group's, in a
+// fixed order; the block's 16 groups joined in group 0.
+__device__ __forceinline__ float column_sum(size_t n, size_t D, const float* p, bool on) {
   __shared__ float red[16][64];
-  const int c = threadIdx.x & 63, g = threadIdx.x >> 6, d = blockIdx.x * 64 + c;
+  const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
   float s = 0.0f;
-  if (d < D)
+  if (on)
 #pragma unroll 8
-    for (size_t k = g; k < n; k += 16) s += part[k * D + d];
+    for (size_t k = g; k < n; k += 16) s += p[k * D];
   red[g][c] = s;
   __syncthreads();
-  if (g == 0 && d < D) {
+  if (g == 0)
 #pragma unroll
     for (int k = 1; k < 16; ++k) s += red[k][c];
+  return s;
+}
+
+// Where there are many rows, rows blockIdx.x kRows and on are summed first, into
+// the first of them: the block alone reads its rows and columns.
+constexpr int kRows = 512;
+constexpr size_t kManyRows = 1024;
+
+__global__ void __launch_bounds__(1024) gatedrec_rows(size_t n, size_t row, int D, float* __restrict__ part) {
+  const int d = blockIdx.y * 64 + (threadIdx.x & 63);
+  const size_t from = static_cast<size_t>(blockIdx.x) * kRows;
+  float* p = part + from * row + d;
+  const float s = column_sum(n - from < kRows ? n - from : kRows, row, p, d < D);
+  if (threadIdx.x < 64 && d < D) *p = s;
+}
+
+// dlam: the sum over the rows of part, row numbers apart, a block 64 columns, times d(log rate) / d(lam).
+__global__ void __launch_bounds__(1024) gatedrec_rates(size_t n, size_t row, int D, const float* __restrict__ part,
+                                                       const float* __restrict__ lam, float* __restrict__ dlam) {
+  const int d = blockIdx.x * 64 + (threadIdx.x & 63);
+  const float s = column_sum(n, row, part + d, d < D);
+  if (threadIdx.x < 64 && d < D) {
     // sigmoid(lam) / softplus(lam), which is 1 - e^lam / 2 + ... far to the left
     const float e = expf(lam[d]);
     dlam[d] = s * (lam[d] < -15.0f ? 1.0f - 0.5f * e : 1.0f / ((1.0f + expf(-lam[d])) * softplus(lam[d])));
   }
 }
 
-// One step.  A lane keeps its channels and takes every gridDim.y-th sample: the
-// rates cost as much as ten steps.
+// One step.  A lane keeps its channels, whose rates cost as much as ten steps, and
+// takes sample after sample; where a sample has fewer lanes than a block, the block has
+// several side by side.
 template <typename E>
 __global__ void __launch_bounds__(256) gatedrec_token(Rec p, float* __restrict__ S) {
-  const uint32_t d = (blockIdx.x * blockDim.x + threadIdx.x) * 2;
-  if (d >= static_cast<uint32_t>(p.D)) return;
+  const uint32_t per = p.D / 2, beside = max(1u, 256 / per), row = per < 256 ? threadIdx.x / per : 0;
+  const uint32_t d = (blockIdx.x * 256 + threadIdx.x - row * per) * 2;
+  if (row >= beside || d >= static_cast<uint32_t>(p.D)) return;
   const float rate[2] = {kLog2e * rate_of(p.c, p.lam[d]), kLog2e * rate_of(p.c, p.lam[d + 1])};
-  for (uint32_t b = blockIdx.y; b < static_cast<uint32_t>(p.nb); b += gridDim.y) {
+  for (uint32_t b = blockIdx.y * beside + row; b < static_cast<uint32_t>(p.nb); b += gridDim.y * beside) {
     const Pair<E> x = load<E>(p.x, 0, b * p.x.ld + d * sizeof(E)), r = load<E>(p.r, 0, b * p.r.ld + d * sizeof(E)),
                   i = load<E>(p.i, 0, b * p.i.ld + d * sizeof(E));
     f2_t s = state_in(S, b * p.D + d);
@@ -642,13 +668,31 @@ struct Cut {
 constexpr long long kLanes = 1024 * 64;  // that fill the chip
 constexpr int kShort = 2 * kWavesOf * kMark;
 constexpr int kMostSegments = 512;
+constexpr long long kUnits = 256;  // compute units
 
-Cut cut_of(int T, int B, int D) {
-  const long long lanes = static_cast<long long>(B) * (D / 2);
+// Times in us, bf16, both sides measured.
+// - kLanes or more: each walks the whole sequence (T = 256, B = 32, D = 4096: forward 74, cut in two 98, in blocks
+//   99; backward 120, in blocks 141).  Half as many lanes are too few (B = 32, D = 2048: forward 72, in blocks 50).
+// - Fewer: short sequences in blocks, where a launch and a read of the inputs are saved (T = 256, B = 8, D = 1024:
+//   forward 15, in segments 19.5, backward 21.5 and 25.6; T = 128, B = 4, D = 512: 13 and 19, 17 and 21).  Where blocks
+//   alone have a walk of many rounds, segments are faster (T = 1000, B = 1, D = 64: 18, in blocks 42).
+// - Forward, a block on every compute unit is enough for long sequences too (T = 1000, B = 16, D = 1024: 51, in
+//   segments 63; B = 48, D = 2048: 224 and 328; T = 2000, B = 8, 128 blocks: 86 and 66).  Backward, segments read only
+//   two of five arrays again, and blocks gain at 256 (76 against 83) what they lose at 384 (125 against 113).
+// - More blocks than units take fewer waves, down to 4, so that one's barrier is another's work (B = 32, D = 2048,
+//   T = 256: 4 waves 50 and backward 75, 8 waves 55 and 79, 16 waves 61 and 88; T = 32: equal).
+// - Segments: two lanes for each that fills the chip (four: T = 2000, B = 4, D = 512 29 -> 32; long ones equal), of one
+//   mark's steps at the least (of 4 marks' T = 256, B = 8, D = 1024 28, of one 20), 512 of them at the most, which
+//   one block joins (1024 with four lanes for each: T = 12000, B = 1, D = 512 38 -> 43).
+Cut cut_of(int T, int B, int D, bool back) {
+  const long long lanes = static_cast<long long>(B) * (D / 2), blocks = (lanes + 31) / 32;
   if (lanes >= kLanes) return {0, T, 1};
-  if (T <= kShort) return {std::min(kWavesOf, (T + kMark - 1) / kMark), T, 1};
+  if (T <= kShort || (!back && blocks >= kUnits)) {
+    int waves = kWavesOf;
+    while (waves > 4 && blocks * waves > kUnits * kWavesOf) waves /= 2;
+    return {std::min(waves, (T + kMark - 1) / kMark), T, 1};
+  }
   const long long want = std::min<long long>(std::min<long long>(kMostSegments, 2 * kLanes / std::max(64ll, lanes)), T / kMark);
-  if (want < 2) return {0, T, 1};
   const int len = static_cast<int>(((T + want - 1) / want + kMark - 1) / kMark * kMark);
   return {0, len, (T + len - 1) / len};
 }
@@ -720,7 +764,7 @@ extern "C" size_t o5_gatedrec_marks_bytes(int T, int B, int D) {
 
 extern "C" size_t o5_gatedrec_fwd_workspace_bytes(o5_dtype dt, int T, int B, int D) {
   if (check_sizes("o5_gatedrec_fwd_workspace_bytes", dt, T, B, D) != O5_OK) return 0;
-  return std::max<size_t>(256, cut_bytes(cut_of(T, B, D), B, D));
+  return std::max<size_t>(256, cut_bytes(cut_of(T, B, D, false), B, D));
 }
 
 extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, size_t ldx, const void* r, size_t ldr,
@@ -739,7 +783,7 @@ extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, 
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
   const size_t es = dtype_size(dt);
-  const Cut cut = cut_of(T, B, D);
+  const Cut cut = cut_of(T, B, D, false);
   Rec all = {};
   all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
   all.h = rows_of(h, ldh, B, es);
@@ -762,7 +806,7 @@ extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, 
 
 extern "C" size_t o5_gatedrec_bwd_workspace_bytes(o5_dtype dt, int T, int B, int D) {
   if (check_sizes("o5_gatedrec_bwd_workspace_bytes", dt, T, B, D) != O5_OK) return 0;
-  const Cut c = cut_of(T, B, D);
+  const Cut c = cut_of(T, B, D, true);
   return cut_bytes(c, B, D) + static_cast<size_t>(c.segments) * B * D * sizeof(float);
 }
 
@@ -787,7 +831,7 @@ extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, 
            "%s: ws is NULL or ws_bytes=%zu is too small", fn, ws_bytes);
   O5_PTR(ws, "ws");
   const size_t es = dtype_size(dt);
-  const Cut cut = cut_of(T, B, D);
+  const Cut cut = cut_of(T, B, D, true);
   Rec all = {};
   all.x = rows_of(x, ldx, B, es), all.r = rows_of(r, ldr, B, es), all.i = rows_of(i, ldi, B, es);
   all.dh = rows_of(dh, lddh, B, es);
@@ -807,8 +851,12 @@ extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, 
     }
     run_lanes(all, most, cut.segments, bf16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>, as_stream(stream));
   }
-  hipLaunchKernelGGL(gatedrec_rates, dim3((D + 63) / 64), dim3(1024), 0, as_stream(stream),
-                     static_cast<size_t>(cut.segments) * B, D, all.part, lam, dlam);
+  size_t n = static_cast<size_t>(cut.segments) * B, row = D;
+  const unsigned across = (D + 63) / 64;
+  for (; n > kManyRows; n = (n + kRows - 1) / kRows, row *= kRows)
+    hipLaunchKernelGGL(gatedrec_rows, dim3(static_cast<unsigned>((n + kRows - 1) / kRows), across), dim3(1024), 0,
+                       as_stream(stream), n, row, D, all.part);
+  hipLaunchKernelGGL(gatedrec_rates, dim3(across), dim3(1024), 0, as_stream(stream), n, row, D, all.part, lam, dlam);
   return check_launch(fn);
 }
 
@@ -829,8 +877,9 @@ extern "C" int o5_gatedrec_step(o5_dtype dt, int B, int D, const void* x, size_t
   all.h = rows_of(h, ldh, B, es);
   all.lam = lam, all.reset = reset, all.hT = S, all.T = 1, all.B = B, all.D = D, all.c = c;
   launch_samples(all, std::max(std::max(ldx, ldr), std::max(ldi, ldh)), [&](const Rec& p) {
-    const unsigned across = (D / 2 + 255) / 256;
-    const unsigned down = std::min<unsigned>(65535, std::max<unsigned>(std::min<unsigned>(p.nb, 1024 / across), p.nb / kTokenRows));
+    const unsigned across = (D / 2 + 255) / 256, beside = std::max(1, 256 / (D / 2));
+    const unsigned rows = (p.nb + beside - 1) / beside;
+    const unsigned down = std::min<unsigned>(65535, std::max<unsigned>(std::min<unsigned>(rows, 1024 / across), rows / kTokenRows));
     hipLaunchKernelGGL(dt == O5_BF16 ? gatedrec_token<uint16_t> : gatedrec_token<float>, dim3(across, down), dim3(256), 0,
                        as_stream(stream), p, p.hT);
   });

@@ -125,6 +125,16 @@ WIDE = [
     (21, 260, 520, 0.05, True),
     (16, 2048, 64, 0.1, False),
 ]
+#        (enough channels for a block of them on every compute unit, which long sequences then pass in blocks too, of 16, 8
+#        and 4 waves; and samples whose parts of a rate's gradient are summed in two and in three launches)
+BETWEEN = [
+    (257, 64, 256, 0.01, False),
+    (300, 33, 512, 0.02, True),
+    (140, 70, 504, 0.05, False),
+    (290, 70, 1000, 0.0, False),
+    (11, 1500, 24, 0.1, True),
+    (1, 600000, 8, 0.3, False),
+]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
@@ -146,7 +156,7 @@ def test_forward_and_backward(bf16, shape):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("shape", WIDE, ids=lambda s: "x".join(map(str, s[:3])))
+@pytest.mark.parametrize("shape", WIDE + BETWEEN, ids=lambda s: "x".join(map(str, s[:3])))
 def test_channels_that_fill_the_chip(bf16, shape):
     need_gpu()
     banner(f"gatedrec many channels bf16={bf16} {shape}")
@@ -259,7 +269,7 @@ def test_what_a_reset_cuts_off_may_hold_anything(bf16, T, B):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("B,D", [(1, 8), (3, 72), (5, 1000), (130, 256), (2000, 64)])
+@pytest.mark.parametrize("B,D", [(1, 8), (3, 72), (5, 1000), (40, 512), (130, 256), (2000, 64), (4097, 40), (70000, 8)])
 def test_single_tokens(bf16, B, D):
     """Three tokens one after another equal three steps of a sequence, bit for bit."""
     need_gpu()
