@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kMark = 8;        // steps between the states that the forward pass leaves for the backward pass
 constexpr float kMost = 1e38f;  // the largest rate: times a gate that is 0 it is 0
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f;
 
 // An array of rows: the row of step t and sample b is step t + ld b bytes from
 // p.  A call goes out in launches of so many samples that a lane's place within
@@ -76,7 +76,23 @@ __device__ __forceinline__ void store(const Rows& a, int t, uint32_t at, float u
 __device__ __forceinline__ float sigmoid2(float x) {  // 1 / (1 + e^-x)
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
 }
-__device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
+// log(1 + e^x): with u = e^-|x| and s = u / (2 + u), at most 1/3, log(1 + u) is twice the
+// series s + s^3/3 + s^5/5 + ..., whose terms from s^15 on are 1e-8 of it (5 steps of
+// 2^-24 off at most).  |x| in binary logs is taken in two parts: its rounding would be
+// |x| 2^-24 of u.  A lane's two rates take 50 instructions, with expf and log1pf 230
+// (a token of 4096 x 4096 59 -> 57.5 us).
+__device__ __forceinline__ float softplus(float x) {
+  const float b = -fabsf(x) * kLog2e, rest = fmaf(-fabsf(x), kLog2eRest, fmaf(-fabsf(x), kLog2e, -b));
+  const float e = __builtin_amdgcn_exp2f(b), u = fabsf(x) < 100.0f ? fmaf(e, 0.693147181f * rest, e) : 0.0f;
+  const float s = u * __builtin_amdgcn_rcpf(2.0f + u), q = s * s;
+  float y = fmaf(q, 1.0f / 13.0f, 1.0f / 11.0f);
+  y = fmaf(q, y, 1.0f / 9.0f);
+  y = fmaf(q, y, 1.0f / 7.0f);
+  y = fmaf(q, y, 1.0f / 5.0f);
+  y = fmaf(q, y, 1.0f / 3.0f);
+  y = fmaf(q, y, 1.0f);
+  return fmaxf(x, 0.0f) + 2.0f * s * y;
+}
 __device__ __forceinline__ float rate_of(float c, float lam) {
   const float rate = c * softplus(lam);
   return rate > kMost ? kMost : rate;  // (a NaN stays one)
