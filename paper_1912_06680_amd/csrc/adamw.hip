@@ -434,16 +434,18 @@ __device__ __forceinline__ double squares(const G* g, size_t i, size_t end) {
   return s;
 }
 
-// The sum over the block in a fixed order, in thread 0.
+// The sum over a block of kWaves in a fixed order, in thread 0.
+template <int kWaves>
 __device__ __forceinline__ double block_sum(double s) {
-  __shared__ double red[256];
-  red[threadIdx.x] = s;
+  __shared__ double red[kWaves];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if (static_cast<int>(threadIdx.x) < w) red[threadIdx.x] += red[threadIdx.x + w];
-    __syncthreads();
-  }
-  return red[0];
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) s += red[w];
+  return s;
 }
 
 constexpr uint32_t kNormBlocks = 2048;
@@ -466,16 +468,16 @@ __global__ void __launch_bounds__(256) grad_squares(const void* __restrict__ pla
     s += t.g_bf16 ? squares(static_cast<const uint16_t*>(t.g), i, stop) : squares(static_cast<const float*>(t.g), i, stop);
     at += take;
   }
-  s = block_sum(s);
+  s = block_sum<4>(s);
   if (threadIdx.x == 0) part[b] = s;
 }
 
 // clip: the norm, and the factor that brings the gradients down to max_norm.
-__global__ void __launch_bounds__(256) grad_norm(int n, const double* __restrict__ part, float max_norm,
+__global__ void __launch_bounds__(1024) grad_norm(int n, const double* __restrict__ part, float max_norm,
                                                  float* __restrict__ clip) {
   double s = 0.0;
-  for (int k = threadIdx.x; k < n; k += 256) s += part[k];
-  s = block_sum(s);
+  for (int k = threadIdx.x; k < n; k += 1024) s += part[k];
+  s = block_sum<16>(s);
   if (threadIdx.x == 0) {
     const double norm = sqrt(s);
     clip[0] = static_cast<float>(norm);
@@ -629,7 +631,7 @@ extern "C" int o5_adamw_grad_norm(const void* plan, const void* plan_dev, float 
   const uint32_t blocks = norm_blocks(plan);
   double* part = static_cast<double*>(ws);
   hipLaunchKernelGGL(grad_squares, dim3(blocks), dim3(256), 0, as_stream(stream), plan_dev, h->tensors, h->chunks, part);
-  hipLaunchKernelGGL(grad_norm, dim3(1), dim3(256), 0, as_stream(stream), static_cast<int>(blocks), part, max_norm, clip);
+  hipLaunchKernelGGL(grad_norm, dim3(1), dim3(1024), 0, as_stream(stream), static_cast<int>(blocks), part, max_norm, clip);
   return check_launch(fn);
 }
 

@@ -851,19 +851,22 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
 }
 
 // The statistics from the blocks' sums, in a fixed order: thread t takes sum t
-// mod 8 of blocks t / 8, t / 8 + 32, ...
-__global__ void __launch_bounds__(256) logits_stats(int blocks, const double* __restrict__ part, float vf_coef,
-                                                    float ent_coef, float kl_coef, float* __restrict__ stats) {
-  __shared__ double red[32][kSums];
-  const int q = threadIdx.x % kSums, r = threadIdx.x / kSums;
+// mod 8 of blocks t / 8, t / 8 + 128, ...
+__global__ void __launch_bounds__(1024) logits_stats(int blocks, const double* __restrict__ part, float vf_coef,
+                                                     float ent_coef, float kl_coef, float* __restrict__ stats) {
+  __shared__ double red[16][kSums];
+  const int q = threadIdx.x % kSums, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double s = 0.0;
 #pragma unroll 8
-  for (int b = r; b < blocks; b += 32) s += part[b * kSums + q];
-  red[r][q] = s;
+  for (int b = threadIdx.x / kSums; b < blocks; b += 128) s += part[b * kSums + q];
+#pragma unroll
+  for (int d = kSums; d < 64; d *= 2) s += __shfl_xor(s, d);
+  if (lane < kSums) red[wave][lane] = s;
   __syncthreads();
-  if (r == 0) {
-    for (int k = 1; k < 32; ++k) s += red[k][q];
-    red[0][q] = s;
+  if (threadIdx.x < kSums) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += red[k][threadIdx.x];
+    red[0][threadIdx.x] = s;
   }
   __syncthreads();
   if (threadIdx.x == 0) write_stats(red[0], vf_coef, ent_coef, kl_coef, stats);
@@ -1003,7 +1006,7 @@ extern "C" int o5_ppo_logits_grad(o5_dtype dt, int N, int K, const int* head_siz
   const int blocks = blocks_of(f, N);
   hipLaunchKernelGGL(f.kernel, dim3(blocks), dim3(f.threads), 0, as_stream(stream), p);
   if (blocks > 1)
-    hipLaunchKernelGGL(logits_stats, dim3(1), dim3(256), 0, as_stream(stream), blocks, p.part, hp.vf_coef, hp.ent_coef,
+    hipLaunchKernelGGL(logits_stats, dim3(1), dim3(1024), 0, as_stream(stream), blocks, p.part, hp.vf_coef, hp.ent_coef,
                        p.kl_coef, stats);
   return check_launch(fn);
 }
