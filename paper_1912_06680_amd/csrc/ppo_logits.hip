@@ -356,17 +356,37 @@ __device__ __forceinline__ void block_sums(const Loss& p, double part) {
 
 // ---------------------------------------------------- reductions of a team
 
-__device__ __forceinline__ float op_max(float a, float b) { return fmaxf(a, b); }
+// (of numbers that are no NaN, which fmaxf would bring into a form of its own first)
+__device__ __forceinline__ float op_max(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
 __device__ __forceinline__ float op_sum(float a, float b) { return a + b; }
+
+template <int ctrl>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true));
+}
 
 // Over a row of 16 lanes or a wave, the result in each lane, in a fixed order.
 template <int G, class Op>
 __device__ __forceinline__ float lanes_reduce(float v, float id, Op op) {
   if (G > 16) return wave_reduce(v, id, op);
-  v = op(v, dpp<0xB1>(id, v));    // quad_perm [1, 0, 3, 2]
-  v = op(v, dpp<0x4E>(id, v));    // quad_perm [2, 3, 0, 1]
-  v = op(v, dpp<0x124>(id, v));   // row_ror 4
-  return op(v, dpp<0x128>(id, v));  // row_ror 8
+  v = op(v, moved<0xB1>(v));    // quad_perm [1, 0, 3, 2]
+  v = op(v, moved<0x4E>(v));    // quad_perm [2, 3, 0, 1]
+  v = op(v, moved<0x124>(v));   // row_ror 4
+  return op(v, moved<0x128>(v));  // row_ror 8
+}
+
+// Over the lanes of a row of 16 from this one on that have the same head (on[d]: the
+// lane 2^d further is one), in a fixed order.
+template <class Op>
+__device__ __forceinline__ float rest_of_head(float v, const bool (&on)[4], float id, Op op) {
+  float x = moved<0x101>(v);  // row_shl 1 (by all lanes)
+  v = op(v, on[0] ? x : id);
+  x = moved<0x102>(v);
+  v = op(v, on[1] ? x : id);
+  x = moved<0x104>(v);
+  v = op(v, on[2] ? x : id);
+  x = moved<0x108>(v);
+  return op(v, on[3] ? x : id);
 }
 
 // What lane k of each wave of a team has of head k, joined over the team's
@@ -390,12 +410,15 @@ __device__ __forceinline__ void team_join(float (&v)[n], Op op, float (*red)[kMa
 // ------------------------------------------------------- rows in registers
 
 // A team of G lanes, I slots to a lane.  kOne: one head.  With several, lane k
-// of each wave (of a row of 16 lanes) keeps head k's numbers.  kTiny: fewer
+// of each wave (of a row of 16 lanes) keeps head k's numbers, whose reductions take
+// head after head; where a lane of 16 has one slot, a head's lanes follow each other,
+// all heads are reduced at once and a head's first lane keeps its numbers.  kTiny: fewer
 // logits than a slot holds.  kMore: the row (of one head) has more slots than the
 // team holds; those behind are read twice, the second time from a cache.
 template <typename E, int G, int I, bool kOne, bool kTiny, bool kAvail, bool kMore, int kThreads>
 __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 3 : 4) logits_slots(Loss p) {
   constexpr int V = Slot<E>::V, kTeams = kThreads / G, kWidth = G < 64 ? G : 64;
+  constexpr bool kRuns = !kOne && G == 16 && I == 1;
   __shared__ float redm[G > 64 ? G / 64 : 1][kMaxHeads][2], reds[G > 64 ? G / 64 : 1][kMaxHeads][4];
   const int lane = threadIdx.x % G, hl = lane % kWidth;
   const int K = kOne ? 1 : p.heads.K, A = p.heads.A;
@@ -427,13 +450,29 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       here |= __builtin_amdgcn_ballot_w64(mine) != 0 ? 1u << k : 0u;
     }
   }
+  // the head whose numbers the lane keeps, and (kRuns) its first lane
+  int mine = min(hl, K - 1), from = mine;
+  bool keeps = hl < K, same[4];
+  if (kRuns) {
+    mine = head[0];
+    from = 0;
+    for (int k = 0; k < mine; ++k) from += (p.heads.off[k + 1] - p.heads.off[k] + V - 1) / V;
+    keeps = hl == from;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const int there = __shfl(mine, min(hl + (1 << d), 15), 16);  // (by all lanes: what a lane out of work has reads as 0)
+      same[d] = hl + (1 << d) < 16 && there == mine;
+    }
+  }
+  // what lane `from` of a head has, in the lanes of slot i
+  const auto of_head = [&](auto v, int i) { return __shfl(v, kRuns ? from : head[i], kWidth); };
   const auto span = [&](int i) {
     if (!kOne) return spans[i];
     int l = lane;
     asm volatile("" : "+v"(l));  // (formed anew each time, not kept in registers)
     return Span<E>((i * G + l) * V, A - (i * G + l) * V, A);
   };
-  const int my_off = p.heads.off[min(hl, K - 1)], my_size = p.heads.off[min(hl, K - 1) + 1] - my_off;
+  const int my_off = p.heads.off[mine], my_size = p.heads.off[mine + 1] - my_off;
   double part = 0.0;
   // whether any of the wave's lanes has a slot i
   const int wave_lane = __builtin_amdgcn_readfirstlane(lane & ~63);
@@ -444,14 +483,14 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
   const int team = G < 64 ? threadIdx.x / G : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams + team, step = static_cast<int64_t>(gridDim.x) * kTeams;
   Ahead next = {0.0f, -1, 0};
-  next.load(p, first, min(hl, K - 1));
+  next.load(p, first, mine);
   for (int64_t n = first; n < p.N; n += step) {
     const E* z = static_cast<const E*>(p.z) + n * p.ldz;
     const E* y = static_cast<const E*>(p.y) + n * p.ldy;
     E* dz = static_cast<E*>(p.dz) + n * p.ldd;
     const uint8_t* av = p.avail + n * p.lda;
     const Ahead now = next;
-    next.load(p, n + step, min(hl, K - 1));
+    next.load(p, n + step, mine);
     Slot<E> zs[I], ys[I];
     if (now.w == 0.0f) {
 #pragma unroll
@@ -485,9 +524,9 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       }
       if (kAvail) at.template load<kTiny>(av, A, avs[i]);
     }
-    // lane k: the action of head k
-    const bool active = hl < K && now.active != 0;
-    int a = hl < K && now.a >= 0 && now.a < my_size ? now.a : -1;
+    // the action of the lane's head
+    const bool active = (kRuns || keeps) && now.active != 0;
+    int a = (kRuns || keeps) && now.a >= 0 && now.a < my_size ? now.a : -1;
     const float za = elem<E>::to_f32(z[my_off + max(a, 0)]);
     if (some && av[my_off + max(a, 0)] == 0) a = -1;
     Row r;
@@ -556,7 +595,11 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         for (int q = 0; q < V; ++q) ym[to] = fmaxf(ym[to], ys[i][q]);
     }
     float mm[2] = {kLowest, kLowest};
-    for (int k = 0; k < K; ++k) {
+    if (kRuns) {
+      mm[0] = of_head(rest_of_head(zm[0], same, kLowest, op_max), 0);
+      if (ref) mm[1] = of_head(rest_of_head(ym[0], same, kLowest, op_max), 0);
+    }
+    for (int k = 0; k < K && !kRuns; ++k) {
       if (!((here >> k) & 1)) continue;
       float u[2] = {kLowest, kLowest};
 #pragma unroll
@@ -571,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     Sums sum[J];
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      const float m = kOne ? mm[0] : __shfl(mm[0], head[i], kWidth), mr = kOne ? mm[1] : __shfl(mm[1], head[i], kWidth);
+      const float m = kOne || kRuns ? mm[0] : of_head(mm[0], i), mr = kOne || kRuns ? mm[1] : of_head(mm[1], i);
       const Rel to_m(m), to_mr(mr);
       if (!kOne || i == 0) {
         sum[i] = more;
@@ -589,7 +632,12 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         for (int q = 0; q < V; ++q) to.add(zs[i][q], to_m);
     }
     float all[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < K; ++k) {
+    if (kRuns) {
+      all[0] = rest_of_head(sum[0].s, same, 0.0f, op_sum);
+      all[1] = rest_of_head(sum[0].t, same, 0.0f, op_sum);
+      if (ref) all[2] = rest_of_head(sum[0].v, same, 0.0f, op_sum), all[3] = rest_of_head(sum[0].sr, same, 0.0f, op_sum);
+    }
+    for (int k = 0; k < K && !kRuns; ++k) {
       if (!((here >> k) & 1)) continue;
       float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -603,9 +651,9 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         for (int q = 0; q < 4; ++q) all[q] = u[q];
     }
     team_join<G, 4, kOne>(all, op_sum, reds);
-    // lane k finishes head k; the row's numbers are sums over its heads
+    // one lane finishes a head; the row's numbers are sums over its heads
     const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
-    const bool use = active && h.some;
+    const bool use = active && h.some && keeps;
     float logpi = use ? (a < 0 ? -INFINITY : kLn2 * (Rel(mm[0])(za) - h.ls)) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
     bool on = use;
     if (kOne) {  // (lane 0 of each wave has the action)
@@ -621,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     }
     const RowGrad g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
     const HeadGrad hg(g, h, mm[0], mm[1]);
-    const int target = on && a >= 0 ? (kOne ? 0 : my_off) + a : -(1 << 30);
+    const int target = (kRuns || on) && a >= 0 ? (kOne ? 0 : my_off) + a : -(1 << 30);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       if (!any(i)) continue;
@@ -631,12 +679,15 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       int to = target;
       bool live = on;
       if (!kOne) {
-        f.m = Rel(__shfl(mm[0], head[i], kWidth));
-        f.mr = Rel(__shfl(mm[1], head[i], kWidth));
-        f.ls = __shfl(hg.ls, head[i], kWidth);
-        f.k0 = __shfl(hg.k0, head[i], kWidth);
-        to = __shfl(target, head[i], kWidth);
-        live = __shfl(static_cast<int>(on), head[i], kWidth) != 0;
+        if (!kRuns) {
+          f.m = Rel(of_head(mm[0], i));
+          f.mr = Rel(of_head(mm[1], i));
+          to = of_head(target, i);
+        }
+        f.ls = of_head(hg.ls, i);
+        f.k0 = of_head(hg.k0, i);
+        live = of_head(static_cast<int>(on), i) != 0;
+        to = live ? to : -(1 << 30);
       }
       float out[V];
       if (!live) {
