@@ -12,7 +12,7 @@
 // they add, the block joins these in LDS, and each wave finishes its steps from the
 // state that enters them, with the gates still in registers.  Long sequences of
 // few channels are cut into segments: one launch forms what each segment leaves and
-// adds, one joins them, and one runs the segments.
+// adds, one joins them if they are many, and one runs the segments.
 //
 // w = 1 - a is formed without the cancellation near a = 1, and the state is
 // taken on as h - w h: a rounded to 24 bits would be off by 2^-25 of itself in
@@ -42,7 +42,7 @@ struct Rec {  // a launch's arrays; the states' pointers are those of its first 
   const uint8_t* reset;
   float *hT, *marks, *dh0, *part;
   float *keep, *add;  // [segments - 1, states]: what a segment leaves of a state (-1: cut off), and what it adds
-  float* enter;       // [segments - 1, states]: the states that enter segments 1, 2, ...
+  float* enter;       // [segments - 1, states]: the states that enter segments 1, 2, ..., or NULL: keep and add give them
   uint64_t states;    // B D of the whole call
   int T, B, nb, D, len;  // len: steps of a segment
   float c;
@@ -170,6 +170,13 @@ __device__ __forceinline__ void state_out(float* p, uint32_t at, float a, float 
   *reinterpret_cast<f2_t*>(p + at) = f2_t{a, b};
 }
 
+// A segment's effect on a state.
+__device__ __forceinline__ float pass(float keep, float add, float h) { return keep < 0.0f ? add : fmaf(keep, h, add); }
+__device__ __forceinline__ f2_t pass(const Rec& p, uint64_t seg, uint32_t at, f2_t h) {
+  const f2_t keep = state_in(p.keep + seg * p.states, at), add = state_in(p.add + seg * p.states, at);
+  return f2_t{pass(keep[0], add[0], h[0]), pass(keep[1], add[1], h[1])};
+}
+
 // The inputs of U steps; those from `end` on repeat the last and are not used.
 template <typename E, int U>
 struct Steps {
@@ -200,11 +207,12 @@ __global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
   const int begin = seg * p.len, end = min(begin + p.len, p.T);
   f2_t h = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
   bool whole = true;
-  if (!kSum) {
-    if (seg > 0)
-      h = state_in(p.enter + (seg - 1) * p.states, l.at);
-    else if (p.h0)
-      h = state_in(p.h0, l.at);
+  if (!kSum && seg > 0 && p.enter) {
+    h = state_in(p.enter + (seg - 1) * p.states, l.at);
+  } else if (!kSum) {
+    if (p.h0) h = state_in(p.h0, l.at);
+#pragma unroll 4
+    for (uint64_t s = 0; s < seg; ++s) h = pass(p, s, l.at, h);
   }
   Steps<E, U> next;
   next.load(p, x_at, r_at, i_at, l.b, begin, end);
@@ -236,9 +244,6 @@ __global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
     state_out(p.hT, l.at, h[0], h[1]);
   }
 }
-
-// A segment's effect on a state.
-__device__ __forceinline__ float pass(float keep, float add, float h) { return keep < 0.0f ? add : fmaf(keep, h, add); }
 
 // The states that enter the segments behind the first, from the one that
 // enters the first (forward), or those that enter the ones before the last from
@@ -519,10 +524,13 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
   const uint64_t seg = blockIdx.y, segs = gridDim.y;
   const int begin = seg * p.len, end = min(begin + p.len, p.T);
   f2_t G = {0.0f, 0.0f}, sum = {0.0f, 0.0f};
-  if (seg + 1 < segs)
+  if (seg + 1 < segs && p.enter) {
     G = state_in(p.enter + seg * p.states, l.at);
-  else if (p.dhT)
-    G = state_in(p.dhT, l.at);
+  } else {
+    if (p.dhT) G = state_in(p.dhT, l.at);
+#pragma unroll 4
+    for (uint64_t s = segs - 1; s-- > seg;) G = pass(p, s, l.at, G);
+  }
   Steps<E, kMark> next;
   Pair<E> next_dh[kMark];
   f2_t next_h;
@@ -762,10 +770,19 @@ void run_blocks(const Rec& all, size_t most_ld, int waves, void (*kernel)(Rec), 
   });
 }
 
-void join(const Rec& p, const Cut& c, const float* first, bool back, hipStream_t s) {
-  const uint64_t blocks = (p.states + 63) / 64;  // (few: a call of many states is not cut)
-  hipLaunchKernelGGL(gatedrec_join, dim3(static_cast<unsigned>(blocks)), dim3(1024), 0, s, p.keep, p.add, first, p.enter,
-                     c.segments - 1, p.states, back);
+// The states that enter the segments; few segments are passed by the launch that
+// runs them (T = 300, B = 32, D = 2048 backward, 3 of them: 81 us, with a launch for it
+// 87; T = 2000, B = 4, 31 of them: 74 and 77).
+constexpr int kFewSegments = 32;
+
+void join(Rec* p, const Cut& c, const float* first, bool back, hipStream_t s) {
+  if (c.segments <= kFewSegments) {
+    p->enter = nullptr;
+    return;
+  }
+  const uint64_t blocks = (p->states + 63) / 64;  // (few: a call of many states is not cut)
+  hipLaunchKernelGGL(gatedrec_join, dim3(static_cast<unsigned>(blocks)), dim3(1024), 0, s, p->keep, p->add, first, p->enter,
+                     c.segments - 1, p->states, back);
 }
 
 }  // namespace
@@ -814,7 +831,7 @@ extern "C" int o5_gatedrec_fwd(o5_dtype dt, int T, int B, int D, const void* x, 
   }
   if (cut.segments > 1) {
     run_lanes(all, most, cut.segments - 1, bf16 ? gatedrec_fwd<uint16_t, true> : gatedrec_fwd<float, true>, as_stream(stream));
-    join(all, cut, h0, false, as_stream(stream));
+    join(&all, cut, h0, false, as_stream(stream));
   }
   run_lanes(all, most, cut.segments, bf16 ? gatedrec_fwd<uint16_t, false> : gatedrec_fwd<float, false>, as_stream(stream));
   return check_launch(fn);
@@ -863,7 +880,7 @@ extern "C" int o5_gatedrec_bwd(o5_dtype dt, int T, int B, int D, const void* x, 
   } else {
     if (cut.segments > 1) {
       run_lanes(all, most, cut.segments - 1, bf16 ? gatedrec_back_sum<uint16_t> : gatedrec_back_sum<float>, as_stream(stream));
-      join(all, cut, dhT, true, as_stream(stream));
+      join(&all, cut, dhT, true, as_stream(stream));
     }
     run_lanes(all, most, cut.segments, bf16 ? gatedrec_bwd<uint16_t> : gatedrec_bwd<float>, as_stream(stream));
   }
