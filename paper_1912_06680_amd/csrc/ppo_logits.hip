@@ -18,8 +18,12 @@
 // A team of lanes takes a row and holds it in registers, 16 bytes of a head's
 // logits and of the reference's to a slot: everything is read once and written
 // once.  Rows too wide for that are read twice, the second time from a cache.
-// HBM-bound by its bytes; the 40 instructions an element, 3 exponentials among
-// them, take nearly as long.
+// HBM-bound by its bytes; the 32 instructions an element, 3 exponentials among
+// them, take nearly as long: 8192 rows of 32000 logits and a reference's in bf16,
+// 1573 MB, 330 us, 4.8 TB/s, with the vector units busy in 82 % of the cycles.  1003
+// rows of 50257 in fp32, which do not fit in a block's registers, 175 us.  Narrow rows are
+// bound by their 640 instructions for four rows: 32768 rows of 74 logits in 4 heads,
+// 17 MB, 16 us; 60 rows 9, most of it one row's chain of dependent steps.
 #include "heads.h"
 #include "reduce.h"
 
@@ -923,7 +927,20 @@ __global__ void __launch_bounds__(1024) logits_stats(int blocks, const double* _
   if (threadIdx.x == 0) write_stats(red[0], vf_coef, ent_coef, kl_coef, stats);
 }
 
-// How a call's rows are taken, by the slots of 16 bytes that a row has.
+// How a call's rows are taken, by the slots of 16 bytes that a row has.  Narrow
+// rows in teams of 16 lanes, whose reductions cost four steps for four rows at once;
+// wider ones in as few lanes as hold them, up to a block.  Times in us of one head and of
+// two, in bf16, in the form taken and, after the stroke, in the next one:
+//
+//   30000 x 74 in 4 heads (one slot a lane) 17.5 | 22     10000 x 1700 37, 46 | 53, 64
+//   20000 x 220 (two)  17, 18 | 30, 33                    6000 x 3600  47, 56 | 50, 68
+//   20000 x 400 (four) 22, 27 | 29, 33 in whole waves     4000 x 7000  50, 65 | 54, 118
+//   20000 x 900 40, 48 | 44, 59                           2000 x 15000 52, 89 | 58, 106
+//   8192 x 32000 334 | 438
+//
+// (eight slots in 16 lanes: 20000 x 900 38, 81, 5000 x 500 in fp32 17, in whole waves 15).
+// Rows of one head that a block does not hold keep 8 slots a lane and read the others
+// twice: 1003 x 50257 in fp32 178, read twice as a whole 192, 2000 x 128000 430 and 445.
 struct Form {
   int teams, threads, blocks;  // teams and threads of a block, blocks at most
   void (*kernel)(Loss);
@@ -932,9 +949,10 @@ struct Form {
 template <typename E, int G, int I, bool kOne, bool kTiny = false, bool kAvail = true, bool kMore = false>
 Form slots_form(int N) {
   constexpr int kThreads = G < 256 ? 256 : G;
-  // a few rows: one block takes them all and writes the statistics too
+  // a few rows: one block takes them all and writes the statistics too (60 rows of 74: 9.8 us, in two launches 11.6)
   if constexpr (G < 256)
     if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, 1024>};
+  // (blocks: 32768 rows of 74 with 1024 22.5 us, with 2048 23.4; 30000 of 10 17.1 and 18.4)
   return {kThreads / G, kThreads, (G == 16 ? 1024 : 2048) * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, kThreads>};
 }
 template <typename E, int G, int I>
@@ -956,7 +974,7 @@ Form form_of(int N, const HeadsMeta& hm, bool avail) {
   if (hm.A < V) return one ? slots_form<E, 16, 1, true, true>(N) : slots_form<E, 16, 1, false, true>(N);
   if (slots <= 16) return slots_form<E, 16, 1>(N, one);
   if (slots <= 32) return slots_form<E, 16, 2>(N, one);
-  if (slots <= 64) return slots_form<E, 64, 1>(N, one);
+  if (slots <= 64) return slots_form<E, 16, 4>(N, one);
   if (slots <= 128) return slots_form<E, 64, 2>(N, one);
   if (slots <= 256) return slots_form<E, 64, 4>(N, one);
   if (slots <= 512) return slots_form<E, 256, 2>(N, one);

@@ -124,6 +124,8 @@ CASES = [
     (70, (700,), True, True, True, False, True),
     (5, (9000, 5), True, True, True, True, False),
     (3, (20000,), False, False, True, False, False),
+    (77, (3, 1, 9, 2, 1, 8, 5, 4), True, True, True, True, True),
+    (1030, (40, 2, 6), False, True, True, True, True),
 ]
 
 
