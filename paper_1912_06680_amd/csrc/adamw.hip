@@ -313,7 +313,8 @@ __device__ __forceinline__ void step8(const Tensor& t, uint32_t index, const Con
 // bytes each, 541 to 615 us, 5.0 to 4.4 TB/s; 5.3M with 32-bit moments 27 us, 5.9 TB/s
 // (partly from the caches).
 // kClip: the gradients are taken times clip[1]; where that is 0 nothing
-// changes.
+// changes.  168M with 32-bit moments and bf16 copies, 28 bytes each, 750 us, 6.3 TB/s;
+// scaling the gradients in a pass of its own would move 4 bytes more.
 template <bool kClip>
 __global__ void __launch_bounds__(256) adamw_kernel(const void* __restrict__ plan, uint32_t tensors, uint32_t first,
                                                     Consts c, const float* __restrict__ clip) {
@@ -451,7 +452,8 @@ __device__ __forceinline__ double block_sum(double s) {
 constexpr uint32_t kNormBlocks = 2048;
 
 // A block takes its share of the chunks, which lie one after another in a
-// tensor.
+// tensor.  HBM-bound: 168M bf16 gradients 35 to 65 us (partly from the cache, 9.7 to
+// 5.2 TB/s); 5.3M in fp32 with the join of the blocks 9 us, two launches.
 __global__ void __launch_bounds__(256) grad_squares(const void* __restrict__ plan, uint32_t tensors, uint32_t chunks,
                                                     double* __restrict__ part) {
   const uint32_t b = blockIdx.x, nb = gridDim.x;

@@ -19,11 +19,11 @@
 // logits and of the reference's to a slot: everything is read once and written
 // once.  Rows too wide for that are read twice, the second time from a cache.
 // HBM-bound by its bytes; the 32 instructions an element, 3 exponentials among
-// them, take nearly as long: 8192 rows of 32000 logits and a reference's in bf16,
-// 1573 MB, 330 us, 4.8 TB/s, with the vector units busy in 82 % of the cycles.  1003
-// rows of 50257 in fp32, which do not fit in a block's registers, 175 us.  Narrow rows are
-// bound by their 640 instructions for four rows: 32768 rows of 74 logits in 4 heads,
-// 17 MB, 16 us; 60 rows 9, most of it one row's chain of dependent steps.
+// them, take nearly as long: 8192 rows of 32000 logits and a reference's in bf16, a
+// tenth of them padding, 1.47 GB, 330 us, 4.5 TB/s, with the vector units busy in 82 %
+// of the cycles.  1003 rows of 50257 in fp32, which do not fit in a block's registers,
+// 175 us, 3.6 TB/s.  Narrow rows are bound by their 680 instructions for four rows: 32768
+// rows of 74 logits in 4 heads, 19 MB, 15.7 us; 60 of them in one block 9.8.
 #include "heads.h"
 #include "reduce.h"
 
