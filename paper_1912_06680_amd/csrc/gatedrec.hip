@@ -121,7 +121,7 @@ struct Decay {
 
 // What a step takes in, and its state from the one before: rounded the same in
 // every kernel (no product is joined with the sum), so that single tokens give
-// the bits of a sequence.
+// the bits of a sequence that is not cut.
 __device__ __forceinline__ float taken_in(float w, float o, float x) {
 #pragma clang fp contract(off)
   return __builtin_amdgcn_sqrtf(__builtin_fmaf(-w, w, w + w)) * (o * x);

@@ -211,6 +211,7 @@ class LinPolicy:
         """The loss and its gradient on the heads' input and parameters; with kl_coef held near the policy whose logits
         are ref [T B, A or more], fp32."""
         if self.kl_coef:
+            assert ref is not None, "kl_coef needs a reference policy's logits"
             z, dz, A = self.logits(), self.dz, sum(self.head_sizes)
             assert ref.dtype == torch.float32 and ref.dim() == 2 and ref.shape[0] == self.N and ref.shape[1] >= A
             assert ref.stride(1) == 1
