@@ -105,3 +105,48 @@ def test_logits_rows_far_apart(heads):
     assert torch.equal(dz, far[2])
     del wide, far
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("heads", [(1 << 24,), (5, (1 << 23) + 1, 3, 1 << 22)])
+def test_as_many_logits_as_there_may_be(heads):
+    """2^24 choices in one head, and nearly as many in several.
+
+    A probability here is 1e-7 and a sum over a head's has 2^23 terms of like size, added by lanes in runs of at most 2^14 and
+    joined in pairs: relative errors of 2^14 2^-24 = 1e-3 at the very most and, as errors of random sign, 2^7 2^-24 = 8e-6.  Of
+    log p, near -17, 1e-5 is allowed on top of an exponential's 2^-22 for each; of the gradient, relative to its largest,
+    (2^-14 + 2^-8)."""
+    need_gpu()
+    banner(f"ppo_logits of {sum(heads)} logits")
+    N, A, dt = 2, sum(heads), o5.O5_BF16
+    g = _gen(3)
+    z, y = (torch.randn((N, A), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    act = torch.stack([torch.randint(0, n, (N,), generator=g, device="cuda", dtype=torch.int32) for n in heads], 1).contiguous()
+    act[1, -1] = heads[-1] - 1
+    adv, w = torch.tensor([1.5, -0.5], device="cuda"), torch.tensor([0.25, 0.75], device="cuda")
+    logp = sum(torch.log_softmax(s.double(), -1).gather(1, act[:, k:k + 1].long())[:, 0]
+               for k, s in enumerate(z.split(heads, 1)))
+    kl = sum((s.double().softmax(-1) * (s.double().log_softmax(-1) - q.double().log_softmax(-1))).sum(-1)
+             for s, q in zip(z.split(heads, 1), y.split(heads, 1)))
+    old = (logp - 0.1).float()
+    stats, got_logp, got_kl = torch.empty(9, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    dz, ws = torch.full((N, A), 7.0, dtype=torch.bfloat16, device="cuda"), workspace(o5.o5_ppo_logits_grad_workspace_bytes(dt, N, heads))
+    o5.o5_ppo_logits_grad(dt, N, heads, z, A, y, A, act, old, adv, None, w, None, None, 0.2, 0.0, 0.0, 1.0, stats, got_logp, got_kl,
+                          dz, A, ws)
+    assert (got_logp.double() - logp).abs().max() <= len(heads) * (1e-5 + 17 * 2.0 ** -22)
+    assert (got_kl.double() - kl).abs().max() <= len(heads) * (1e-5 + 17 * 2.0 ** -22)
+    ratio = (logp - old.double()).exp()  # 1.1: inside the clip
+    at = 0
+    for k, n in enumerate(heads):
+        s, q = z[:, at:at + n].double(), y[:, at:at + n].double()
+        lp = s.log_softmax(-1)
+        d = lp - q.log_softmax(-1)
+        p = lp.exp()
+        ref = p * (ratio * adv.double())[:, None] + p * (d - (p * d).sum(-1, keepdim=True))
+        ref.scatter_add_(1, act[:, k:k + 1].long(), -(ratio * adv.double())[:, None])
+        ref *= w.double()[:, None]
+        got = dz[:, at:at + n].double()
+        others = torch.ones_like(ref, dtype=torch.bool).scatter_(1, act[:, k:k + 1].long(), False)
+        for m in (others, ~others):  # the action's is near 1, the others' near 1e-7
+            assert (got - ref)[m].abs().max() <= (2.0 ** -14 + 2.0 ** -8) * ref[m].abs().max()
+        at += n
+    torch.cuda.empty_cache()
