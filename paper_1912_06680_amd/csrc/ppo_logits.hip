@@ -936,9 +936,10 @@ __global__ void __launch_bounds__(1024) logits_stats(int blocks, const double* _
 //   20000 x 220 (two)  17, 18 | 30, 33                    6000 x 3600  47, 56 | 50, 68
 //   20000 x 400 (four) 22, 27 | 29, 33 in whole waves     4000 x 7000  50, 65 | 54, 118
 //   20000 x 900 40, 48 | 44, 59                           2000 x 15000 52, 89 | 58, 106
-//   8192 x 32000 334 | 438
+//   6000 x 2600 36, 46 | 41, 51                           8192 x 32000 334 | 438
 //
-// (eight slots in 16 lanes: 20000 x 900 38, 81, 5000 x 500 in fp32 17, in whole waves 15).
+// (eight slots in 16 lanes: 20000 x 900 38, 81, 5000 x 500 in fp32 17, in whole waves 15;
+// four in 128: 6000 x 3600 44, 55, 5000 x 1719 in eight heads in fp32 53, two in 256 51).
 // Rows of one head that a block does not hold keep 8 slots a lane and read the others
 // twice: 1003 x 50257 in fp32 178, read twice as a whole 192, 2000 x 128000 430 and 445.
 struct Form {
@@ -948,9 +949,9 @@ struct Form {
 
 template <typename E, int G, int I, bool kOne, bool kTiny = false, bool kAvail = true, bool kMore = false>
 Form slots_form(int N) {
-  constexpr int kThreads = G < 256 ? 256 : G;
+  constexpr int kThreads = G <= 64 ? 256 : G;  // (waves of a team meet at barriers, which are a block's)
   // a few rows: one block takes them all and writes the statistics too (60 rows of 74: 9.8 us, in two launches 11.6)
-  if constexpr (G < 256)
+  if constexpr (G <= 64)
     if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, 1024>};
   // (blocks: 32768 rows of 74 with 1024 22.5 us, with 2048 23.4; 30000 of 10 17.1 and 18.4)
   return {kThreads / G, kThreads, (G == 16 ? 1024 : 2048) * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, kThreads>};
@@ -977,6 +978,7 @@ Form form_of(int N, const HeadsMeta& hm, bool avail) {
   if (slots <= 64) return slots_form<E, 16, 4>(N, one);
   if (slots <= 128) return slots_form<E, 64, 2>(N, one);
   if (slots <= 256) return slots_form<E, 64, 4>(N, one);
+  if (slots <= 384) return slots_form<E, 128, 3>(N, one);
   if (slots <= 512) return slots_form<E, 256, 2>(N, one);
   if (slots <= 1024) return slots_form<E, 256, 4>(N, one);
   if (slots <= 2048) return one ? wide_form<E, 256>(N, avail) : slots_form<E, 512, 4, false>(N);

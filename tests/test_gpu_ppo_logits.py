@@ -126,6 +126,9 @@ CASES = [
     (3, (20000,), False, False, True, False, False),
     (77, (3, 1, 9, 2, 1, 8, 5, 4), True, True, True, True, True),
     (1030, (40, 2, 6), False, True, True, True, True),
+    (41, (1500,), True, True, True, False, True),
+    (23, (1200, 130, 1), True, True, True, True, True),
+    (23, (2500, 300), False, True, False, True, True),
 ]
 
 
@@ -143,7 +146,7 @@ def test_loss_and_gradient(bf16, case):
     assert torch.equal(stats, out[0]) and torch.equal(dz, out[1])
 
 
-@pytest.mark.parametrize("N,heads", [(33000, (3, 5)), (9000, (300,)), (2100, (2500,)), (530, (70000, 2))])
+@pytest.mark.parametrize("N,heads", [(33000, (3, 5)), (9000, (300,)), (2100, (2500,)), (4200, (2000, 600)), (530, (70000, 2))])
 def test_more_rows_than_the_chip_takes_at_once(N, heads):
     need_gpu()
     banner(f"ppo_logits {N} rows of {heads}")
