@@ -629,12 +629,10 @@ __global__ void __launch_bounds__(1024) gatedrec_rows(size_t n, size_t row, int 
 __global__ void __launch_bounds__(1024) gatedrec_rates(size_t n, size_t row, int D, const float* __restrict__ part,
                                                        const float* __restrict__ lam, float* __restrict__ dlam) {
   const int d = blockIdx.x * 64 + (threadIdx.x & 63);
+  const float l = lam[min(d, D - 1)];  // (under way before the sums)
   const float s = column_sum(n, row, part + d, d < D);
-  if (threadIdx.x < 64 && d < D) {
-    // sigmoid(lam) / softplus(lam), which is 1 - e^lam / 2 + ... far to the left
-    const float e = expf(lam[d]);
-    dlam[d] = s * (lam[d] < -15.0f ? 1.0f - 0.5f * e : 1.0f / ((1.0f + expf(-lam[d])) * softplus(lam[d])));
-  }
+  // sigmoid(lam) / softplus(lam), which is 1 - e^lam / 2 + ... far to the left
+  if (threadIdx.x < 64 && d < D) dlam[d] = s * (l < -15.0f ? 1.0f - 0.5f * expf(l) : 1.0f / ((1.0f + expf(-l)) * softplus(l)));
 }
 
 // One step.  A lane keeps its channels, whose rates cost as much as ten steps, and
