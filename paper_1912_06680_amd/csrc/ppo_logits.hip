@@ -310,23 +310,29 @@ __device__ __forceinline__ float beyond(float d, float r) {
 }
 
 // The row's loss: the factors of its gradient, and, of the eight sums, the
-// row's part of number q.
+// row's parts of those that the lane keeps (kParts of them, where a team has fewer than
+// eight lanes).
+template <int kParts>
 __device__ __forceinline__ RowGrad row_loss(const Loss& p, const Row& r, float logpi, float ent, float kl, float kl_coef,
-                                            int q, double* part) {
+                                            int lane, double (&part)[kParts]) {
   const float dlog = logpi - r.old, ratio = exp2_of(dlog * kLog2e);
   const float cut = fminf(fmaxf(ratio, 1.0f - p.clip_eps), 1.0f + p.clip_eps);
   const float surr = fminf(ratio * r.adv, cut * r.adv);
   const bool flow = (r.adv >= 0.0f && ratio <= 1.0f + p.clip_eps) || (r.adv < 0.0f && ratio >= 1.0f - p.clip_eps);
   const float loss = -surr + p.vf_coef * r.err * r.err - p.ent_coef * ent + (kl_coef != 0.0f ? kl_coef * kl : 0.0f);
-  float x = -surr;
-  x = q == 1 ? r.err * r.err : x;
-  x = q == 2 ? ent : x;
-  x = q == 3 ? (fabsf(ratio - 1.0f) > p.clip_eps ? 1.0f : 0.0f) : x;
-  x = q == 4 ? beyond(dlog, ratio) : x;
-  x = q == 5 ? ratio : x;
-  x = q == 7 ? kl : x;
-  const double d = static_cast<double>(r.w) * x;
-  *part += q == 6 ? (isfinite(loss) ? 0.0 : 1.0) : d;
+#pragma unroll
+  for (int j = 0; j < kParts; ++j) {
+    const int q = lane % (kSums / kParts) + j * (kSums / kParts);
+    float x = -surr;
+    x = q == 1 ? r.err * r.err : x;
+    x = q == 2 ? ent : x;
+    x = q == 3 ? (fabsf(ratio - 1.0f) > p.clip_eps ? 1.0f : 0.0f) : x;
+    x = q == 4 ? beyond(dlog, ratio) : x;
+    x = q == 5 ? ratio : x;
+    x = q == 7 ? kl : x;
+    const double d = static_cast<double>(r.w) * x;
+    part[j] += q == 6 ? (isfinite(loss) ? 0.0 : 1.0) : d;
+  }
   return {flow ? -r.w * ratio * r.adv : 0.0f, r.w * p.ent_coef, r.w * kl_coef};
 }
 
@@ -337,18 +343,26 @@ __device__ __forceinline__ void write_stats(const double* x, float vf_coef, floa
   for (int k = 0; k < kSums; ++k) stats[k + 1] = static_cast<float>(x[k]);
 }
 
-// The block's sums, of which lane q of each team has the team's number q; a
-// call's only block writes the statistics itself.
-template <int G, int kThreads>
-__device__ __forceinline__ void block_sums(const Loss& p, double part) {
-  constexpr int kTeams = kThreads / G;
-  __shared__ double sums[kTeams][kSums];
-  const int team = threadIdx.x / G, lane = threadIdx.x % G;
-  if (lane < kSums) sums[team][lane] = part;
+// The block's sums, of which lane q of each team has the team's numbers q, q + G,
+// ...; a call's only block writes the statistics itself.
+template <int G, int kThreads, int kParts>
+__device__ __forceinline__ void block_sums(const Loss& p, double (&part)[kParts]) {
+  constexpr int kWaves = kThreads / 64;
+  __shared__ double sums[kWaves][kSums];
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < kParts; ++j) {
+#pragma unroll
+    for (int d = G; d < 64; d *= 2) part[j] += __shfl_xor(part[j], d);
+    if (lane < kSums / kParts) sums[threadIdx.x >> 6][lane + j * G] = part[j];
+  }
   __syncthreads();
+  // (a team of several waves has its numbers in the first)
+  constexpr int kStep = G > 64 ? G / 64 : 1;
   double s = 0.0;
   if (threadIdx.x < kSums) {
-    for (int k = 0; k < kTeams; ++k) s += sums[k][threadIdx.x];
+#pragma unroll
+    for (int k = 0; k < kWaves; k += kStep) s += sums[k][threadIdx.x];
     if (gridDim.x > 1) p.part[static_cast<size_t>(blockIdx.x) * kSums + threadIdx.x] = s;
   }
   if (gridDim.x > 1) return;
@@ -369,12 +383,14 @@ __device__ __forceinline__ float moved(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true));
 }
 
-// Over a row of 16 lanes or a wave, the result in each lane, in a fixed order.
+// Over 4, 8 or a row of 16 lanes or a wave, the result in each lane, in a fixed order.
 template <int G, class Op>
 __device__ __forceinline__ float lanes_reduce(float v, float id, Op op) {
   if (G > 16) return wave_reduce(v, id, op);
   v = op(v, moved<0xB1>(v));    // quad_perm [1, 0, 3, 2]
   v = op(v, moved<0x4E>(v));    // quad_perm [2, 3, 0, 1]
+  if (G == 4) return v;
+  if (G == 8) return op(v, moved<0x141>(v));  // row_half_mirror
   v = op(v, moved<0x124>(v));   // row_ror 4
   return op(v, moved<0x128>(v));  // row_ror 8
 }
@@ -477,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     return Span<E>((i * G + l) * V, A - (i * G + l) * V, A);
   };
   const int my_off = p.heads.off[mine], my_size = p.heads.off[mine + 1] - my_off;
-  double part = 0.0;
+  double part[G < kSums ? kSums / G : 1] = {};
   // whether any of the wave's lanes has a slot i
   const int wave_lane = __builtin_amdgcn_readfirstlane(lane & ~63);
   const auto any = [&](int i) {
@@ -671,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       ent = lanes_reduce<G>(ent, 0.0f, op_sum);
       kl = lanes_reduce<G>(kl, 0.0f, op_sum);
     }
-    const RowGrad g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
+    const RowGrad g = row_loss(p, r, logpi, ent, kl, kl_coef, lane, part);
     const HeadGrad hg(g, h, mm[0], mm[1]);
     const int target = (kRuns || on) && a >= 0 ? (kOne ? 0 : my_off) + a : -(1 << 30);
 #pragma unroll
@@ -760,7 +776,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
   const int lane = threadIdx.x, hl = lane & 63, K = p.heads.K, A = p.heads.A;
   const bool ref = p.has_ref != 0, some = p.has_avail != 0;
   const float kl_coef = p.kl_coef;
-  double part = 0.0;
+  double part[1] = {};
   for (int64_t n = blockIdx.x; n < p.N; n += gridDim.x) {
     const E* z = static_cast<const E*>(p.z) + n * p.ldz;
     const E* y = static_cast<const E*>(p.y) + n * p.ldy;
@@ -848,7 +864,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
     const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : kLn2 * (Rel(m)(za) - h.ls)) : 0.0f, 0.0f, op_sum);
     const float ent = wave_reduce(use ? h.S : 0.0f, 0.0f, op_sum), kl = wave_reduce(use ? h.D : 0.0f, 0.0f, op_sum);
     RowGrad g = {0.0f, 0.0f, 0.0f};
-    if (!r.pad) g = row_loss(p, r, logpi, ent, kl, kl_coef, lane % kSums, &part);
+    if (!r.pad) g = row_loss(p, r, logpi, ent, kl, kl_coef, lane, part);
     const HeadGrad hg(g, h, m, mr);
     for (int k = 0; k < K; ++k) {
       const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
@@ -928,10 +944,11 @@ __global__ void __launch_bounds__(1024) logits_stats(int blocks, const double* _
 }
 
 // How a call's rows are taken, by the slots of 16 bytes that a row has.  Narrow
-// rows in teams of 16 lanes, whose reductions cost four steps for four rows at once;
+// rows in teams of 4, 8 or 16 lanes, whose reductions cost two to four steps for all of a wave's rows;
 // wider ones in as few lanes as hold them, up to a block.  Times in us of one head and of
 // two, in bf16, in the form taken and, after the stroke, in the next one:
 //
+//   300000 x 18 (four lanes) 26 | 80 in 16                30000 x 60 (eight) 14 | 16 in 16
 //   30000 x 74 in 4 heads (one slot a lane) 17.5 | 22     10000 x 1700 37, 46 | 53, 64
 //   20000 x 220 (two)  17, 18 | 30, 33                    6000 x 3600  47, 56 | 50, 68
 //   20000 x 400 (four) 22, 27 | 29, 33 in whole waves     4000 x 7000  50, 65 | 54, 118
@@ -953,8 +970,8 @@ Form slots_form(int N) {
   // a few rows: one block takes them all and writes the statistics too (60 rows of 74: 9.8 us, in two launches 11.6)
   if constexpr (G <= 64)
     if (N > kThreads / G && N <= 1024 / G) return {1024 / G, 1024, 1, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, 1024>};
-  // (blocks: 32768 rows of 74 with 1024 22.5 us, with 2048 23.4; 30000 of 10 17.1 and 18.4)
-  return {kThreads / G, kThreads, (G == 16 ? 1024 : 2048) * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, kThreads>};
+  // (blocks: 32768 rows of 74 with 1024 22.5 us, with 2048 23.4; 300000 of 18 26.1 and 27.4, with 512 31.4)
+  return {kThreads / G, kThreads, (G <= 16 ? 1024 : 2048) * 256 / kThreads, logits_slots<E, G, I, kOne, kTiny, kAvail, kMore, kThreads>};
 }
 template <typename E, int G, int I>
 Form slots_form(int N, bool one) {
@@ -972,7 +989,9 @@ Form form_of(int N, const HeadsMeta& hm, bool avail) {
   int slots = 0;
   for (int k = 0; k < hm.K; ++k) slots += (hm.off[k + 1] - hm.off[k] + V - 1) / V;
   const bool one = hm.K == 1;
-  if (hm.A < V) return one ? slots_form<E, 16, 1, true, true>(N) : slots_form<E, 16, 1, false, true>(N);
+  if (hm.A < V) return one ? slots_form<E, 4, 1, true, true>(N) : slots_form<E, 16, 1, false, true>(N);
+  if (slots <= 4 && one) return slots_form<E, 4, 1, true>(N);
+  if (slots <= 8 && one) return slots_form<E, 8, 1, true>(N);
   if (slots <= 16) return slots_form<E, 16, 1>(N, one);
   if (slots <= 32) return slots_form<E, 16, 2>(N, one);
   if (slots <= 64) return slots_form<E, 16, 4>(N, one);

@@ -126,6 +126,11 @@ CASES = [
     (3, (20000,), False, False, True, False, False),
     (77, (3, 1, 9, 2, 1, 8, 5, 4), True, True, True, True, True),
     (1030, (40, 2, 6), False, True, True, True, True),
+    (300, (10,), True, True, True, True, True),
+    (5000, (3,), False, True, True, False, True),
+    (1500, (30,), True, True, True, True, True),
+    (1100, (61,), False, True, False, True, True),
+    (70, (13,), True, False, True, False, False),
     (41, (1500,), True, True, True, False, True),
     (23, (1200, 130, 1), True, True, True, True, True),
     (23, (2500, 300), False, True, False, True, True),
@@ -146,7 +151,7 @@ def test_loss_and_gradient(bf16, case):
     assert torch.equal(stats, out[0]) and torch.equal(dz, out[1])
 
 
-@pytest.mark.parametrize("N,heads", [(33000, (3, 5)), (9000, (300,)), (2100, (2500,)), (4200, (2000, 600)), (530, (70000, 2))])
+@pytest.mark.parametrize("N,heads", [(33000, (3, 5)), (140000, (12,)), (70000, (40,)), (9000, (300,)), (2100, (2500,)), (4200, (2000, 600)), (530, (70000, 2))])
 def test_more_rows_than_the_chip_takes_at_once(N, heads):
     need_gpu()
     banner(f"ppo_logits {N} rows of {heads}")
@@ -158,7 +163,7 @@ def test_more_rows_than_the_chip_takes_at_once(N, heads):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("spare", [(0, 0, 0), (1, 2, 3), (8, 16, 24), (5, 1, 0)])
-@pytest.mark.parametrize("heads", [(4099,), (17, 600), (33,)])
+@pytest.mark.parametrize("heads", [(4099,), (17, 600), (33,), (11,)])
 def test_strides(bf16, heads, spare):
     """The same numbers whatever the rows' strides and alignments."""
     need_gpu()
@@ -185,7 +190,7 @@ def test_gradient_against_differences(heads):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("heads", [(9, 4), (300, 70), (5000, 3), (20000,)])
+@pytest.mark.parametrize("heads", [(9, 4), (14,), (300, 70), (5000, 3), (20000,)])
 def test_what_masks_hide_may_hold_anything(bf16, heads):
     """NaN and infinities in padded rows and in unavailable logits reach nothing; rows without a choice, impossible actions."""
     need_gpu()
@@ -210,7 +215,7 @@ def test_what_masks_hide_may_hold_anything(bf16, heads):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("heads", [(9, 4), (300, 70), (5000,), (20000,)])
+@pytest.mark.parametrize("heads", [(9, 4), (14,), (300, 70), (5000,), (20000,)])
 def test_extreme_logits(bf16, heads):
     """-infinity, the type's lowest and largest values, offsets of 1e4, choices that only one of the policies excludes."""
     need_gpu()
