@@ -20,7 +20,7 @@
 // once.  Rows too wide for that are read twice, the second time from a cache.
 // HBM-bound by its bytes; the 32 instructions an element, 3 exponentials among
 // them, take nearly as long: 8192 rows of 32000 logits and a reference's in bf16, a
-// tenth of them padding, 1.47 GB, 330 us, 4.5 TB/s, with the vector units busy in 82 %
+// tenth of them padding, 1.47 GB, 335 us, 4.4 TB/s, with the vector units busy in 82 %
 // of the cycles.  1003 rows of 50257 in fp32, which do not fit in a block's registers,
 // 175 us, 3.6 TB/s.  Narrow rows are bound by their 680 instructions for four rows: 32768
 // rows of 74 logits in 4 heads, 19 MB, 15.7 us; 60 of them in one block 9.8.
@@ -185,44 +185,35 @@ struct Span {
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 
-// Logits relative to the largest, m, in binary logs: z -> fma(z, scale, shift).
-// The shift's rounding is the same for all and goes out of every difference.
-// Beyond 2^120, where binary logs overflow, different floats are 2^96 apart and
-// any scale tells them apart.
-struct Rel {
-  float scale, shift;
-  __device__ __forceinline__ Rel() = default;
-  __device__ __forceinline__ explicit Rel(float m) {
-    scale = fabsf(m) < 0x1p120f ? kLog2e : 0x1p-80f;
-    shift = -m * scale;
-  }
-  __device__ __forceinline__ float operator()(float z) const { return fmaf(z, scale, shift); }
-};
+// Sums and probabilities are of z - m, rounded to 2^-24 of itself and 0 for the largest logit wherever it
+// lies.  (One instruction more than fma(z, log2 e, -m log2 e), whose rounding of m log2 e is no longer small
+// beside 1 from |m| = 1e7 on, and overflows e^(z-m) from 2^31 on.)
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(kLog2e * d); }
 // What goes from sums relative to `from` to sums relative to the larger `to`.
-__device__ __forceinline__ float between(float from, float to) { return fmaxf((from - to) * kLog2e, kLowest); }
+__device__ __forceinline__ float between(float from, float to) { return fmaxf(from - to, kLowest); }
 
-// The sums of a head's logits, relative to m and mr, in binary logs.
+// The sums of a head's logits, relative to m and mr.
 struct Sums {
   float s, t, v, sr;
-  __device__ __forceinline__ void add(float z, const Rel& m) {
-    const float d = m(z), e = exp2_of(d);
+  __device__ __forceinline__ void add(float z, float m) {
+    const float d = z - m, e = exp_of(d);
     s += e;
     t += times(e, d);
   }
-  __device__ __forceinline__ void add(float z, const Rel& m, float y, const Rel& mr) {
-    const float d = m(z), e = exp2_of(d), dy = mr(y);
+  __device__ __forceinline__ void add(float z, float m, float y, float mr) {
+    const float d = z - m, e = exp_of(d), dy = y - mr;
     s += e;
     t += times(e, d);
     v += times(e, dy);
-    sr += exp2_of(dy);
+    sr += exp_of(dy);
   }
   // From m, mr to mn, mrn.
   __device__ __forceinline__ void move(float m, float mr, float mn, float mrn) {
-    const float d = between(m, mn), dr = between(mr, mrn), f = exp2_of(d);
+    const float d = between(m, mn), dr = between(mr, mrn), f = exp_of(d);
     t = times(f, t + times(s, d));
     s *= f;
     v = times(f, v) + times(s, dr);
-    sr *= exp2_of(dr);
+    sr *= exp_of(dr);
   }
 };
 
@@ -236,34 +227,34 @@ struct HeadStats {
     const float inv = __builtin_amdgcn_rcpf(x.s);
     ls = __builtin_amdgcn_logf(x.s);
     lsr = __builtin_amdgcn_logf(x.sr);
-    S = kLn2 * (ls - x.t * inv);
-    D = ref ? fmaf(kLn2 * (x.t - x.v), inv, log_of(x.sr * inv)) : 0.0f;
+    S = fmaf(kLn2, ls, -x.t * inv);
+    D = ref ? fmaf(x.t - x.v, inv, log_of(x.sr * inv)) : 0.0f;
   }
 };
 
 // What the row gives its heads' gradients, and a head's p_j (kd d + ky dy + k0)
-// of a logit d and the reference's dy in binary logs, with p_j = 2^(d - ls).
+// of d = z - m and the reference's dy, with log p_j = d - log s.
 struct RowGrad {
   float pg, ent, kl;
 };
 struct HeadGrad {
-  Rel m, mr;
-  float ls, kd, ky, k0;
+  float m, mr, ls, kd, ky, k0;
   __device__ __forceinline__ HeadGrad() = default;
   __device__ __forceinline__ HeadGrad(const RowGrad& g, const HeadStats& h, float m_, float mr_) : m(m_), mr(mr_) {
     ls = h.ls;
-    kd = kLn2 * (g.ent + g.kl);
-    ky = -kLn2 * g.kl;
+    kd = g.ent + g.kl;
+    ky = -g.kl;
     k0 = fmaf(g.ent, fmaf(-kLn2, h.ls, h.S), -g.pg);
     if (g.kl != 0.0f) k0 = fmaf(g.kl, kLn2 * (h.lsr - h.ls) - h.D, k0);
   }
+  __device__ __forceinline__ float p(float d) const { return exp2_of(fmaf(d, kLog2e, -ls)); }
   __device__ __forceinline__ float operator()(float z) const {
-    const float d = m(z);
-    return times(exp2_of(d - ls), fmaf(kd, d, k0));
+    const float d = z - m;
+    return times(p(d), fmaf(kd, d, k0));
   }
   __device__ __forceinline__ float operator()(float z, float y) const {
-    const float d = m(z);
-    return times(exp2_of(d - ls), fmaf(kd, d, fmaf(ky, mr(y), k0)));
+    const float d = z - m;
+    return times(p(d), fmaf(kd, d, fmaf(ky, y - mr, k0)));
   }
 };
 
@@ -590,13 +581,12 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
         more_m[1] = mn[1];
         zx.hold();
         yx.hold();
-        const Rel to_m(mn[0]), to_mr(mn[1]);
         if (ref)
 #pragma unroll
-          for (int q = 0; q < V; ++q) more.add(zx[q], to_m, yx[q], to_mr);
+          for (int q = 0; q < V; ++q) more.add(zx[q], mn[0], yx[q], mn[1]);
         else
 #pragma unroll
-          for (int q = 0; q < V; ++q) more.add(zx[q], to_m);
+          for (int q = 0; q < V; ++q) more.add(zx[q], mn[0]);
       }
     // the largest
     constexpr int J = kOne ? 1 : I;
@@ -635,7 +625,6 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const float m = kOne || kRuns ? mm[0] : of_head(mm[0], i), mr = kOne || kRuns ? mm[1] : of_head(mm[1], i);
-      const Rel to_m(m), to_mr(mr);
       if (!kOne || i == 0) {
         sum[i] = more;
         if (kMore) sum[i].move(more_m[0], more_m[1], m, mr);
@@ -646,10 +635,10 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       ys[i].hold();
       if (ref)
 #pragma unroll
-        for (int q = 0; q < V; ++q) to.add(zs[i][q], to_m, ys[i][q], to_mr);
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], m, ys[i][q], mr);
       else
 #pragma unroll
-        for (int q = 0; q < V; ++q) to.add(zs[i][q], to_m);
+        for (int q = 0; q < V; ++q) to.add(zs[i][q], m);
     }
     float all[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (kRuns) {
@@ -674,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
     // one lane finishes a head; the row's numbers are sums over its heads
     const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some && keeps;
-    float logpi = use ? (a < 0 ? -INFINITY : kLn2 * (Rel(mm[0])(za) - h.ls)) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
+    float logpi = use ? (a < 0 ? -INFINITY : fmaf(-kLn2, h.ls, za - mm[0])) : 0.0f, ent = use ? h.S : 0.0f, kl = use ? h.D : 0.0f;
     bool on = use;
     if (kOne) {  // (lane 0 of each wave has the action)
       logpi = __shfl(logpi, 0, kWidth);
@@ -700,8 +689,8 @@ __global__ void __launch_bounds__(kThreads, !kOne && I > 2 && kThreads < 1024 ? 
       bool live = on;
       if (!kOne) {
         if (!kRuns) {
-          f.m = Rel(of_head(mm[0], i));
-          f.mr = Rel(of_head(mm[1], i));
+          f.m = of_head(mm[0], i);
+          f.mr = of_head(mm[1], i);
           to = of_head(target, i);
         }
         f.ls = of_head(hg.ls, i);
@@ -824,17 +813,16 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
         s.move(mk[0], mk[1], mn[0], mn[1]);
         mk[0] = mn[0];
         mk[1] = mn[1];
-        const Rel to_m(mk[0]), to_mr(mk[1]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           zs[u].hold();
           ys[u].hold();
           if (ref)
 #pragma unroll
-            for (int q = 0; q < V; ++q) s.add(zs[u][q], to_m, ys[u][q], to_mr);
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0], ys[u][q], mk[1]);
           else
 #pragma unroll
-            for (int q = 0; q < V; ++q) s.add(zs[u][q], to_m);
+            for (int q = 0; q < V; ++q) s.add(zs[u][q], mk[0]);
         }
       }
       float mm[2];
@@ -861,7 +849,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
     }
     const HeadStats h({all[0], all[1], all[2], all[3]}, ref);
     const bool use = active && h.some;
-    const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : kLn2 * (Rel(m)(za) - h.ls)) : 0.0f, 0.0f, op_sum);
+    const float logpi = wave_reduce(use ? (a < 0 ? -INFINITY : fmaf(-kLn2, h.ls, za - m)) : 0.0f, 0.0f, op_sum);
     const float ent = wave_reduce(use ? h.S : 0.0f, 0.0f, op_sum), kl = wave_reduce(use ? h.D : 0.0f, 0.0f, op_sum);
     RowGrad g = {0.0f, 0.0f, 0.0f};
     if (!r.pad) g = row_loss(p, r, logpi, ent, kl, kl_coef, lane, part);
@@ -869,8 +857,8 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
     for (int k = 0; k < K; ++k) {
       const int o = p.heads.off[k], size = p.heads.off[k + 1] - o;
       HeadGrad f;
-      f.m = Rel(__shfl(m, k));
-      f.mr = Rel(__shfl(mr, k));
+      f.m = __shfl(m, k);
+      f.mr = __shfl(mr, k);
       f.ls = __shfl(hg.ls, k);
       f.k0 = __shfl(hg.k0, k);
       f.kd = hg.kd;
