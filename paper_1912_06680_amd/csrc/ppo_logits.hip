@@ -863,7 +863,7 @@ __global__ void __launch_bounds__(kWide) logits_stream(Loss p) {
       f.k0 = __shfl(hg.k0, k);
       f.kd = hg.kd;
       f.ky = hg.ky;
-      const int target = __shfl(a < 0 ? -(1 << 30) : a + p.heads.off[min(hl, K - 1)], k);
+      const int target = __shfl(use && a >= 0 ? a + p.heads.off[min(hl, K - 1)] : -(1 << 30), k);
       const bool live = __shfl(static_cast<int>(use), k) != 0;
       for (int j0 = lane * V; j0 < size; j0 += kWide * V * U) {
         Slot<E> zs[U], ys[U];

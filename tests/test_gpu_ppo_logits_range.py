@@ -104,3 +104,30 @@ class Wide(base.Case):
 def test_what_masks_hide_where_rows_are_read_twice(monkeypatch, bf16, heads):
     monkeypatch.setattr(base, "Case", Wide)
     base.test_what_masks_hide_may_hold_anything(bf16, heads)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("avail", [False, True])
+@pytest.mark.parametrize("heads", [(2, 3), (14,), (9, 4), (300, 70), (2600, 5), (9000, 5), (9000, 9000), (40000, 3), (3, 40000), (70000,)],
+                         ids=lambda h: "_".join(map(str, h)))
+def test_a_head_of_infinities_adds_nothing(bf16, avail, heads):
+    """A head whose available logits are all -infinity is as one without a choice, also where its action could be one."""
+    need_gpu()
+    banner(f"ppo_logits heads of -infinity bf16={bf16} avail={avail} {heads}")
+    c = Wide(bf16, 9, heads, avail=avail, seed=14)
+    at, dead = 0, []
+    for k, n in enumerate(heads):
+        for row in ((1, 4) if k % 2 == 0 else (2, 4)):
+            c.z[row, at:at + n] = -float("inf")
+            dead.append((row, slice(at, at + n)))
+        at += n
+    out = c.run()
+    c.check(out, ppo_logits_grad(**c.args()))
+    for row, cols in dead:
+        assert not out[1][row, cols].any()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("heads", [(70000,), (140000,), (40000, 3), (9000, 9000)], ids=lambda h: "_".join(map(str, h)))
+def test_extreme_logits_where_rows_are_read_twice(bf16, heads):
+    base.test_extreme_logits(bf16, heads)
