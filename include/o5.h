@@ -647,7 +647,8 @@ int o5_linattn_step(o5_dtype dt, int B, int nh, int nkv, int dk, int dv,
  * x, r, i  row t*B + b at x + (t*B + b)*ldx; row strides ld* in elements:
  *          multiples of 8, at least D and below 2^31, so that x, r and i may
  *          be parts of one wider buffer.   h: the same.
- * lam      [D] fp32, finite (not checked).   c: > 0 and finite.
+ * lam      [D] fp32, finite (not checked; a NaN makes its channel's states NaN).
+ *          c: > 0 and finite.
  * h0       [B, D] fp32, the states before the first step, or NULL (= 0).
  *          hT: out, the states after the last step, or NULL.
  * reset    [T, B] uint8 or NULL (no resets): nonzero cuts the carried state

@@ -98,7 +98,7 @@ __device__ __forceinline__ float softplus(float x) {
   y = fmaf(q, y, 1.0f / 5.0f);
   y = fmaf(q, y, 1.0f / 3.0f);
   y = fmaf(q, y, 1.0f);
-  return fmaxf(x, 0.0f) + 2.0f * s * y;
+  return (x < 0.0f ? 0.0f : x) + 2.0f * s * y;  // (a NaN stays one: the state of a lost rate must not look like one that is kept)
 }
 __device__ __forceinline__ float rate_of(float c, float lam) {
   const float rate = c * softplus(lam);
