@@ -17,7 +17,8 @@
 // w = 1 - a is formed without the cancellation near a = 1, and the state is
 // taken on as h - w h: a rounded to 24 bits would be off by 2^-25 of itself in
 // every step, which over the 1/w steps that a state lasts grows to 2^-25 / w.
-// beta is sqrt(w (2 - w)).
+// Away from 1 it is taken on as a h, since 1 - w keeps nothing of a small a, to
+// which the gates' and the rates' gradients are proportional.  beta is sqrt(w (2 - w)).
 //
 // HBM-bound by its bytes, with 38 instructions an element forward, 6 of them at half
 // rate, that keep the vector units busy for 70 to 80 % of the time.  bf16, D = 4096 unless
@@ -105,41 +106,49 @@ __device__ __forceinline__ float rate_of(float c, float lam) {
   return rate > kMost ? kMost : rate;  // (a NaN stays one)
 }
 
-// 1 - 2^-y and 2^-y of y >= 0: below 0.3 binary logs of e a polynomial, 2e-8 of
-// the value off (a minimax fit), where the difference would be 3e-7 off.
+// The decay a = 2^-y, y >= 0, as one number that keeps the last digits of a and of w = 1 - a:
+// w, below 0.3 binary logs of e a polynomial, 2e-8 of the value off (a minimax fit; the
+// difference would be 3e-7 off), and from there on -a, told by its sign.
 struct Decay {
-  float w, a;
+  float s;
+  bool near;
   __device__ __forceinline__ explicit Decay(float y) {
-    a = __builtin_amdgcn_exp2f(-y);
-    float s = fmaf(y, 0x1.34893cp-10f, -0x1.3941b2p-7f);
-    s = fmaf(y, s, 0x1.c69daep-5f);
-    s = fmaf(y, s, -0x1.ebfb9ep-3f);
-    s = fmaf(y, s, 0x1.62e430p-1f);
-    w = y < 0.3f * kLog2e ? y * s : 1.0f - a;
+    const float a = __builtin_amdgcn_exp2f(-y);
+    float q = fmaf(y, 0x1.34893cp-10f, -0x1.3941b2p-7f);
+    q = fmaf(y, q, 0x1.c69daep-5f);
+    q = fmaf(y, q, -0x1.ebfb9ep-3f);
+    q = fmaf(y, q, 0x1.62e430p-1f);
+    near = y < 0.3f * kLog2e;
+    s = near ? y * q : -a;
   }
+  __device__ __forceinline__ Decay(float s_, bool near_) : s(s_), near(near_) {}
+  __device__ __forceinline__ float a() const { return near ? 1.0f - s : -s; }
+  __device__ __forceinline__ float beta2() const { return __builtin_fmaf(-s, s, near ? s + s : 1.0f); }  // 1 - a^2
+  __device__ __forceinline__ float carried(float h) const { return __builtin_fmaf(-s, h, near ? h : 0.0f); }  // a h
 };
+__device__ __forceinline__ Decay kept(float s) { return Decay(s, __float_as_int(s) >= 0); }  // (-0 is an a of 0)
 
 // What a step takes in, and its state from the one before: rounded the same in
 // every kernel (no product is joined with the sum), so that single tokens give
 // the bits of a sequence that is not cut.
-__device__ __forceinline__ float taken_in(float w, float o, float x) {
+__device__ __forceinline__ float taken_in(float beta2, float o, float x) {
 #pragma clang fp contract(off)
-  return __builtin_amdgcn_sqrtf(__builtin_fmaf(-w, w, w + w)) * (o * x);
+  return __builtin_amdgcn_sqrtf(beta2) * (o * x);
 }
-__device__ __forceinline__ float next_state(float h, float w, float v) {
+__device__ __forceinline__ float next_state(float h, const Decay& a, float v) {
 #pragma clang fp contract(off)
-  return __builtin_fmaf(-w, h, h) + v;
+  return a.carried(h) + v;
 }
 __device__ __forceinline__ float next_state(float h, float y, float i, float x) {  // y: the decay in binary logs
-  const float w = Decay(y).w;
-  return next_state(h, w, taken_in(w, sigmoid2(i), x));
+  const Decay a(y);
+  return next_state(h, a, taken_in(a.beta2(), sigmoid2(i), x));
 }
 
 // One step's gradients, from G, that of its state.
 struct Grad {
   float dx, dr, di, e;  // e = G d(log a) log a
-  __device__ __forceinline__ Grad(float G, float rate, float x, float g, float o, float w, float before) {
-    const float v = fmaf(-w, w, w + w), a = 1.0f - w;
+  __device__ __forceinline__ Grad(float G, float rate, float x, float g, float o, const Decay& d, float v, float before) {
+    const float a = d.a();
     // 1 / beta; log a / beta goes to 0 with log a
     const float ib = v < 0x1p-126f ? 0.0f : __builtin_amdgcn_rsqf(v);
     e = G * (a * (-rate * g) * fmaf(-a * ib, o * x, before));
@@ -353,16 +362,17 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_fwd_block(Rec p) {
   int buf = 0;
   for (int c0 = 0; c0 < end; c0 += round, buf ^= 1) {
     const int t0 = c0 + wave * U;
-    float w[U], v[U], e = 0.0f, y = 0.0f;
+    float s[U], v[U], e = 0.0f, y = 0.0f;
     const uint32_t off = cut;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const bool there = t0 + k < end;
       const float yk = there ? rate * sigmoid2(r[k]) : 0.0f;
-      w[k] = Decay(yk).w;
-      v[k] = there ? taken_in(w[k], sigmoid2(i[k]), x[k]) : 0.0f;
+      const Decay d(yk);
+      s[k] = d.s;
+      v[k] = there ? taken_in(d.beta2(), sigmoid2(i[k]), x[k]) : 0.0f;
       if ((off >> k) & 1) e = 0.0f;
-      e = next_state(e, w[k], v[k]);
+      e = next_state(e, d, v[k]);
       y += yk;
     }
     if (c0 + round < end) fetch(t0 + round);
@@ -377,7 +387,7 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_fwd_block(Rec p) {
     for (int k = 0; k < U; ++k) {
       if (t0 + k >= end) break;
       if ((off >> k) & 1) in = 0.0f;
-      in = next_state(in, w[k], v[k]);
+      in = next_state(in, kept(s[k]), v[k]);
       if (l.on) put<E>(p.h, t0 + k, h_at, in);
     }
     if (p.hT && t0 + U >= p.T && l.on) p.hT[l.at] = in;
@@ -398,7 +408,7 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_bwd_block(Rec p) {
   int buf = 0;
   for (int c0 = (end - 1) / round * round; c0 >= 0; c0 -= round, buf ^= 1) {
     const int t0 = c0 + wave * U;
-    float x[U], g[U], o[U], dh[U], w[U], before[U];
+    float x[U], g[U], o[U], dh[U], s[U], beta2[U], before[U];
     uint32_t cut = 0;
     float h = p.marks[(min(t0, end - 1) / kMark) * p.states + l.at];
 #pragma unroll
@@ -421,8 +431,10 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_bwd_block(Rec p) {
       before[k] = h;
       g[k] = sigmoid2(g[k]);
       o[k] = sigmoid2(o[k]);
-      w[k] = Decay(kLog2e * l.rate[0] * g[k]).w;
-      h = next_state(h, w[k], taken_in(w[k], o[k], x[k]));
+      const Decay d(kLog2e * l.rate[0] * g[k]);
+      s[k] = d.s;
+      beta2[k] = d.beta2();
+      h = next_state(h, d, taken_in(beta2[k], o[k], x[k]));
     }
     float e = 0.0f, y = 0.0f;
     bool open = true;
@@ -430,7 +442,7 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_bwd_block(Rec p) {
     for (int k = U - 1; k >= 0; --k) {
       if (t0 + k >= end) continue;
       e += dh[k];
-      e = fmaf(-w[k], e, e);
+      e = kept(s[k]).carried(e);
       y += g[k];
       if ((cut >> k) & 1) {
         e = 0.0f;
@@ -446,9 +458,10 @@ __global__ void __launch_bounds__(64 * kWavesOf) gatedrec_bwd_block(Rec p) {
 #pragma unroll
     for (int k = U - 1; k >= 0; --k) {
       if (t0 + k >= end) continue;
-      const Grad d(in += dh[k], l.rate[0], x[k], g[k], o[k], w[k], before[k]);
+      const Decay a = kept(s[k]);
+      const Grad d(in += dh[k], l.rate[0], x[k], g[k], o[k], a, beta2[k], before[k]);
       sum += d.e;
-      in = (cut >> k) & 1 ? 0.0f : fmaf(-w[k], in, in);
+      in = (cut >> k) & 1 ? 0.0f : a.carried(in);
       if (l.on) {
         put<E>(p.dx, t0 + k, dx_at, d.dx);
         put<E>(p.dr, t0 + k, dr_at, d.dr);
@@ -506,7 +519,7 @@ __global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
         const float y = rate[j] * sigmoid2(r[k][j]);
         sum[j] += y;
         G[j] += d[k][j];
-        G[j] = fmaf(-Decay(y).w, G[j], G[j]);
+        G[j] = Decay(y).carried(G[j]);
       }
       if (cut[k]) {
         G = f2_t{0.0f, 0.0f};
@@ -557,7 +570,7 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
     for (int k = 0; k < kMark; ++k) dh[k] = next_dh[k];
     f2_t h = next_h;
     fetch(max(t0 - kMark, begin));
-    float before[kMark][2], g[kMark][2], o[kMark][2], w[kMark][2];
+    float before[kMark][2], g[kMark][2], o[kMark][2], decay[kMark][2], beta2[kMark][2];
 #pragma unroll
     for (int k = 0; k < kMark; ++k) {
       if (s.cut[k]) h = f2_t{0.0f, 0.0f};
@@ -566,8 +579,10 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
         before[k][j] = h[j];
         g[k][j] = sigmoid2(s.r[k][j]);
         o[k][j] = sigmoid2(s.i[k][j]);
-        w[k][j] = Decay(kLog2e * l.rate[j] * g[k][j]).w;
-        h[j] = next_state(h[j], w[k][j], taken_in(w[k][j], o[k][j], s.x[k][j]));
+        const Decay d(kLog2e * l.rate[j] * g[k][j]);
+        decay[k][j] = d.s;
+        beta2[k][j] = d.beta2();
+        h[j] = next_state(h[j], d, taken_in(beta2[k][j], o[k][j], s.x[k][j]));
       }
     }
 #pragma unroll
@@ -577,12 +592,13 @@ __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         G[j] += dh[k][j];
-        const Grad d(G[j], l.rate[j], s.x[k][j], g[k][j], o[k][j], w[k][j], before[k][j]);
+        const Decay a = kept(decay[k][j]);
+        const Grad d(G[j], l.rate[j], s.x[k][j], g[k][j], o[k][j], a, beta2[k][j], before[k][j]);
         dx[j] = d.dx;
         dr[j] = d.dr;
         di[j] = d.di;
         sum[j] += d.e;
-        G[j] = fmaf(-w[k][j], G[j], G[j]);
+        G[j] = a.carried(G[j]);
       }
       if (s.cut[k]) G = f2_t{0.0f, 0.0f};
       store<E>(p.dx, t0 + k, dx_at, dx[0], dx[1]);
