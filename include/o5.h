@@ -784,7 +784,9 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
  *          o5_adamw_grad_norm_workspace_bytes(plan) bytes (0 for no plan).
  * o5_adamw_step_clipped  o5_adamw_step on clip[1] g in place of g (clip from
  *          device memory, as o5_adamw_grad_norm left it); where clip[1] is 0 the step
- *          is left out: p, p_bf16 and the moments stay as they are.
+ *          is left out: p, p_bf16 and the moments stay as they are.  The next step
+ *          then has the same `step`: the bias corrections go by the steps that the
+ *          moments have seen.
  * o5_adamw_moments  the values of the moments, as a checkpoint holds them: m,
  *          v out, fp32; tensor k starts at the sum of the earlier tensors'
  *          n, each rounded up to 256 (the gaps are not written).

@@ -56,7 +56,8 @@ class LinPolicy:
 
     D: width, a multiple of 64; heads: of D / heads, a multiple of 8 up to 128 (linattn only); head_sizes: of the action
     heads.  core: "linattn" or "gatedrec".  kl_coef: of the divergence from a reference policy, whose logits train_step then
-    takes.  max_norm: the largest global norm of a step's gradients (self.clip: its norm and factor), or None.
+    takes.  max_norm: the largest global norm of a step's gradients (self.clip: its norm and factor), or None.  A step whose
+    norm is not finite is left out: weights and moments stay, and self.step_count does not count it.
 
     self.S0 holds the blocks' states before the segments, zeros at first.  To train on the segments that follow, copy
     self.ST into it, with zeros where the last step's `dones` is set: a segment's resets begin at its second step.
@@ -70,7 +71,7 @@ class LinPolicy:
         self.N, self.d = T * B, D // heads
         self.bf16 = dtype == "bf16"
         self.dt, self.et = (o5.O5_BF16, torch.bfloat16) if self.bf16 else (o5.O5_F32, torch.float32)
-        self.dev, self.lr, self.seed, self.step_count = device, lr, seed, 0
+        self.dev, self.lr, self.seed = device, lr, seed
         self.scale = self.d ** -0.5
         self.decay = _decays(heads, device)
         A1 = sum(self.head_sizes) + 1
@@ -111,6 +112,9 @@ class LinPolicy:
             size = (self.dt, T, B, heads, heads, self.d, self.d)
             need = max(o5.o5_linattn_fwd_workspace_bytes(*size), o5.o5_linattn_bwd_workspace_bytes(*size))
         self.clip = torch.zeros(2, **f32)
+        self._steps, self._open = 0, False  # (open: whether the last of them was left out is not known yet)
+        if max_norm is not None:
+            self._factor, self._known = torch.zeros(1, pin_memory=True), torch.cuda.Event()
         if kl_coef:
             self.dz, self.logp, self.kl = torch.empty((N, A1), **f32), torch.empty(N, **f32), torch.empty(N, **f32)
             self.ones = torch.ones((1, N), **f32)
@@ -238,13 +242,33 @@ class LinPolicy:
         self.forward(x, self.reset)
         self.loss(act, logp_old, self.adv_s, self.ret_s, ref=ref)
         self.backward(self.reset)
-        self.step_count += 1
         hp = (self.lr, 0.9, 0.999, 1e-8, 5.0)
         if self.max_norm is None:
+            self.step_count += 1
             o5.o5_adamw_step(self.plan, self.plan_dev, *hp, self.seed, self.step_count)
+            return
+        o5.o5_adamw_grad_norm(self.plan, self.plan_dev, self.max_norm, self.clip, self.ws)
+        if torch.cuda.is_current_stream_capturing():  # (a captured step keeps its number)
+            self._steps += 1
         else:
-            o5.o5_adamw_grad_norm(self.plan, self.plan_dev, self.max_norm, self.clip, self.ws)
-            o5.o5_adamw_step_clipped(self.plan, self.plan_dev, *hp, self.clip, self.seed, self.step_count)
+            self.step_count += 1  # (waits for the norm before this one, with all of this step but its update enqueued)
+            self._factor.copy_(self.clip[1:], non_blocking=True)
+            self._known.record()
+            self._open = True
+        o5.o5_adamw_step_clipped(self.plan, self.plan_dev, *hp, self.clip, self.seed, self._steps)
+
+    @property
+    def step_count(self):
+        """Optimizer steps taken so far, without those that were left out; with max_norm it waits for the last step's norm."""
+        if self._open:
+            self._known.synchronize()
+            self._open = False
+            self._steps -= int(self._factor.item() == 0.0)
+        return self._steps
+
+    @step_count.setter
+    def step_count(self, n):
+        self._steps, self._open = n, False
 
     # --------------------------------------------------------------- rollout
     def new_states(self):
