@@ -131,3 +131,29 @@ def test_a_head_of_infinities_adds_nothing(bf16, avail, heads):
 @pytest.mark.parametrize("heads", [(70000,), (140000,), (40000, 3), (9000, 9000)], ids=lambda h: "_".join(map(str, h)))
 def test_extreme_logits_where_rows_are_read_twice(bf16, heads):
     base.test_extreme_logits(bf16, heads)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("heads", HEADS, ids=lambda h: "_".join(map(str, h)))
+def test_a_reference_near_by(bf16, heads):
+    """KL of 1e-5 to 1e-2 a head, to what the terms of its sums hold.
+
+    KL = sum p (d - dy) + log(sr / s), with d and dy what the logits lie below the largest, 10 on the average over p for these
+    (ln A and less): each product and the two sums are off by 4e-6 of themselves at most in the worst case, but p's errors are
+    the ones that log(sr / s) has with the other sign, so that 4 roundings to 2^-24 of 10 are left, 2.4e-6 a head; 4e-6 with
+    log2's and the reciprocal's."""
+    need_gpu()
+    banner(f"ppo_logits near reference bf16={bf16} {heads}")
+    c = base.Case(bf16, 24, heads, seed=15)
+    g = np.random.Generator(np.random.PCG64(16))
+    near = torch.from_numpy(g.standard_normal((24, c.A)).astype(np.float32)).cuda()
+    for n in range(24):
+        # (bf16 has neighbours of a logit at 2^-8 of it; in fp32 the reference as near as 1e-5 of KL)
+        c.y[n] = (c.z[n, :c.A].float() + (0.005, 0.02, 0.08)[n % 3] * near[n]).to(c.et)
+    _, _, _, r_kl = ppo_logits_grad(**c.args())
+    kl = host(c.run()[3])
+    worst = float(np.max(np.abs(kl - r_kl)))
+    print(f"    kl: {worst:.2e} of {np.min(r_kl):.1e} to {np.max(r_kl):.1e}", flush=True)
+    assert worst <= len(heads) * 4e-6
+    # a KL of 0 would not pass, where there is more than one choice
+    assert max(heads) == 1 or np.max(r_kl) > 8 * len(heads) * 4e-6
