@@ -779,8 +779,9 @@ int o5_resnorm_bwd(o5_dtype xt, o5_dtype dt, int N, int D, const void* xo,
  *          max_norm / norm) (max_norm > 0, infinity for the norm alone) that
  *          clips them to max_norm: clip out [2] fp32 = (norm, factor).  The
  *          factor is 0 where the norm is not finite, as with an infinity or a
- *          NaN in any gradient, and positive otherwise.  The gradients stay
- *          as they are.  ws: scratch of
+ *          NaN in any gradient, and positive otherwise: 2^-126 at the least,
+ *          and that of the 64-bit norm where clip[0], rounded to fp32, is
+ *          infinite.  The gradients stay as they are.  ws: scratch of
  *          o5_adamw_grad_norm_workspace_bytes(plan) bytes (0 for no plan).
  * o5_adamw_step_clipped  o5_adamw_step on clip[1] g in place of g (clip from
  *          device memory, as o5_adamw_grad_norm left it); where clip[1] is 0 the step

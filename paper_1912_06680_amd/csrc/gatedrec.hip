@@ -20,11 +20,11 @@
 // Away from 1 it is taken on as a h, since 1 - w keeps nothing of a small a, to
 // which the gates' and the rates' gradients are proportional.  beta is sqrt(w (2 - w)).
 //
-// HBM-bound by its bytes, with 38 instructions an element forward, 6 of them at half
+// HBM-bound by its bytes, with 39 instructions an element forward, 6 of them at half
 // rate, that keep the vector units busy for 70 to 80 % of the time.  bf16, D = 4096 unless
-// said: T = 256, B = 128 forward for training 248 us, 4.6 TB/s; B = 64 backward 202 us,
-// 4.8 TB/s; T = 10007, B = 1, D = 2048 forward 70 us, 2.3 TB/s, since a sequence cut in
-// segments computes every step twice; a token of 4096 samples 57 us, 4.7 TB/s; of one
+// said: T = 256, B = 128 forward for training 250 us, 4.6 TB/s; B = 64 backward 203 us,
+// 4.8 TB/s; T = 10007, B = 1, D = 2048 forward 72 us, 2.3 TB/s, since a sequence cut in
+// segments computes every step twice; a token of 4096 samples 56 us, 4.8 TB/s; of one
 // 6.2 us, which is the call and the launch.
 #include "common.h"
 
@@ -212,7 +212,7 @@ struct Steps {
 
 // Forward, two channels to a lane, over segment blockIdx.y.  kSum: only what the segment leaves of the
 // state that enters it, and what it adds.  Four steps are in flight while four are worked on
-// (T = 256, B = 128, D = 4096 248 us; eight 264; one channel to a lane is no faster).
+// (T = 256, B = 128, D = 4096 250 us; eight 264; one channel to a lane is no faster).
 template <typename E, bool kSum>
 __global__ void __launch_bounds__(256) gatedrec_fwd(Rec p) {
   constexpr int U = 4;
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(256) gatedrec_back_sum(Rec p) {
 // Backward, two channels to a lane, over segment blockIdx.y.  The steps between two marks are run forward
 // from the mark, which leaves the state before each step and its gates in
 // registers, then backward, while those before them are in flight (T = 256, B = 64,
-// D = 4096 202 us; fetched when they are needed 390).
+// D = 4096 203 us; fetched when they are needed 390).
 template <typename E>
 __global__ void __launch_bounds__(256) gatedrec_bwd(Rec p) {
   const Place<2> l(p, blockIdx.x * blockDim.x + threadIdx.x);
@@ -718,7 +718,7 @@ constexpr int kShort = 2 * kWavesOf * kMark;
 constexpr int kMostSegments = 512;
 constexpr long long kUnits = 256;  // compute units
 
-// Times in us, bf16, both sides measured.
+// Times in us, bf16, both sides measured (with two instructions a step less than it takes now: all up to 3 % longer).
 // - kLanes or more: each walks the whole sequence (T = 256, B = 32, D = 4096: forward 74, cut in two 98, in blocks
 //   99; backward 120, in blocks 141).  Half as many lanes are too few (B = 32, D = 2048: forward 72, in blocks 50).
 // - Fewer: short sequences in blocks, where a launch and a read of the inputs are saved (T = 256, B = 8, D = 1024:

@@ -18,12 +18,12 @@
 // A team of lanes takes a row and holds it in registers, 16 bytes of a head's
 // logits and of the reference's to a slot: everything is read once and written
 // once.  Rows too wide for that are read twice, the second time from a cache.
-// HBM-bound by its bytes; the 32 instructions an element, 3 exponentials among
+// HBM-bound by its bytes; the 33 instructions an element, 3 exponentials among
 // them, take nearly as long: 8192 rows of 32000 logits and a reference's in bf16, a
-// tenth of them padding, 1.47 GB, 335 us, 4.4 TB/s, with the vector units busy in 82 %
+// tenth of them padding, 1.47 GB, 337 us, 4.4 TB/s, with the vector units busy in 84 %
 // of the cycles.  1003 rows of 50257 in fp32, which do not fit in a block's registers,
-// 175 us, 3.6 TB/s.  Narrow rows are bound by their 680 instructions for four rows: 32768
-// rows of 74 logits in 4 heads, 19 MB, 15.7 us; 60 of them in one block 9.8.
+// 175 us, 3.6 TB/s.  Narrow rows are bound by their 690 instructions for four rows: 32768
+// rows of 74 logits in 4 heads, 19 MB, 15.8 us; 60 of them in one block 9.4.
 #include "heads.h"
 #include "reduce.h"
 
@@ -943,7 +943,8 @@ __global__ void __launch_bounds__(1024) logits_stats(int blocks, const double* _
 //   20000 x 900 40, 48 | 44, 59                           2000 x 15000 52, 89 | 58, 106
 //   6000 x 2600 36, 46 | 41, 51                           8192 x 32000 334 | 438
 //
-// (eight slots in 16 lanes: 20000 x 900 38, 81, 5000 x 500 in fp32 17, in whole waves 15;
+// (measured with one instruction a logit less than it takes now: both sides are up to 2 % longer;
+// eight slots in 16 lanes: 20000 x 900 38, 81, 5000 x 500 in fp32 17, in whole waves 15;
 // four in 128: 6000 x 3600 44, 55, 5000 x 1719 in eight heads in fp32 53, two in 256 51).
 // Rows of one head that a block does not hold keep 8 slots a lane and read the others
 // twice: 1003 x 50257 in fp32 178, read twice as a whole 192, 2000 x 128000 430 and 445.
